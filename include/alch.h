@@ -435,6 +435,94 @@ size_t alch_gemm_workspace_bytes(void);
 int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batch, const void* Q,
                            const void* K, const void* V, void* O, float* LSE, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------
+ * The two ends of a training step: the embedding rows in front of layer 0 (Section 4.1: the prefill starts
+ * from the token ids), their gradient behind dX_embed, and what is done with the gradients (Section 3: the
+ * weights are updated every iteration while they serve).
+ */
+
+/*
+ * alch_embed_forward: X[t] = scale * W_embed[token_ids[t]]; a token id outside 0..vocab-1 marks a position without
+ * a token (padding): its row is zero.
+ *   token_ids  device int32 [n_tokens], 4-byte aligned;  W_embed [vocab, hidden];  X [n_tokens, hidden] out
+ * The product is rounded once; scale = 1 copies the rows' bits.  Supported: n_tokens <= 2^30, hidden <= 2^20.
+ */
+int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids,
+                       const void* W_embed, float scale, void* X, void* hip_stream);
+
+/*
+ * alch_embed_backward: dW_embed[v] (+)= scale * sum over t with token_ids[t] = v of dX[t]; rows of dX whose token id
+ * is outside 0..vocab-1 are not read.
+ *   dX         [n_tokens, hidden], the dX_embed of a stack's backward
+ *   dW_embed   [vocab, hidden] out.  accumulate == 0: every row is written, zeros where no token has the id.
+ *              accumulate != 0: only rows of ids that occur are read and written (sum in fp32, one rounding), for
+ *              micro-batches and for a table shared with the head, whose dW_lm it may be.
+ *   workspace  alch_embed_backward_workspace_bytes() bytes, 16-byte aligned
+ * Sums are in fp32, in an order that the token ids alone determine: results repeat bit for bit.
+ */
+int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids,
+                        const void* dX, float scale, void* dW_embed, int32_t accumulate, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+size_t alch_embed_backward_workspace_bytes(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens);
+
+/* The tensors of the two calls below come as a table that the caller makes once, for as long as they stay where they
+ * are: a device array that the kernels read, and a host copy of the same values for validation and launch planning.
+ * Tensors are dense, of any number of elements (0 too: pointers may be NULL then), 2^40 elements in all, at most
+ * ALCH_MAX_TENSORS of them, each of its own type.  Memory that a call writes may not overlap other memory of the call,
+ * except where it says so. */
+#define ALCH_MAX_TENSORS 4096
+
+typedef struct {
+    const void* grad;
+    void* out;     /* grad itself (clipped in place), other memory, or NULL: counted in the norm only */
+    int64_t n;     /* elements */
+    int32_t dtype; /* alch_dtype of grad and out */
+    int32_t reserved;
+} alch_grad_tensor;
+
+/*
+ * alch_grad_clip: the 2-norm over all elements of all tensors, and the gradients scaled so that it does not exceed max_norm:
+ *   norm = sqrt(sum g^2);  factor = max_norm / norm where norm > max_norm, else 1;  out = factor * grad
+ * A norm that is no finite number (an infinity or NaN among the gradients) gives factor NaN: clipped gradients are NaN
+ * then, and alch_adamw_step leaves everything as it was.  The sum is held in 64 bits: finite gradients of any size have
+ * a finite sum (the norm is rounded to fp32 when it is written).
+ *   max_norm   >= 0; an infinity only measures
+ *   norm_out   device float [2] out: { norm, factor }, 4-byte aligned
+ *   workspace  alch_grad_clip_workspace_bytes() bytes, 16-byte aligned
+ */
+int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alch_grad_tensor* tensors_host, float max_norm,
+                   float* norm_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t alch_grad_clip_workspace_bytes(void);
+
+/* m, v and master are fp32 [n].  With master the update is made on it and param is its rounding (param is only written);
+ * without (NULL) param itself is updated and rounded. */
+typedef struct {
+    void* param;
+    const void* grad; /* of param's type */
+    float *master, *m, *v;
+    int64_t n;
+    float weight_decay;
+    int32_t dtype; /* alch_dtype of param and grad */
+} alch_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int32_t step;             /* of this update, the first one is 1 */
+    const float* schedule;    /* device float [2] or NULL: { lr, step } in place of the two above, read when the kernel runs, so that
+                                 a captured step can be replayed with other values */
+    const float* grad_factor; /* device float [1] or NULL: multiplies every gradient (norm_out + 1 of alch_grad_clip) */
+} alch_adamw;
+
+/*
+ * alch_adamw_step: one AdamW update of all tensors, in fp32:
+ *   g' = grad_factor * g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   w -= lr * (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay * w)
+ * If grad_factor is NaN or an infinity nothing is written.  0 <= beta < 1, eps >= 0.
+ * Records captured before the update are stale behind it: raise weights_version.
+ */
+int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* tensors_host,
+                    const alch_adamw* params, void* hip_stream);
+
 /*
  * Launch timing for benchmarks.  While enabled, the library brackets its main kernels with two
  * HIP events on the caller's stream; alch_trace_collect waits for them, writes up to max_records
@@ -448,7 +536,8 @@ int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batc
 typedef enum {
     ALCH_TRACE_GEMM_MFMA = 0, ALCH_TRACE_GEMM_GENERIC = 1, ALCH_TRACE_PACK_SCAN = 2,
     ALCH_TRACE_PACK_GATHER = 3, ALCH_TRACE_ATTN_BWD = 4, ALCH_TRACE_ATTN_FWD = 5,
-    ALCH_TRACE_ROW_OPS = 6, ALCH_TRACE_CROSS_ENTROPY = 7, ALCH_TRACE_LORA = 8
+    ALCH_TRACE_ROW_OPS = 6, ALCH_TRACE_CROSS_ENTROPY = 7, ALCH_TRACE_LORA = 8, ALCH_TRACE_EMBED = 9,
+    ALCH_TRACE_UPDATE = 10
 } alch_trace_kind;
 typedef struct {
     int32_t kind; /* alch_trace_kind */

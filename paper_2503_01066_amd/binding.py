@@ -91,8 +91,22 @@ class CTraceRecord(C.Structure):
     _fields_ = [("kind", C.c_int32), ("flops", C.c_double), ("bytes", C.c_double), ("ms", C.c_float)]
 
 
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("dtype", C.c_int32)]
+
+
+class CAdamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int32),
+                ("schedule", C.c_void_p), ("grad_factor", C.c_void_p)]
+
+
 TRACE_KINDS = ("gemm_mfma", "gemm_generic", "pack_scan", "pack_gather", "attn_bwd", "attn_fwd", "row_ops",
-               "cross_entropy", "lora")
+               "cross_entropy", "lora", "embed", "update")
 
 HOOK_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int)
 
@@ -187,6 +201,19 @@ def lib():
     L.alch_attention_forward.restype = C.c_int
     L.alch_attention_forward.argtypes = [C.POINTER(LayerShape), C.POINTER(CBatch), C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_void_p]
+    L.alch_embed_forward.restype = C.c_int
+    L.alch_embed_forward.argtypes = [C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p]
+    L.alch_embed_backward.restype = C.c_int
+    L.alch_embed_backward.argtypes = [C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int32,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]
+    L.alch_embed_backward_workspace_bytes.restype = C.c_size_t
+    L.alch_embed_backward_workspace_bytes.argtypes = [C.c_int, C.c_int32, C.c_int32, C.c_int32]
+    L.alch_grad_clip.restype = C.c_int
+    L.alch_grad_clip.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.alch_grad_clip_workspace_bytes.restype = C.c_size_t
+    L.alch_grad_clip_workspace_bytes.argtypes = []
+    L.alch_adamw_step.restype = C.c_int
+    L.alch_adamw_step.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(CAdamw), C.c_void_p]
     L.alch_trace_enable.argtypes = [C.c_int32]
     L.alch_trace_collect.argtypes = [C.POINTER(CTraceRecord), C.c_int32, C.POINTER(C.c_int32)]
     _PACK = C.cast(L.alch_capture_pack, C.c_void_p).value
@@ -605,6 +632,192 @@ def alch_attention_forward(shape, batch, Q, K, V, stream=None):
     _check(L.alch_attention_forward(C.byref(shape), C.byref(batch.c), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(LSE),
                                     _stream_handle(stream)))
     return O, LSE
+
+
+def _code(dtype):
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("dtype %s: bfloat16 or float32" % dtype)
+    return ALCH_BF16 if dtype == torch.bfloat16 else ALCH_F32
+
+
+def _check_dense(t, name, dtype, device, shape=None):
+    """A library call takes the address of a tensor alone: what else it assumes of it is checked here."""
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError("%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s%s" % (
+            name, dtype, "" if shape is None else " of shape %s" % (tuple(shape),), device, t.dtype, tuple(t.shape), t.device,
+            "" if t.is_contiguous() else ", not contiguous"))
+
+
+def _check_current(device, stream):
+    """Kernels go to the current device; a stream that is given belongs to it."""
+    if device.type != "cuda":
+        raise ValueError("tensors on %s" % device)
+    at = torch.cuda.current_device()
+    if device.index != at or (stream is not None and stream.device_index != at):
+        raise ValueError("tensors on %s%s, the current device is %d" % (device, "" if stream is None else ", a stream of %d" % stream.device_index, at))
+
+
+def _empty(shape, dtype, device, stream, fill=torch.empty):
+    """Memory of the stream that the call goes to: what was freed on another one may still be in use there, and what is freed
+    behind the call is not handed out elsewhere while it runs."""
+    if stream is None:
+        return fill(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return fill(shape, dtype=dtype, device=device)
+
+
+def embed_backward_workspace_bytes(dtype, vocab, hidden, n_tokens):
+    return lib().alch_embed_backward_workspace_bytes(_code(dtype), vocab, hidden, n_tokens)
+
+
+def alch_embed_forward(token_ids, W_embed, scale=1.0, X=None, stream=None):
+    """Returns X [n_tokens, hidden], X[t] = scale * W_embed[token_ids[t]] (token_ids int32 [n_tokens]; a zero row where the id
+    is no row of W_embed [vocab, hidden])."""
+    L = lib()
+    dev, (vocab, hidden), n = W_embed.device, W_embed.shape, token_ids.numel()
+    _check_current(dev, stream)
+    _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
+    _check_dense(W_embed, "W_embed", W_embed.dtype, dev)
+    if X is None:
+        X = _empty((n, hidden), W_embed.dtype, dev, stream)
+    else:
+        _check_dense(X, "X", W_embed.dtype, dev, (n, hidden))
+    _check(L.alch_embed_forward(_code(W_embed.dtype), vocab, hidden, n, _ptr(token_ids), _ptr(W_embed), scale, _ptr(X), _stream_handle(stream)))
+    return X
+
+
+def alch_embed_backward(token_ids, dX, vocab, scale=1.0, dW_embed=None, accumulate=False, workspace=None, stream=None):
+    """Returns dW_embed [vocab, hidden], dW_embed[v] (+)= scale * the sum of dX[t] over the tokens with id v.  accumulate: adds to
+    dW_embed, of which only the rows that occur are touched (the gradient of a head that shares the table, for one)."""
+    L = lib()
+    dev, (n, hidden) = dX.device, dX.shape
+    _check_current(dev, stream)
+    _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
+    _check_dense(dX, "dX", dX.dtype, dev)
+    if dW_embed is None:
+        dW_embed = _empty((vocab, hidden), dX.dtype, dev, stream, torch.zeros if accumulate else torch.empty)
+    else:
+        _check_dense(dW_embed, "dW_embed", dX.dtype, dev, (vocab, hidden))
+    code = _code(dX.dtype)
+    ws = workspace if workspace is not None else _empty((max(L.alch_embed_backward_workspace_bytes(code, vocab, hidden, n), 256),), torch.uint8, dev, stream)
+    _check_dense(ws, "workspace", torch.uint8, dev)
+    _check(L.alch_embed_backward(code, vocab, hidden, n, _ptr(token_ids), _ptr(dX), scale, _ptr(dW_embed), 1 if accumulate else 0, _ptr(ws),
+                                 ws.numel(), _stream_handle(stream)))
+    return dW_embed
+
+
+def _check_apart(ranges):
+    """ranges: (first byte, byte behind the last, written, name).  What is written overlaps nothing else."""
+    ranges = sorted(r for r in ranges if r[1] > r[0])
+    end, last = 0, None      # of the ranges before, the one that reaches furthest, and the written one that does
+    wend, wlast = 0, None
+    for a, b, written, name in ranges:
+        if a < (end if written else wend):
+            raise ValueError("%s overlaps %s" % (name, last if written else wlast))
+        if b > end:
+            end, last = b, name
+        if written and b > wend:
+            wend, wlast = b, name
+
+
+class _TensorTable:
+    """Pointers and lengths of many tensors: a host array for the library's checks, the same on the device for its kernels,
+    uploaded once.  Keeps the tensors, which must stay where they are."""
+
+    def _make(self, row, rows, device, keep):
+        self.n, self.device, self.keep = len(rows), device, keep
+        self.host = (row * max(self.n, 1))(*[row(*r) for r in rows])
+        self.host_ptr = C.addressof(self.host)
+        self.dev = torch.frombuffer(bytearray(C.string_at(self.host_ptr, C.sizeof(self.host))), dtype=torch.uint8).to(device)
+        self.dev_ptr = self.dev.data_ptr()
+
+
+def _bytes_of(t, written, name):
+    return (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), written, name)
+
+
+class GradList(_TensorTable):
+    """The tensors of alch_grad_clip.  outs: None (norm only), or per gradient the tensor its clipped values go to (the
+    gradient itself: in place) or None.  device: where a list without tensors belongs."""
+
+    def __init__(self, grads, outs=None, device="cuda"):
+        grads = list(grads)
+        outs = [None] * len(grads) if outs is None else list(outs)
+        if len(outs) != len(grads):
+            raise ValueError("%d outs for %d gradients" % (len(outs), len(grads)))
+        dev = grads[0].device if grads else torch.zeros(0, device=device).device
+        rows, ranges = [], []
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            _check_dense(g, "grads[%d]" % i, g.dtype, dev)
+            if o is not None:
+                _check_dense(o, "outs[%d]" % i, g.dtype, dev, g.shape)
+                ranges.append(_bytes_of(o, True, "outs[%d]" % i))
+            if o is None or o.data_ptr() != g.data_ptr():
+                ranges.append(_bytes_of(g, False, "grads[%d]" % i))
+            rows.append((g.data_ptr(), _ptr(o), g.numel(), _code(g.dtype), 0))
+        _check_apart(ranges)
+        self._make(GradTensor, rows, dev, (grads, outs))
+
+
+class AdamwList(_TensorTable):
+    """The tensors of alch_adamw_step: per parameter its gradient (same type), its fp32 moments m and v, in masters its fp32
+    master copy or None, and its weight decay (one number for all, or one each).  device: where a list without tensors belongs."""
+
+    def __init__(self, params, grads, m, v, masters=None, weight_decay=0.0, device="cuda"):
+        params = list(params)
+        n = len(params)
+        masters = [None] * n if masters is None else list(masters)
+        decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        lists = dict(grads=list(grads), m=list(m), v=list(v), masters=masters, weight_decay=decay)
+        for name, l in lists.items():
+            if len(l) != n:
+                raise ValueError("%d %s for %d parameters" % (len(l), name, n))
+        dev = params[0].device if params else torch.zeros(0, device=device).device
+        rows, ranges = [], []
+        for i, p in enumerate(params):
+            g, mi, vi, w = lists["grads"][i], lists["m"][i], lists["v"][i], masters[i]
+            _check_dense(p, "params[%d]" % i, p.dtype, dev)
+            _check_dense(g, "grads[%d]" % i, p.dtype, dev, p.shape)
+            ranges += [_bytes_of(p, True, "params[%d]" % i), _bytes_of(g, False, "grads[%d]" % i)]
+            for t, name in ((mi, "m"), (vi, "v")) + (((w, "masters"),) if w is not None else ()):
+                _check_dense(t, "%s[%d]" % (name, i), torch.float32, dev, p.shape)
+                ranges.append(_bytes_of(t, True, "%s[%d]" % (name, i)))
+            rows.append((p.data_ptr(), g.data_ptr(), _ptr(w), mi.data_ptr(), vi.data_ptr(), p.numel(), decay[i], _code(p.dtype)))
+        _check_apart(ranges)
+        self._make(AdamwTensor, rows, dev, (params, lists))
+
+
+def grad_clip_workspace_bytes():
+    return lib().alch_grad_clip_workspace_bytes()
+
+
+def alch_grad_clip(grads, max_norm, norm_out=None, workspace=None, stream=None):
+    """grads: a GradList.  Returns the device float tensor [2] {norm over all gradients, factor they were multiplied with};
+    norm_out[1:] is the grad_factor of alch_adamw_step."""
+    L = lib()
+    _check_current(grads.device, stream)
+    if norm_out is None:
+        norm_out = _empty((2,), torch.float32, grads.device, stream)
+    else:
+        _check_dense(norm_out, "norm_out", torch.float32, grads.device, (2,))
+    ws = workspace if workspace is not None else _empty((L.alch_grad_clip_workspace_bytes(),), torch.uint8, grads.device, stream)
+    _check_dense(ws, "workspace", torch.uint8, grads.device)
+    _check(L.alch_grad_clip(grads.n, grads.dev_ptr, grads.host_ptr, max_norm, _ptr(norm_out), _ptr(ws), ws.numel(), _stream_handle(stream)))
+    return norm_out
+
+
+def alch_adamw_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, schedule=None, grad_factor=None, stream=None):
+    """One AdamW update of an AdamwList, in place.  schedule: device float tensor [2] {lr, step} that is read when the kernel
+    runs, in place of lr and step (for captured steps).  grad_factor: device float tensor [1] that every gradient is multiplied
+    with; where it is NaN or infinite nothing changes."""
+    L = lib()
+    _check_current(tensors.device, stream)
+    if schedule is not None:
+        _check_dense(schedule, "schedule", torch.float32, tensors.device, (2,))
+    if grad_factor is not None:
+        _check_dense(grad_factor, "grad_factor", torch.float32, tensors.device, (1,))
+    p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
+    _check(L.alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), _stream_handle(stream)))
 
 
 def alch_trace_enable(on):

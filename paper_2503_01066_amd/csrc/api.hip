@@ -748,6 +748,28 @@ int launch_attn_bwd(const AttnArgs& a, hipStream_t stream) {
     return attn_mfma_supported(a) ? launch_attn_bwd_mfma(a, stream) : launch_attn_bwd_generic(a, stream);
 }
 
+// Number and lengths of a table's tensors; the rest is checked by the callers.
+template <typename Tensor>
+static int check_tensors(int32_t n, const Tensor* tensors, const Tensor* host) {
+    if (n < 0) return fail(ALCH_ERR_INVALID_ARG, "n_tensors %d", n);
+    if (n > ALCH_MAX_TENSORS) return fail(ALCH_ERR_UNSUPPORTED, "n_tensors %d > %d", n, ALCH_MAX_TENSORS);
+    if (n > 0 && (!tensors || !host)) return fail(ALCH_ERR_INVALID_ARG, "tensors / tensors_host is NULL");
+    if (reinterpret_cast<uintptr_t>(tensors) & 7u) return fail(ALCH_ERR_INVALID_ARG, "tensors is not 8-byte aligned");
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (host[i].n < 0) return fail(ALCH_ERR_SHAPE, "tensor %d has %lld elements", i, (long long)host[i].n);
+        if (host[i].n > (int64_t)1 << 40 || (total += host[i].n) > (int64_t)1 << 40)
+            return fail(ALCH_ERR_UNSUPPORTED, "more than 2^40 elements");
+        if (host[i].dtype != ALCH_F32 && host[i].dtype != ALCH_BF16) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: bad dtype %d", i, (int)host[i].dtype);
+    }
+    return ALCH_OK;
+}
+static int check_tensor_ptr(const void* p, int i, const char* name) {
+    if (!p) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: %s is NULL", i, name);
+    if (!aligned16(p)) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: %s is not 16-byte aligned", i, name);
+    return ALCH_OK;
+}
+
 }  // namespace alch
 
 using namespace alch;
@@ -1386,6 +1408,101 @@ int alch_layer_forward_from(const alch_layer_shape* shape, const alch_batch* bat
                             size_t workspace_bytes, void* hip_stream) {
     clear_error();
     return layer_forward_impl(shape, batch, seq_begin, X, w, Y, rec, workspace, workspace_bytes, hip_stream);
+}
+
+// ---- the two ends of a training step ---------------------------------------------------------
+
+static int check_embed(alch_dtype dtype, int vocab, int hidden, int n_tokens) {
+    if (dtype != ALCH_F32 && dtype != ALCH_BF16) return fail(ALCH_ERR_INVALID_ARG, "bad dtype %d", (int)dtype);
+    if (vocab <= 0 || hidden <= 0) return fail(ALCH_ERR_SHAPE, "non-positive vocab / hidden");
+    if (n_tokens < 0) return fail(ALCH_ERR_INVALID_ARG, "n_tokens %d", n_tokens);
+    if (n_tokens > 1 << 30) return fail(ALCH_ERR_UNSUPPORTED, "n_tokens %d > 2^30", n_tokens);
+    if (hidden > 1 << 20) return fail(ALCH_ERR_UNSUPPORTED, "hidden %d > 2^20", hidden);
+    return ALCH_OK;
+}
+
+#define REQUIRE_WORDS(p, name)                                                                                                \
+    do {                                                                                                                      \
+        if (!(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is NULL", name);                                                      \
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(ALCH_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);         \
+    } while (0)
+
+int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids, const void* W_embed,
+                       float scale, void* X, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_embed(dtype, vocab, hidden, n_tokens));
+    if (n_tokens == 0) return ALCH_OK;
+    REQUIRE_WORDS(token_ids, "token_ids");
+    REQUIRE_PTR(W_embed, "W_embed"); REQUIRE_PTR(X, "X");
+    return launch_embed(dtype, token_ids, W_embed, X, n_tokens, vocab, hidden, scale, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t alch_embed_backward_workspace_bytes(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens) {
+    if (check_embed(dtype, vocab, hidden, n_tokens) != ALCH_OK) return 0;
+    return embed_backward_workspace_bytes(vocab, hidden, n_tokens);
+}
+
+int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids, const void* dX, float scale,
+                        void* dW_embed, int32_t accumulate, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_embed(dtype, vocab, hidden, n_tokens));
+    if (n_tokens == 0 && accumulate) return ALCH_OK;
+    if (n_tokens > 0) {
+        REQUIRE_WORDS(token_ids, "token_ids");
+        REQUIRE_PTR(dX, "dX");
+    }
+    REQUIRE_PTR(dW_embed, "dW_embed");
+    const size_t need = embed_backward_workspace_bytes(vocab, hidden, n_tokens);
+    if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+    return launch_embed_backward(dtype, token_ids, dX, n_tokens, vocab, hidden, scale, accumulate != 0, dW_embed, workspace, workspace_bytes,
+                                 static_cast<hipStream_t>(hip_stream));
+}
+
+size_t alch_grad_clip_workspace_bytes(void) { return grad_clip_workspace_bytes(); }
+
+int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alch_grad_tensor* tensors_host, float max_norm, float* norm_out,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_tensors(n_tensors, tensors, tensors_host));
+    for (int i = 0; i < n_tensors; ++i) {
+        const alch_grad_tensor& t = tensors_host[i];
+        if (t.n == 0) continue;
+        ALCH_TRY(check_tensor_ptr(t.grad, i, "grad"));
+        if (!t.out || t.out == t.grad) continue;
+        ALCH_TRY(check_tensor_ptr(t.out, i, "out"));
+        const uintptr_t g = reinterpret_cast<uintptr_t>(t.grad), o = reinterpret_cast<uintptr_t>(t.out);
+        const uintptr_t bytes = (uintptr_t)t.n * dtype_size((alch_dtype)t.dtype);
+        if (g < o ? o - g < bytes : g - o < bytes) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: out overlaps grad", i);
+    }
+    if (!(max_norm >= 0.f)) return fail(ALCH_ERR_INVALID_ARG, "max_norm %g", (double)max_norm);
+    REQUIRE_WORDS(norm_out, "norm_out");
+    const size_t need = grad_clip_workspace_bytes();
+    if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+    return launch_grad_clip(n_tensors, tensors, tensors_host, max_norm, norm_out, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* tensors_host, const alch_adamw* p,
+                    void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_tensors(n_tensors, tensors, tensors_host));
+    if (!p) return fail(ALCH_ERR_INVALID_ARG, "params is NULL");
+    if (!(p->beta1 >= 0 && p->beta1 < 1 && p->beta2 >= 0 && p->beta2 < 1)) return fail(ALCH_ERR_INVALID_ARG, "beta outside 0 <= beta < 1");
+    if (!(p->eps >= 0)) return fail(ALCH_ERR_INVALID_ARG, "eps %g", p->eps);
+    if (p->schedule) REQUIRE_WORDS(p->schedule, "schedule");
+    else if (p->step < 1) return fail(ALCH_ERR_INVALID_ARG, "step %d, the first one is 1", p->step);
+    if (p->grad_factor) REQUIRE_WORDS(p->grad_factor, "grad_factor");
+    for (int i = 0; i < n_tensors; ++i) {
+        const alch_adamw_tensor& t = tensors_host[i];
+        if (t.n == 0) continue;
+        ALCH_TRY(check_tensor_ptr(t.param, i, "param"));
+        ALCH_TRY(check_tensor_ptr(t.grad, i, "grad"));
+        ALCH_TRY(check_tensor_ptr(t.m, i, "m"));
+        ALCH_TRY(check_tensor_ptr(t.v, i, "v"));
+        if (t.master) ALCH_TRY(check_tensor_ptr(t.master, i, "master"));
+    }
+    return launch_adamw(n_tensors, tensors, tensors_host, *p, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

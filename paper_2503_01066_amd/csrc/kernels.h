@@ -333,4 +333,14 @@ int launch_dpo_scatter(alch_dtype dt, const void* src, const int* item_row, int 
 // loss_out[0] = sum(row_loss) / max(N, 1)   (fixed summation order)
 int launch_finish_loss(const float* row_loss, const int* n_counted, float* loss_out, int T, hipStream_t stream);
 
+// ---- the two ends of a training step -------------------------------------------------------
+int launch_embed(alch_dtype dt, const int* ids, const void* W, void* X, int n_tokens, int vocab, int hidden, float scale, hipStream_t stream);
+size_t embed_backward_workspace_bytes(int vocab, int hidden, int n_tokens);
+int launch_embed_backward(alch_dtype dt, const int* ids, const void* dX, int n_tokens, int vocab, int hidden, float scale, int accumulate,
+                          void* dW, void* workspace, size_t workspace_bytes, hipStream_t stream);
+size_t grad_clip_workspace_bytes();
+int launch_grad_clip(int n_tensors, const alch_grad_tensor* tensors, const alch_grad_tensor* host, float max_norm, float* norm_out, void* workspace,
+                     hipStream_t stream);
+int launch_adamw(int n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* host, const alch_adamw& p, hipStream_t stream);
+
 }  // namespace alch

@@ -1,0 +1,175 @@
+"""alch_embed_forward and alch_embed_backward against their definitions.
+
+The forward pass has one rounding: bits are compared.  A sum of the backward pass over n tokens has at most n - 1 additions
+of 2^-24 each in whatever order, the product with the scale and the addition to the old value one each, the storage type half
+a step: |error| <= half * |value| + 2^-24 * ((n + 1) * scale * sum |dX| + |old value|), per element, with
+half = torch.finfo(type).eps / 2, and a second 2^-24 |value| for the rounding before it."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def randn(shape, dtype, seed, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(DT[dtype])
+
+
+def make_ids(kind, T, V, seed=0):
+    r = np.random.default_rng(seed)
+    if kind == "one":
+        ids = np.full(T, V // 2)
+    elif kind == "ascending":
+        ids = np.arange(T) % V
+    elif kind == "runs":      # two ids share most of the tokens
+        ids = np.where(r.random(T) < 0.6, V - 1, np.where(r.random(T) < 0.5, 0, r.integers(0, V, T)))
+    elif kind == "padding":   # no row at all
+        ids = r.choice([-1, V, V + 7, -2 ** 31, 2 ** 31 - 1], T)
+    else:                     # "mixed": some of them no row
+        ids = np.where(r.random(T) < 0.2, r.choice([-1, V, -2 ** 31, 2 ** 31 - 1], T), r.integers(0, V, T))
+    return ids.astype(np.int32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,V,scale", [(1, 4096, 1000, 1.0), (1, 1, 1, 0.3), (487, 487, 97, 22.06), (33, 8, 50, 1.0), (5003, 256, 1000, -16.0),
+                                         (70, 8200, 31, 64.0), (3, 20000, 5, 0.5)])
+def test_forward(T, H, V, scale, dtype):
+    import paper_2503_01066_amd as A
+    ids, W = make_ids("mixed", T, V), randn((V, H), dtype, 1)
+    big = torch.full((T + 2, H), 7.0, dtype=DT[dtype], device="cuda")
+    if H * big.element_size() % 16:
+        X = A.alch_embed_forward(torch.from_numpy(ids).cuda(), W.cuda(), scale=scale)
+    else:  # rows around the output stay as they were
+        X = A.alch_embed_forward(torch.from_numpy(ids).cuda(), W.cuda(), scale=scale, X=big[1:T + 1])
+        assert bool((big[0] == 7).all()) and bool((big[T + 1] == 7).all())
+    ok = (ids >= 0) & (ids < V)
+    ref = torch.zeros((T, H), dtype=DT[dtype])
+    ref[ok] = (W[torch.from_numpy(ids[ok]).long()].float() * np.float32(scale)).to(DT[dtype])
+    assert torch.equal(X.cpu(), ref)
+
+
+def check_backward(ids, dX, V, scale, dW, old):
+    """dW: device result; old: what it held (accumulate), or None."""
+    T, H = dX.shape
+    ok = (ids >= 0) & (ids < V)
+    at, rows = torch.from_numpy(ids[ok]).long().cuda(), dX.cuda()[torch.from_numpy(np.flatnonzero(ok)).cuda()].double()
+    n = torch.bincount(at, minlength=V).double()
+    met, order = torch.nonzero(n)[:, 0], torch.argsort(at, stable=True)
+    last = torch.cumsum(n[met].long(), 0) - 1
+
+    def by_id(x):  # as differences of a running sum over the sorted tokens
+        out, total = torch.zeros((V, H), dtype=torch.float64, device="cuda"), torch.cumsum(x[order], 0)[last]
+        out[met] = total - torch.cat([torch.zeros_like(total[:1]), total[:-1]])
+        return out
+
+    ref, size = by_id(rows) * scale, by_id(rows.abs()) * abs(scale)
+    before = torch.zeros_like(ref) if old is None else old.cuda().double()
+    ref = ref + before
+    half = torch.finfo(dX.dtype).eps / 2
+    bound = (half + 2.0 ** -24) * ref.abs() + 2.0 ** -24 * ((n[:, None] + 1) * size + before.abs()) + 1e-44
+    err = (dW.double() - ref).abs()
+    assert bool(torch.isfinite(dW).all())
+    assert bool((err <= bound).all()), float((err / bound).max())
+    absent = n == 0
+    assert torch.equal(dW[absent], torch.zeros_like(dW[absent]) if old is None else old.cuda()[absent])
+
+
+CASES = [(1, 4096, 1000, "mixed"), (31, 256, 64, "mixed"), (32, 256, 64, "one"), (33, 487, 64, "one"), (64, 64, 3, "runs"), (65, 8, 1, "one"),
+         (487, 4096, 5000, "mixed"), (487, 130, 128256, "ascending"), (1025, 72, 1023, "runs"), (1500, 40, 1024, "mixed"), (5003, 256, 1000, "runs"),
+         (16384, 64, 128256, "runs"), (9000, 520, 7, "mixed"), (70001, 24, 40000, "one"), (200, 64, 9, "padding"), (300, 1, 17, "mixed"),
+         (2049, 8200, 300, "runs"), (4097, 16, 4097, "ascending")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,V,kind", CASES)
+def test_backward(T, H, V, kind, dtype):
+    import paper_2503_01066_amd as A
+    ids, dX = make_ids(kind, T, V, T), randn((T, H), dtype, T + 1, 0.01)
+    bad = (ids < 0) | (ids >= V)
+    dX[torch.from_numpy(bad)] = float("nan")  # rows without a token are not read
+    dev_ids, dev = torch.from_numpy(ids).cuda(), dX.cuda()
+    ws = torch.full((A.embed_backward_workspace_bytes(DT[dtype], V, H, T),), 0x7f, dtype=torch.uint8, device="cuda")
+    whole = torch.full((V + 2, H), 3.0, dtype=DT[dtype], device="cuda")
+    own = H * whole.element_size() % 16 == 0  # rows around the table stay as they were
+    dW = whole[1:V + 1] if own else whole[:V].clone()
+    A.alch_embed_backward(dev_ids, dev, V, scale=1.7, dW_embed=dW, workspace=ws)
+    check_backward(ids, dX, V, np.float32(1.7).astype(np.float64), dW, None)
+    old = randn((V, H), dtype, 5, 0.1)
+    first = dW.clone()
+    dW.copy_(old)
+    A.alch_embed_backward(dev_ids, dev, V, scale=1.7, dW_embed=dW, accumulate=True, workspace=ws)
+    check_backward(ids, dX, V, np.float32(1.7).astype(np.float64), dW, old)
+    if own:
+        assert bool((whole[0] == 3).all()) and bool((whole[V + 1] == 3).all())
+    ws.fill_(0)  # what the workspace held makes no difference
+    again = A.alch_embed_backward(dev_ids, dev, V, scale=1.7, workspace=ws)
+    assert torch.equal(again, first)
+
+
+def test_backward_without_tokens_writes_zeros():
+    import paper_2503_01066_amd as A
+    dW = torch.full((37, 24), 5.0, device="cuda")
+    A.alch_embed_backward(torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 24, device="cuda"), 37, dW_embed=dW)
+    assert bool((dW == 0).all())
+    dW.fill_(5.0)
+    A.alch_embed_backward(torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, 24, device="cuda"), 37, dW_embed=dW, accumulate=True)
+    assert bool((dW == 5).all())
+
+
+def test_infinities_and_nan_reach_their_own_row_alone():
+    import paper_2503_01066_amd as A
+    ids = np.array([3, 1, 3, 2, 1] * 20, np.int32)
+    dX = torch.ones((100, 16))
+    dX[0, 5], dX[1, 6], dX[3, 7], dX[8, 7] = float("inf"), float("nan"), float("inf"), -float("inf")
+    dW = A.alch_embed_backward(torch.from_numpy(ids).cuda(), dX.cuda(), 5).cpu()
+    assert dW[3, 5] == float("inf") and torch.isnan(dW[1, 6]) and torch.isnan(dW[2, 7])
+    assert int((~torch.isfinite(dW)).sum()) == 3
+
+
+def test_table_beyond_32_bit_offsets():
+    import paper_2503_01066_amd as A
+    V, H = 300000, 8192  # 2.46e9 elements
+    W = torch.zeros((V, H), dtype=torch.bfloat16, device="cuda")
+    W[V - 1].fill_(3.0)
+    W[V - 2].fill_(2.0)
+    ids = torch.tensor([V - 1, 0, V - 2, V - 1], dtype=torch.int32, device="cuda")
+    X = A.alch_embed_forward(ids, W, scale=0.5)
+    assert X[:, 0].tolist() == [1.5, 0.0, 1.0, 1.5] and bool((X == X[:, :1]).all())
+    dW = A.alch_embed_backward(ids, X, V, dW_embed=W, accumulate=True)  # 3 + 3, 2 + 1
+    assert dW[-1, 0] == 6 and dW[-2, 0] == 3 and bool((dW[-2:] == dW[-2:, :1]).all()) and bool((dW[:V - 2] == 0).all())
+    dW = A.alch_embed_backward(ids, X, V, dW_embed=W)
+    assert dW[-1, 0] == 3 and dW[-2, 0] == 1 and bool((dW[-2:] == dW[-2:, :1]).all()) and bool((dW[:V - 2] == 0).all())
+
+
+def test_other_streams_and_two_calls_at_once():
+    import paper_2503_01066_amd as A
+    T, H, V = 3000, 512, 2000
+    jobs = []
+    for k in range(2):
+        ids, dX = make_ids("runs", T, V, k), randn((T, H), "bf16", k)
+        jobs.append((torch.from_numpy(ids).cuda(), dX.cuda(), torch.cuda.Stream(), torch.empty((V, H), dtype=torch.bfloat16, device="cuda")))
+    alone = [A.alch_embed_backward(i, d, V) for i, d, _, _ in jobs]
+    torch.cuda.synchronize()
+    for rep in range(3):
+        for ids, dX, s, dW in jobs:
+            A.alch_embed_backward(ids, dX, V, dW_embed=dW, stream=s)
+        torch.cuda.synchronize()
+        for (_, _, _, dW), a in zip(jobs, alone):
+            assert torch.equal(dW, a)
+
+
+def test_gradient_against_differences():
+    # f(W) = <R, X(W)> is linear in W: (f(W + h E) - f(W)) / h = <dW, E> up to rounding, for any direction E
+    import paper_2503_01066_amd as A
+    T, H, V, scale = 700, 48, 60, 3.0
+    ids = make_ids("mixed", T, V)
+    dev = torch.from_numpy(ids).cuda()
+    W, R, E = (randn(s, "f32", k).cuda() for k, s in enumerate([(V, H), (T, H), (V, H)]))
+    f = lambda w: (A.alch_embed_forward(dev, w, scale=scale).double() * R.double()).sum()
+    dW = A.alch_embed_backward(dev, R, V, scale=scale)
+    h = 0.5
+    measured, formula = (f(W + h * E) - f(W)) / h, (dW.double() * E.double()).sum()
+    # X and X(W + hE) are rounded twice (2^-24 of at most ~5 * 3 each), 33600 products with |R| ~ 1, over h: about 1e-4 of ~ 540
+    assert abs(float(measured - formula)) <= 2.0 ** -23 * 2 / h * float((A.alch_embed_forward(dev, W.abs() + h * E.abs(), scale=scale) * R.abs()).double().sum()) + 1e-9
