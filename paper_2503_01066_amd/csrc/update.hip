@@ -18,15 +18,21 @@ static constexpr int kNormBlocks = 1024;
 
 typedef float f32x4_u __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_u __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_u __attribute__((ext_vector_type(4)));
 
-// first[i] = chunks of the tensors before i, first[n] = all of them.  Work-groups of 256 threads.
-template <typename Tensor>
-__device__ __forceinline__ void chunk_table(const Tensor* __restrict__ tensors, int n, int chunk, int* first /*[n + 1]*/) {
+// first[i] = chunks of the tensors before i, first[n] = all of them; chunk_of(tensor): its elements a chunk.  Work-groups of 256 threads.
+template <typename Tensor, typename F>
+__device__ __forceinline__ void chunk_table(const Tensor* __restrict__ tensors, int n, F chunk_of, int* first /*[n + 1]*/) {
     __shared__ int wave_total[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int carry = 0;
     for (int base = 0; base < n; base += 256) {
-        const int i = base + tid, own = i < n ? (int)((tensors[i].n + chunk - 1) / chunk) : 0;
+        const int i = base + tid;
+        int own = 0;
+        if (i < n) {
+            const int chunk = chunk_of(tensors[i].dtype);  // (a power of two)
+            own = (int)((tensors[i].n + chunk - 1) >> (31 - __clz(chunk)));
+        }
         int inc = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -70,141 +76,168 @@ __device__ __forceinline__ double block_sum(double v, double* red /*[4]*/) {
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Eight elements of a tensor from element at on, as fp32; what lies behind its end counts as 0.
-__device__ __forceinline__ void load8(const void* p, int dtype, long long at, int count, float (&x)[8]) {
-    if (count >= 8) {
-        if (dtype == ALCH_BF16) {
-            const bf16x8_u v = *reinterpret_cast<const bf16x8_u*>(static_cast<const __bf16*>(p) + at);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-        } else {
-            const f32x4_u *q = reinterpret_cast<const f32x4_u*>(static_cast<const float*>(p) + at);
-            const f32x4_u a = q[0], b = q[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = e >= count ? 0.f : dtype == ALCH_BF16 ? (float)static_cast<const __bf16*>(p)[at + e] : static_cast<const float*>(p)[at + e];
-    }
-}
-__device__ __forceinline__ void store8(void* p, int dtype, long long at, int count, const float (&x)[8]) {
-    if (count >= 8) {
-        if (dtype == ALCH_BF16) {
-            bf16x8_u v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
-            *reinterpret_cast<bf16x8_u*>(static_cast<__bf16*>(p) + at) = v;
-        } else {
-            f32x4_u a, b;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { a[e] = x[e]; b[e] = x[4 + e]; }
-            f32x4_u* q = reinterpret_cast<f32x4_u*>(static_cast<float*>(p) + at);
-            q[0] = a;
-            q[1] = b;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < count) {
-                if (dtype == ALCH_BF16) static_cast<__bf16*>(p)[at + e] = (__bf16)x[e];
-                else static_cast<float*>(p)[at + e] = x[e];
-            }
-    }
-}
-
 // ---- norm and clipping --------------------------------------------------------------------
-static constexpr int kClipChunk = 8192;  // elements
+// A chunk is kBatch pieces of 16 bytes a thread, 16 KB (4 KB: 436 MB 242 instead of 209 us, and the 4 MB of a small fp32 layer, which
+// then are chunks for all compute units, 8.7 instead of 7.9).  Both kernels deal the chunks out in the same order, so that what
+// fits into an XCD's L2 is there when it is clipped.  Loads and stores are non-temporal: with ordinary stores the norm of 436 MB
+// behind a clipping takes 105 us instead of 73, with ordinary loads beside them the clipping 139 instead of 125.
+static constexpr int kBatch = 4;
 
-// The squares are added in 64 bits: no gradient of finite numbers overflows there, none vanishes, and the order of the additions
-// (that of the chunks, which differs with the lengths of the tensors) is not seen in a norm of 32 bits.
+struct ClipChunk {
+    const char* grad;
+    char* out;
+    int elements, dtype;
+};
+__host__ __device__ inline int clip_elements(int dtype) { return 256 * kBatch * (dtype == ALCH_BF16 ? 8 : 4); }
+__device__ __forceinline__ ClipChunk clip_chunk(const alch_grad_tensor* __restrict__ tensors, const int* first, int n, int c) {
+    const int t = tensor_of(first, n, c);
+    const alch_grad_tensor a = tensors[t];
+    const int chunk = clip_elements(a.dtype);
+    const long long begin = (long long)(c - first[t]) * chunk, at = begin * (a.dtype == ALCH_BF16 ? 2 : 4);
+    return {static_cast<const char*>(a.grad) + at, a.out ? static_cast<char*>(a.out) + at : nullptr, (int)min((long long)chunk, (long long)a.n - begin), a.dtype};
+}
+__device__ __forceinline__ void clip_load(const ClipChunk& c, f32x4_u (&v)[kBatch]) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) v[b] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(c.grad) + threadIdx.x + 256 * b);
+}
+
+// The squares are added in 64 bits: no gradient of finite numbers overflows there, none vanishes, and the order of the
+// additions (which differs with the lengths of the tensors) is not seen in a norm of 32 bits.  They cost nothing beside the
+// loads (436 MB: 73.9 us, 73.1 with sums in fp32).
 __global__ __launch_bounds__(256) void k_norm(const alch_grad_tensor* __restrict__ tensors, int n, double* __restrict__ partial) {
     __shared__ int first[kMaxTensors + 1];
     __shared__ double red[4];
-    chunk_table(tensors, n, kClipChunk, first);
+    chunk_table(tensors, n, clip_elements, first);
     const int chunks = first[n];
     double s = 0.0;
+    ClipChunk next = {};
+    if ((int)blockIdx.x < chunks) next = clip_chunk(tensors, first, n, blockIdx.x);
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int t = tensor_of(first, n, c);
-        const alch_grad_tensor a = tensors[t];
-        const long long begin = (long long)(c - first[t]) * kClipChunk;
-        const int len = (int)min((long long)kClipChunk, (long long)a.n - begin);
-#pragma unroll 4
-        for (int i = threadIdx.x * 8; i < len; i += 2048) {
-            float x[8];
-            load8(a.grad, a.dtype, begin + i, len - i, x);
+        const ClipChunk a = next;
+        const bool full = a.elements == clip_elements(a.dtype);
+        f32x4_u v[kBatch];
+        if (full) clip_load(a, v);
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
+        if (full && a.dtype == ALCH_BF16) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += (double)x[e] * (double)x[e];
+            for (int b = 0; b < kBatch; ++b) {
+                const bf16x8_u x = __builtin_bit_cast(bf16x8_u, v[b]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s += (double)(float)x[e] * (double)(float)x[e];
+            }
+        } else if (full) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += (double)v[b][e] * (double)v[b][e];
+        } else {
+            for (int i = threadIdx.x; i < a.elements; i += 256) {
+                const double x = a.dtype == ALCH_BF16 ? (float)reinterpret_cast<const __bf16*>(a.grad)[i] : reinterpret_cast<const float*>(a.grad)[i];
+                s += x * x;
+            }
         }
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-__device__ __forceinline__ float clip_factor(double sum, float max_norm, float* norm_out) {
-    const double norm = sqrt(sum);
+// The factor from the sums that k_norm left, by every work-group for itself and in the same order: a launch for it alone costs more.
+struct NormSums {
+    double of[kNormBlocks / 256];
+};
+__device__ __forceinline__ NormSums norm_sums(const double* __restrict__ partial, int blocks) {
+    NormSums s;
+#pragma unroll
+    for (int i = 0; i < kNormBlocks / 256; ++i) s.of[i] = (int)threadIdx.x + 256 * i < blocks ? partial[threadIdx.x + 256 * i] : 0.0;
+    return s;
+}
+__device__ __forceinline__ float clip_factor(const NormSums& sums, float max_norm, float* __restrict__ norm_out) {
+    __shared__ double red[4];
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kNormBlocks / 256; ++i) s += sums.of[i];
+    const double norm = sqrt(block_sum(s, red));
     const float factor = !(norm < INFINITY) ? NAN : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
-    if (norm_out) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
         norm_out[0] = (float)norm;
         norm_out[1] = factor;
     }
     return factor;
 }
 
-__global__ __launch_bounds__(256) void k_norm_finish(const double* __restrict__ partial, int blocks, float max_norm, float* __restrict__ norm_out) {
-    __shared__ double red[4];
-    double s = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += 256) s += partial[i];
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) clip_factor(s, max_norm, norm_out);
+__global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict__ tensors, int n, const double* __restrict__ partial, int blocks,
+                                              float max_norm, float* __restrict__ norm_out) {
+    __shared__ int first[kMaxTensors + 1];
+    const NormSums sums = norm_sums(partial, blocks);
+    chunk_table(tensors, n, clip_elements, first);
+    const int chunks = first[n];
+    ClipChunk a = clip_chunk(tensors, first, n, blockIdx.x);  // (no more work-groups than chunks)
+    float factor = 0.f;
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+        bool used = a.out, full = used && a.elements == clip_elements(a.dtype);
+        f32x4_u v[kBatch];
+        if (full) clip_load(a, v);
+        ClipChunk next = {};
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
+        if (c == (int)blockIdx.x) factor = clip_factor(sums, max_norm, norm_out);
+        if (a.out == a.grad && factor == 1.f) used = full = false;
+        if (full) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (a.dtype == ALCH_BF16) {
+                    bf16x8_u x = __builtin_bit_cast(bf16x8_u, v[b]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = (__bf16)((float)x[e] * factor);
+                    v[b] = __builtin_bit_cast(f32x4_u, x);
+                } else {
+                    v[b] *= factor;
+                }
+                __builtin_nontemporal_store(v[b], reinterpret_cast<f32x4_u*>(a.out) + threadIdx.x + 256 * b);
+            }
+        } else if (used) {
+            for (int i = threadIdx.x; i < a.elements; i += 256) {
+                if (a.dtype == ALCH_BF16)
+                    reinterpret_cast<__bf16*>(a.out)[i] = (__bf16)((float)reinterpret_cast<const __bf16*>(a.grad)[i] * factor);
+                else
+                    reinterpret_cast<float*>(a.out)[i] = reinterpret_cast<const float*>(a.grad)[i] * factor;
+            }
+        }
+        a = next;
+    }
 }
 
-__global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict__ tensors, int n, const float* __restrict__ norm) {
-    __shared__ int first[kMaxTensors + 1];
-    chunk_table(tensors, n, kClipChunk, first);
-    const int chunks = first[n];
-    const float factor = norm[1];
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int t = tensor_of(first, n, c);
-        const alch_grad_tensor a = tensors[t];
-        if (!a.out) continue;
-        const long long begin = (long long)(c - first[t]) * kClipChunk;
-        const int len = (int)min((long long)kClipChunk, (long long)a.n - begin);
-        for (int i = threadIdx.x * 8; i < len; i += 2048) {
-            float x[8];
-            load8(a.grad, a.dtype, begin + i, len - i, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= factor;
-            store8(a.out, a.dtype, begin + i, len - i, x);
-        }
-    }
+__global__ __launch_bounds__(256) void k_norm_finish(const double* __restrict__ partial, int blocks, float max_norm, float* __restrict__ norm_out) {
+    clip_factor(norm_sums(partial, blocks), max_norm, norm_out);
 }
 
 size_t grad_clip_workspace_bytes() { return kNormBlocks * sizeof(double); }
 
 int launch_grad_clip(int n_tensors, const alch_grad_tensor* tensors, const alch_grad_tensor* host, float max_norm, float* norm_out, void* workspace,
                      hipStream_t stream) {
-    long long chunks = 0;
     double bytes = 0;
+    long long chunks = 0;
     bool any_out = false;
     for (int i = 0; i < n_tensors; ++i) {
-        chunks += (host[i].n + kClipChunk - 1) / kClipChunk;
+        const int chunk = clip_elements(host[i].dtype);
+        chunks += (host[i].n + chunk - 1) / chunk;
         any_out = any_out || (host[i].out && host[i].n > 0);
-        bytes += (double)host[i].n * dtype_size((alch_dtype)host[i].dtype) * (host[i].out ? 2 : 1);
+        bytes += (double)host[i].n * dtype_size((alch_dtype)host[i].dtype);
     }
-    TraceScope ts(kTraceUpdate, 0.0, bytes, stream);
+    TraceScope ts(kTraceUpdate, 0.0, bytes * (any_out ? 3 : 1), stream);
     double* partial = static_cast<double*>(workspace);
     const int blocks = (int)std::min<long long>(std::max<long long>(chunks, 1), kNormBlocks);
     k_norm<<<blocks, 256, 0, stream>>>(tensors, n_tensors, partial);
-    k_norm_finish<<<1, 256, 0, stream>>>(partial, blocks, max_norm, norm_out);
-    if (any_out) k_clip<<<(int)std::min<long long>(chunks, 2048), 256, 0, stream>>>(tensors, n_tensors, norm_out);
+    if (any_out)
+        k_clip<<<blocks, 256, 0, stream>>>(tensors, n_tensors, partial, blocks, max_norm, norm_out);
+    else
+        k_norm_finish<<<1, 256, 0, stream>>>(partial, blocks, max_norm, norm_out);
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }
 
 // ---- AdamW --------------------------------------------------------------------------------
-static constexpr int kAdamwChunk = 2048;  // elements: eight a thread
+static constexpr int kAdamwBatch = 2, kAdamwChunk = 1024 * kAdamwBatch;  // elements
+static constexpr int kAdamwBlocks = 1 << 22;  // one work-group a chunk: 1061 us for 218 M elements, 1192 with 2048 work-groups that walk them
 
 struct AdamwArgs {
     const alch_adamw_tensor* tensors;
@@ -218,6 +251,83 @@ struct AdamwArgs {
 // 1 / (1 - b^t), in 64 bits: for b = 0.999 and t = 1 three of seven digits are lost in 32.
 __host__ __device__ inline float correction(double beta, double step) { return (float)(1.0 / (1.0 - pow(beta, step))); }
 
+// Four elements a lane, so that the 64 lanes of a load of fp32 read 1 KB without a gap (eight a lane, as two loads of every other
+// 16 bytes, cost 10 % with non-temporal loads).
+__device__ __forceinline__ f32x4_u load4(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p)); }
+__device__ __forceinline__ f32x4_u load4(const __bf16* p) {
+    return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const bf16x4_u*>(p)), f32x4_u);
+}
+__device__ __forceinline__ void store4(float* p, f32x4_u v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4_u*>(p)); }
+__device__ __forceinline__ void store4(__bf16* p, f32x4_u v) {
+    __builtin_nontemporal_store(__builtin_convertvector(v, bf16x4_u), reinterpret_cast<bf16x4_u*>(p));
+}
+
+struct AdamwChunk {
+    alch_adamw_tensor t;
+    long long at;
+    int elements;
+};
+__device__ __forceinline__ AdamwChunk adamw_chunk(const alch_adamw_tensor* __restrict__ tensors, const int* first, int n, int c) {
+    const int i = tensor_of(first, n, c);
+    AdamwChunk a;
+    a.t = tensors[i];
+    a.at = (long long)(c - first[i]) * kAdamwChunk;
+    a.elements = (int)min((long long)kAdamwChunk, (long long)a.t.n - a.at);
+    return a;
+}
+
+struct AdamwRates {
+    float factor, lr, c1, c2;
+};
+__device__ __forceinline__ void adamw_element(const AdamwArgs& a, const AdamwRates& r, float decay, float g, float& m, float& v, float& w) {
+    const float x = g * r.factor;
+    m = a.b1 * m + a.d1 * x;
+    v = a.b2 * v + a.d2 * x * x;
+    w -= r.lr * (m * r.c1 / (sqrtf(v * r.c2) + a.eps) + decay * w);
+}
+
+template <typename T, bool kMaster>
+__device__ __forceinline__ void adamw(const AdamwChunk& k, const AdamwArgs& a, const AdamwRates& r) {
+    T* param = static_cast<T*>(k.t.param) + k.at;
+    const T* grad = static_cast<const T*>(k.t.grad) + k.at;
+    float *m = k.t.m + k.at, *v = k.t.v + k.at, *master = kMaster ? k.t.master + k.at : nullptr;
+    if (k.elements == kAdamwChunk) {
+        f32x4_u gv[kAdamwBatch], mv[kAdamwBatch], vv[kAdamwBatch], wv[kAdamwBatch];
+#pragma unroll
+        for (int b = 0; b < kAdamwBatch; ++b) {
+            const int i = (threadIdx.x + 256 * b) * 4;
+            gv[b] = load4(grad + i);
+            mv[b] = load4(m + i);
+            vv[b] = load4(v + i);
+            if constexpr (kMaster) wv[b] = load4(master + i);
+            else wv[b] = load4(param + i);
+        }
+#pragma unroll
+        for (int b = 0; b < kAdamwBatch; ++b) {
+            const int i = (threadIdx.x + 256 * b) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float me = mv[b][e], ve = vv[b][e], we = wv[b][e];
+                adamw_element(a, r, k.t.weight_decay, gv[b][e], me, ve, we);
+                mv[b][e] = me; vv[b][e] = ve; wv[b][e] = we;
+            }
+            store4(m + i, mv[b]);
+            store4(v + i, vv[b]);
+            if constexpr (kMaster) store4(master + i, wv[b]);
+            store4(param + i, wv[b]);
+        }
+    } else {
+        for (int i = threadIdx.x; i < k.elements; i += 256) {
+            float me = m[i], ve = v[i], we = kMaster ? master[i] : (float)param[i];
+            adamw_element(a, r, k.t.weight_decay, (float)grad[i], me, ve, we);
+            m[i] = me;
+            v[i] = ve;
+            if constexpr (kMaster) master[i] = we;
+            param[i] = (T)we;
+        }
+    }
+}
+
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
     __shared__ int first[kMaxTensors + 1];
     __shared__ float shared_c[3];
@@ -229,32 +339,18 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
         shared_c[1] = correction(a.beta1, step);
         shared_c[2] = correction(a.beta2, step);
     }
-    chunk_table(a.tensors, a.n, kAdamwChunk, first);
+    chunk_table(a.tensors, a.n, [](int) { return kAdamwChunk; }, first);
     const int chunks = first[a.n];
-    const float lr = a.schedule ? shared_c[0] : a.lr, c1 = a.schedule ? shared_c[1] : a.c1, c2 = a.schedule ? shared_c[2] : a.c2;
+    const AdamwRates r{factor, a.schedule ? shared_c[0] : a.lr, a.schedule ? shared_c[1] : a.c1, a.schedule ? shared_c[2] : a.c2};
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int ti = tensor_of(first, a.n, c);
-        const alch_adamw_tensor t = a.tensors[ti];
-        const long long at = (long long)(c - first[ti]) * kAdamwChunk + threadIdx.x * 8;
-        const int count = (int)min((long long)8, (long long)t.n - at);
-        if (count <= 0) continue;
-        float g[8], m[8], v[8], w[8];
-        load8(t.grad, t.dtype, at, count, g);
-        load8(t.m, ALCH_F32, at, count, m);
-        load8(t.v, ALCH_F32, at, count, v);
-        if (t.master) load8(t.master, ALCH_F32, at, count, w);
-        else load8(t.param, t.dtype, at, count, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = g[e] * factor;
-            m[e] = a.b1 * m[e] + a.d1 * x;
-            v[e] = a.b2 * v[e] + a.d2 * x * x;
-            w[e] -= lr * (m[e] * c1 / (sqrtf(v[e] * c2) + a.eps) + t.weight_decay * w[e]);
+        const AdamwChunk k = adamw_chunk(a.tensors, first, a.n, c);
+        if (k.t.dtype == ALCH_BF16) {
+            if (k.t.master) adamw<__bf16, true>(k, a, r);
+            else adamw<__bf16, false>(k, a, r);
+        } else {
+            if (k.t.master) adamw<float, true>(k, a, r);
+            else adamw<float, false>(k, a, r);
         }
-        store8(t.m, ALCH_F32, at, count, m);
-        store8(t.v, ALCH_F32, at, count, v);
-        if (t.master) store8(t.master, ALCH_F32, at, count, w);
-        store8(t.param, t.dtype, at, count, w);
     }
 }
 
@@ -271,7 +367,7 @@ int launch_adamw(int n_tensors, const alch_adamw_tensor* tensors, const alch_ada
     const AdamwArgs a{tensors, n_tensors, (float)p.lr, p.schedule ? 0.f : correction(p.beta1, p.step), p.schedule ? 0.f : correction(p.beta2, p.step),
                       (float)p.beta1, (float)p.beta2, (float)(1.0 - p.beta1), (float)(1.0 - p.beta2), (float)p.eps, p.beta1, p.beta2,
                       p.schedule, p.grad_factor};
-    k_adamw<<<(int)std::min<long long>(chunks, 2048), 256, 0, stream>>>(a);
+    k_adamw<<<(int)std::min<long long>(chunks, kAdamwBlocks), 256, 0, stream>>>(a);
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }
