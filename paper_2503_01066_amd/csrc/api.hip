@@ -1418,6 +1418,7 @@ static int check_embed(alch_dtype dtype, int vocab, int hidden, int n_tokens) {
     if (n_tokens < 0) return fail(ALCH_ERR_INVALID_ARG, "n_tokens %d", n_tokens);
     if (n_tokens > 1 << 30) return fail(ALCH_ERR_UNSUPPORTED, "n_tokens %d > 2^30", n_tokens);
     if (hidden > 1 << 20) return fail(ALCH_ERR_UNSUPPORTED, "hidden %d > 2^20", hidden);
+    if ((long long)std::max(vocab, n_tokens) * hidden > 1LL << 40) return fail(ALCH_ERR_UNSUPPORTED, "a table or X of more than 2^40 elements");
     return ALCH_OK;
 }
 

@@ -7,70 +7,104 @@
 // so that every sum runs over ascending tokens and results repeat bit for bit; no float atomics), and the sorted tokens are
 // cut into parts of equal length, so that one id that half of a batch shares is no longer a chain than any other.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
 namespace alch {
 
-typedef unsigned int u32x4_e __attribute__((ext_vector_type(4)));
+// kVec elements of a row, 16 bytes (single elements where a row has fewer): rows of any width lie one behind the other, so that they
+// need not begin at a multiple of 16 bytes.  The last piece of a row is moved back to end with it and overlaps the one before.
+template <typename T, int kVec>
+struct Piece {
+    typedef T type __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
+};
+
+// A work-group goes over 8 KB of rows that lie behind one another, two pieces a thread: `1 << log_lanes` threads to a row, one row
+// in `segments` work-groups where it is longer.  Work-groups with more, or with fewer that have more of them under way, are slower:
+// 70,001 rows of 8 KB copied in 134 us, with two rows a work-group 143, with four 146; 1.05 GB zeroed in 154, with four rows 190.
+struct RowGrid {
+    int log_lanes, segments, blocks;
+};
+static RowGrid row_grid(long long rows, int hidden, int vec) {
+    RowGrid g;
+    const int pieces = ceil_div(hidden, vec);
+    g.log_lanes = 0;
+    while (g.log_lanes < 8 && (2 << g.log_lanes) < pieces) ++g.log_lanes;
+    g.segments = ceil_div(pieces, 2 << g.log_lanes);
+    g.blocks = (int)((rows + (256 >> g.log_lanes) - 1) / (256 >> g.log_lanes) * g.segments);  // (at most 2^30: 2^40 elements)
+    return g;
+}
+// First row of a work-group, and its part of it.
+__device__ __forceinline__ long long first_row(const RowGrid& g, int block, int* segment) {
+    const int group = g.segments == 1 ? block : block / g.segments;
+    *segment = block - group * g.segments;
+    return (long long)group * (256 >> g.log_lanes);
+}
+static constexpr int kMaxBlocks = 1 << 23;  // of a launch; what is more is gone over in rounds
 
 // ---- forward ----------------------------------------------------------------------------
-
-// kVec elements a lane (16 bytes, or single elements where rows are not made of aligned 16-byte pieces), lanes_per_row lanes
-// (a power of two) share a row.
-template <typename T, int kVec>
+// kWide: a wavefront has one row, whose id is then read as a scalar.
+template <typename T, int kVec, bool kWide>
 __global__ __launch_bounds__(256) void k_embed(const int* __restrict__ ids, const T* __restrict__ W, T* __restrict__ X, int n_tokens, int vocab,
-                                               int hidden, float scale, int log_lanes) {
-    typedef T vec __attribute__((ext_vector_type(kVec)));
-    const int lanes = 1 << log_lanes, rows = 256 >> log_lanes, c0 = (threadIdx.x & (lanes - 1)) * kVec;
-    for (long long t = (long long)blockIdx.x * rows + (threadIdx.x >> log_lanes); t < n_tokens; t += (long long)gridDim.x * rows) {
-        const int id = ids[t];
+                                               int hidden, float scale, RowGrid g) {
+    typedef typename Piece<T, kVec>::type vec;
+    const int lane = threadIdx.x & ((1 << g.log_lanes) - 1);
+    for (int b = blockIdx.x; b < g.blocks; b += gridDim.x) {
+        int segment;
+        long long t = first_row(g, b, &segment) + (threadIdx.x >> g.log_lanes);
+        if (kWide) t = __builtin_amdgcn_readfirstlane((int)t);
+        if (t >= n_tokens) continue;
+        const int id = ids[t], c0 = ((segment << (g.log_lanes + 1)) + lane) * kVec, step = kVec << g.log_lanes;
         const bool valid = (unsigned)id < (unsigned)vocab;
         const T* src = W + (long long)(valid ? id : 0) * hidden;
-        T* dst = X + t * hidden;
-        for (int c = c0; c < hidden; c += lanes * kVec) {
-            vec v = {};
-            if (valid) {
-                v = *reinterpret_cast<const vec*>(src + c);
+        vec v[2] = {};
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) v[e] = (T)((float)v[e] * scale);
-            }
-            *reinterpret_cast<vec*>(dst + c) = v;
+        for (int j = 0; j < 2; ++j)
+            if (valid && c0 + j * step < hidden) v[j] = *reinterpret_cast<const vec*>(src + min(c0 + j * step, hidden - kVec));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[j][e] = (T)((float)v[j][e] * scale);
+            if (!valid) v[j] = vec{};  // (also where the scale is negative or no number)
+            if (c0 + j * step < hidden) __builtin_nontemporal_store(v[j], reinterpret_cast<vec*>(X + t * hidden + min(c0 + j * step, hidden - kVec)));
         }
     }
 }
 
-template <typename T>
-static void embed_launch(const int* ids, const void* W, void* X, int n, int vocab, int hidden, float scale, hipStream_t stream) {
-    constexpr int kVec = 16 / sizeof(T);
-    const bool vec = hidden % kVec == 0;
-    const int pieces = vec ? hidden / kVec : hidden;
-    int log_lanes = 0;
-    while (log_lanes < 8 && (1 << log_lanes) < pieces) ++log_lanes;
-    const int grid = std::min(ceil_div(n, 256 >> log_lanes), 1 << 20);
-    if (vec)
-        k_embed<T, kVec><<<grid, 256, 0, stream>>>(ids, (const T*)W, (T*)X, n, vocab, hidden, scale, log_lanes);
-    else
-        k_embed<T, 1><<<grid, 256, 0, stream>>>(ids, (const T*)W, (T*)X, n, vocab, hidden, scale, log_lanes);
+// f(type, pieces of how many elements) for rows of a type and width
+template <typename F>
+static void with_pieces(alch_dtype dt, int hidden, F f) {
+    using std::integral_constant;
+    if (dt == ALCH_BF16) hidden >= 8 ? f(__bf16{}, integral_constant<int, 8>{}) : f(__bf16{}, integral_constant<int, 1>{});
+    else hidden >= 4 ? f(float{}, integral_constant<int, 4>{}) : f(float{}, integral_constant<int, 1>{});
 }
 
 int launch_embed(alch_dtype dt, const int* ids, const void* W, void* X, int n_tokens, int vocab, int hidden, float scale, hipStream_t stream) {
     if (n_tokens <= 0) return ALCH_OK;
     TraceScope ts(kTraceEmbed, (double)n_tokens * hidden, 2.0 * n_tokens * hidden * dtype_size(dt), stream);
-    if (dt == ALCH_BF16)
-        embed_launch<__bf16>(ids, W, X, n_tokens, vocab, hidden, scale, stream);
-    else
-        embed_launch<float>(ids, W, X, n_tokens, vocab, hidden, scale, stream);
+    with_pieces(dt, hidden, [&](auto type, auto vec) {
+        typedef decltype(type) T;
+        constexpr int kVec = decltype(vec)::value;
+        const RowGrid g = row_grid(n_tokens, hidden, kVec);
+        const int grid = std::min(g.blocks, kMaxBlocks);
+        if (g.log_lanes >= 6)
+            k_embed<T, kVec, true><<<grid, 256, 0, stream>>>(ids, (const T*)W, (T*)X, n_tokens, vocab, hidden, scale, g);
+        else
+            k_embed<T, kVec, false><<<grid, 256, 0, stream>>>(ids, (const T*)W, (T*)X, n_tokens, vocab, hidden, scale, g);
+    });
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }
 
 // ---- backward: tokens sorted by id --------------------------------------------------------
-// A radix sort from the lowest digit, two launches a digit: counts of the digits in every block of tokens, then every block
-// finds the places of its tokens from the counts of all blocks (at most kSortBlocks of them) and writes them there.  An id
-// outside the table counts as `vocab`: it is sorted behind all others.
-static constexpr int kSortBlocks = 512;
-static constexpr int kDigitBits = 10;
+// A radix sort from the lowest digit.  The first launch counts the lowest digits in every block of tokens; one launch a digit then
+// finds the places of a block's tokens from the counts of all blocks, writes them there, and counts the next digit for the blocks
+// that they come to lie in (whole numbers: the order of these atomics is not seen).  An id outside the table counts as `vocab`:
+// it is sorted behind all others.
+static constexpr int kSortBlocks = 512;  // at most
+static constexpr int kDigitBits = 10;    // at most
+static constexpr int kSortBlockMin = 512;  // tokens
 
 struct SortPlan {
     int bits, passes, digit;  // of the key, digits, bits a digit
@@ -82,60 +116,146 @@ static SortPlan plan_sort(int n, int vocab) {
     while (p.bits < 31 && (1u << p.bits) <= (unsigned)vocab) ++p.bits;
     p.passes = ceil_div(p.bits, kDigitBits);
     p.digit = ceil_div(p.bits, p.passes);
-    p.per_block = std::max(1024, (int)round_up((size_t)ceil_div(n, kSortBlocks), 256));
+    p.per_block = std::max(kSortBlockMin, (int)round_up((size_t)ceil_div(n, kSortBlocks), 256));
     p.blocks = ceil_div(n, p.per_block);
     return p;
 }
 
 __device__ __forceinline__ int key_of(int id, int vocab) { return (unsigned)id < (unsigned)vocab ? id : vocab; }
 
-__global__ __launch_bounds__(256) void k_sort_count(const int* __restrict__ keys, int n, int vocab, int shift, int bins, int per_block,
-                                                    int* __restrict__ counts) {
+// where (may be null): where[v] = some token with id v; nothing else of it is written, a reader checks what it finds there
+// against the ids.  clear: the counts of the digits behind the lowest one.
+__global__ __launch_bounds__(256) void k_sort_count(const int* __restrict__ ids, int n, int vocab, int bins, int per_block, int* __restrict__ counts,
+                                                    int* __restrict__ clear, int n_clear, int* __restrict__ where) {
     __shared__ int hist[1 << kDigitBits];
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n_clear; i += gridDim.x * 256) clear[i] = 0;
     for (int b = threadIdx.x; b < bins; b += 256) hist[b] = 0;
     __syncthreads();
     const int begin = blockIdx.x * per_block, end = min(n, begin + per_block);
-    for (int t = begin + threadIdx.x; t < end; t += 256) atomicAdd(&hist[(key_of(keys[t], vocab) >> shift) & (bins - 1)], 1);
+    for (int t = begin + threadIdx.x; t < end; t += 256) {
+        const int key = key_of(ids[t], vocab);
+        atomicAdd(&hist[key & (bins - 1)], 1);
+        if (where && key < vocab) where[key] = t;
+    }
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += 256) counts[(long long)blockIdx.x * bins + b] = hist[b];
 }
 
-// tokens == null: the order before the first digit.  where (may be null): where[v] = some token with id v; nothing else of it is
-// written, a reader checks what it finds there against the ids.
-__global__ __launch_bounds__(256) void k_sort_place(const int* __restrict__ keys, const int* __restrict__ tokens, int n, int vocab, int shift,
-                                                    int digit_bits, int per_block, const int* __restrict__ counts, int blocks,
-                                                    int* __restrict__ keys_out, int* __restrict__ tokens_out, int* __restrict__ where) {
-    constexpr int kBins = 1 << kDigitBits;
-    __shared__ int base[kBins];             // tokens of lower digits, and of this digit in blocks before this one
-    __shared__ int place[4][kBins];         // first place of this digit's tokens of every wavefront
-    __shared__ int sums[4];
-    const int bins = 1 << digit_bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int before[kBins / 256], total[kBins / 256];
+// Zeros a work-group's rows of a table, the block-th of the grid; present(row): whether a token has it.
+template <typename T, int kVec, typename F>
+__device__ __forceinline__ void zero_block(T* __restrict__ dW, int block, int vocab, int hidden, const RowGrid& g, F present) {
+    typedef typename Piece<T, kVec>::type vec;
+    int segment;
+    const long long row = first_row(g, block, &segment) + (threadIdx.x >> g.log_lanes);
+    const auto zero = [&](long long r) {
+        if (r >= vocab || present(r)) return;
+        // (a thread's two pieces next to one another: 154 us for 1.05 GB, 171 with the second 4 KB behind the first)
+        const int c0 = ((segment << (g.log_lanes + 1)) + 2 * (threadIdx.x & ((1 << g.log_lanes) - 1))) * kVec;
 #pragma unroll
-    for (int j = 0; j < kBins / 256; ++j) {
-        const int b = tid + 256 * j;
-        before[j] = total[j] = 0;
-        if (b < bins) {
-            for (int k = 0; k < blocks; ++k) {
-                const int c = counts[(long long)k * bins + b];
-                total[j] += c;
-                if (k < (int)blockIdx.x) before[j] += c;
-            }
-            base[b] = total[j];
+        for (int j = 0; j < 2; ++j)
+            if (c0 + j * kVec < hidden) *reinterpret_cast<vec*>(dW + r * hidden + min(c0 + j * kVec, hidden - kVec)) = vec{};
+    };
+    if (g.log_lanes >= 6) zero(__builtin_amdgcn_readfirstlane((int)row));  // (one row a wavefront: looked up as scalars)
+    else zero(row);
+}
+
+// Blocks begin .. end-1 of the table's grid.
+struct ZeroRows {
+    int n, vocab;  // tokens
+    RowGrid grid;
+    int begin, end;
+};
+template <typename T, int kVec>
+__device__ __forceinline__ void zero_rows(const ZeroRows& z, const int* __restrict__ ids, const int* __restrict__ where, T* __restrict__ dW, int hidden,
+                                          int block, int blocks) {
+    for (int b = z.begin + block; b < z.end; b += blocks)
+        zero_block<T, kVec>(dW, b, z.vocab, hidden, z.grid, [&](long long row) {
+            const int t = z.n > 0 ? where[row] : -1;  // (whatever the workspace held where no token has this id)
+            return (unsigned)t < (unsigned)z.n && ids[t] == (int)row;
+        });
+}
+template <typename T, int kVec>
+__global__ __launch_bounds__(256) void k_embed_zero(ZeroRows z, const int* __restrict__ ids, const int* __restrict__ where, T* __restrict__ dW, int hidden) {
+    zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x, gridDim.x);
+}
+
+// Up to kRankTokens tokens are sorted by one launch: a token's place is the number of tokens with a lower id, and of those with the
+// same one before it.  A work-group finds the places of 64 tokens, a token a lane; its wavefronts go over a sixteenth of all tokens
+// each, 64 of them with one load, and compare them with their own one after the other.
+static constexpr int kRankTokens = 4096;
+__global__ __launch_bounds__(1024) void k_sort_rank(const int* __restrict__ ids, int n, int vocab, int* __restrict__ keys_out, int* __restrict__ tokens_out,
+                                                    int* __restrict__ where) {
+    __shared__ int counts[16][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), block = blockIdx.x, t = block * 64 + lane;
+    const auto key_at = [&](int i) { return i < n ? min((unsigned)ids[i], (unsigned)vocab) : 0xffffffffu; };  // (none is counted behind the last)
+    const unsigned key = key_at(t);
+    const int chunks = (n + 63) / 64, per = (chunks + 15) / 16, end = min(chunks, (wave + 1) * per);
+    int count = 0;
+    unsigned next = key_at(wave * per * 64 + lane);
+    for (int c = wave * per; c < end; ++c) {
+        const unsigned others = next;
+        next = key_at((c + 1) * 64 + lane);
+        if (c == block) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) count += (unsigned)__builtin_amdgcn_readlane((int)others, i) < key + (i < lane);
+        } else {
+            const unsigned limit = key + (c < block);  // (a key is at most 2^31 - 1)
+#pragma unroll
+            for (int i = 0; i < 64; ++i) count += (unsigned)__builtin_amdgcn_readlane((int)others, i) < limit;
         }
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (b < bins) place[w][b] = 0;
     }
+    counts[wave][lane] = count;
     __syncthreads();
-    // exclusive scan over the digits, kBins / 256 consecutive ones a thread
-    int own[kBins / 256], run = 0;
+    if (wave != 0 || t >= n) return;
+    int at = 0;
 #pragma unroll
-    for (int j = 0; j < kBins / 256; ++j) {
-        const int b = tid * (kBins / 256) + j;
-        own[j] = run;
-        run += b < bins ? base[b] : 0;
+    for (int w = 0; w < 16; ++w) at += counts[w][lane];
+    keys_out[at] = (int)key;
+    tokens_out[at] = t;
+    if (where && key < (unsigned)vocab) where[key] = t;
+}
+
+struct SortPass {
+    const int *keys, *tokens;  // tokens null: the order before the first digit, keys are the ids then
+    int *keys_out, *tokens_out;
+    const int* counts;         // [block][digit]
+    int* next_counts;          // of the next digit, null for the last one
+    int n, vocab, shift, digit_bits, per_block, blocks;
+};
+
+// The work-groups behind the sort's own zero rows of the table meanwhile: the sort is a chain of latencies on a few compute units.
+// kRun consecutive digits a thread.
+template <typename T, int kVec, int kRun>
+__global__ __launch_bounds__(256) void k_sort_place(SortPass a, ZeroRows z, const int* __restrict__ ids, const int* __restrict__ where,
+                                                    T* __restrict__ dW, int hidden) {
+    if ((int)blockIdx.x >= a.blocks) {
+        zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+        return;
     }
+    constexpr int kBins = 256 * kRun;
+    __shared__ int place[4][kBins];  // first place of this digit's tokens of every wavefront
+    __shared__ int sums[4];
+    const int bins = 1 << a.digit_bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b0 = tid * kRun;
+    // tokens of a digit in all blocks, and in those before this one
+    int before[kRun], total[kRun], run = 0;
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) before[j] = total[j] = 0;
+    if (b0 < bins) {
+#pragma unroll 8
+        for (int k = 0; k < a.blocks; ++k)
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) {
+                const int c = a.counts[(long long)k * bins + b0 + j];
+                total[j] += c;
+                before[j] += k < (int)blockIdx.x ? c : 0;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) run += total[j];
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) place[w][b0 + j] = 0;
     int inc = run;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -144,28 +264,21 @@ __global__ __launch_bounds__(256) void k_sort_place(const int* __restrict__ keys
     }
     if (lane == 63) sums[wave] = inc;
     __syncthreads();
-    int ahead = inc - run;
+    int ahead = inc - run;  // tokens of lower digits
     for (int w = 0; w < wave; ++w) ahead += sums[w];
-#pragma unroll
-    for (int j = 0; j < kBins / 256; ++j) {
-        const int b = tid * (kBins / 256) + j;
-        if (b < bins) base[b] = ahead + own[j];
-    }
     // every wavefront counts its quarter of the block
-    const int quarter = per_block / 4, begin = blockIdx.x * per_block + wave * quarter, end = min(n, begin + quarter);
-    for (int t = begin + lane; t < end; t += 64) atomicAdd(&place[wave][(key_of(keys[t], vocab) >> shift) & (bins - 1)], 1);
+    const int quarter = a.per_block / 4, begin = blockIdx.x * a.per_block + wave * quarter, end = min(a.n, begin + quarter);
+    for (int t = begin + lane; t < end; t += 64) atomicAdd(&place[wave][(key_of(a.keys[t], a.vocab) >> a.shift) & (bins - 1)], 1);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kBins / 256; ++j) {
-        const int b = tid + 256 * j;
-        if (b < bins) {
-            int at = base[b] + before[j];
+    for (int j = 0; j < kRun; ++j) {
+        int at = ahead + before[j];
+        ahead += total[j];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int c = place[w][b];
-                place[w][b] = at;
-                at += c;
-            }
+        for (int w = 0; w < 4; ++w) {
+            const int c = place[w][b0 + j];
+            place[w][b0 + j] = at;
+            at += c;
         }
     }
     __syncthreads();
@@ -174,151 +287,291 @@ __global__ __launch_bounds__(256) void k_sort_place(const int* __restrict__ keys
     for (int t0 = begin; t0 < end; t0 += 64) {
         const int t = t0 + lane;
         const bool live = t < end;
-        const int key = live ? key_of(keys[t], vocab) : 0, digit = (key >> shift) & (bins - 1);
+        const int key = live ? key_of(a.keys[t], a.vocab) : 0, digit = (key >> a.shift) & (bins - 1);
+        const int token = live && a.tokens ? a.tokens[t] : t;
         unsigned long long same = __ballot(live);
-        for (int b = 0; b < digit_bits; ++b) {
+        for (int b = 0; b < a.digit_bits; ++b) {
             const unsigned long long set = __ballot((digit >> b) & 1);
             same &= (digit >> b) & 1 ? set : ~set;
         }
         const int rank = __popcll(same & ((1ull << lane) - 1));
-        const int at = live ? mine[digit] : 0;
+        const int at = (live ? mine[digit] : 0) + rank;
         __builtin_amdgcn_wave_barrier();  // (a wavefront's LDS accesses are carried out in their order)
         if (live && rank == 0) mine[digit] = at + __popcll(same);
         __builtin_amdgcn_wave_barrier();
         if (live) {
-            const int token = tokens ? tokens[t] : t;
-            keys_out[at + rank] = key;
-            tokens_out[at + rank] = token;
-            if (where && key < vocab) where[key] = token;
+            a.keys_out[at] = key;
+            a.tokens_out[at] = token;
+            if (a.next_counts) atomicAdd(&a.next_counts[(long long)(at / a.per_block) * bins + ((key >> (a.shift + a.digit_bits)) & (bins - 1))], 1);
         }
     }
 }
 
 // ---- backward: sums ----------------------------------------------------------------------
-// kPart sorted tokens a wavefront and 64 * kVec columns.  A row whose tokens lie in one part is finished here; what crosses
-// into other parts is left as fp32 sums, [part][0] of the row that came from the part before, [part][1] of the one that
-// begins here and goes on.
+// A wavefront takes the rows whose tokens begin among its `part` sorted tokens (at most kPart), in 64 * kVec columns, and sums
+// each to its end, also past its own tokens.  The work-groups from `blocks` on zero rows.  Only rows of more than two parts' tokens are cut: every wavefront sums those among its
+// own tokens and leaves them in fp32, [part][1] where the row begins here, [part][0] where it came from the part before.
 static constexpr int kPart = 32;
+__host__ __device__ inline int longest_whole(int part_len) { return 2 * part_len; }  // at most 64: the keys that a wavefront looks at
 
-template <typename T, int kVec>
-__device__ __forceinline__ void store_row(T* dst, const float (&s)[kVec], float scale, int accumulate) {
-    typedef T vec __attribute__((ext_vector_type(kVec)));
-    vec o;
-    if (accumulate) {
-        o = *reinterpret_cast<const vec*>(dst);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) o[e] = (T)((float)o[e] + scale * s[e]);
+template <typename T, int kVec, typename V>
+__device__ __forceinline__ void store_own(T* p, const V& v, int skip) {
+    if (skip == 0) {
+        __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
     } else {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) o[e] = (T)(scale * s[e]);
+        for (int e = 0; e < kVec; ++e)
+            if (e >= skip) p[e] = v[e];
     }
-    *reinterpret_cast<vec*>(dst) = o;
 }
 
-template <typename T, int kVec>
+template <typename T, int kVec, bool kAccumulate>
 __global__ __launch_bounds__(256) void k_embed_sums(const int* __restrict__ keys, const int* __restrict__ tokens, int n, int vocab, int hidden,
-                                                    const T* __restrict__ dX, float scale, int accumulate, T* __restrict__ dW,
-                                                    float* __restrict__ partial, int stride, int tiles, long long units) {
-    typedef T vec __attribute__((ext_vector_type(kVec)));
+                                                    const T* __restrict__ dX, float scale, T* __restrict__ dW, float* __restrict__ partial,
+                                                    int* __restrict__ cut, int stride, int part_len, int tiles, long long units, int blocks, ZeroRows z,
+                                                    const int* __restrict__ ids, const int* __restrict__ where) {
+    if ((int)blockIdx.x >= blocks) {
+        zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x - blocks, gridDim.x - blocks);
+        return;
+    }
+    typedef typename Piece<T, kVec>::type vec;
+    constexpr int kBatch = 8;  // rows that are on their way while as many are summed
     const int lane = threadIdx.x & 63;
-    for (long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (long long)gridDim.x * 4) {
+    for (long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (long long)blocks * 4) {
         const int part = __builtin_amdgcn_readfirstlane((int)(u / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(u % tiles));
-        const int p0 = part * kPart, count = min(kPart, n - p0), c = (tile * 64 + lane) * kVec;
-        const bool in = c < hidden;
-        // the keys of the part, of its neighbours, and the tokens
-        const int my_key = lane < count ? keys[p0 + lane] : -1, my_token = lane < count ? tokens[p0 + lane] : 0;
-        const int key_before = p0 > 0 ? keys[p0 - 1] : -1, key_behind = p0 + count < n ? keys[p0 + count] : -1;
+        const int p0 = part * part_len, own = (tile * 64 + lane) * kVec;
+        const int longest = longest_whole(part_len);
+        const bool in = own < hidden;
+        // the last lane of a row may have fewer columns of its own: it reads some of the lane's before it too, and stores none of them
+        const int c = min(own, hidden - kVec);
+        // keys of the 64 tokens before the part, of its own and those behind it up to 128; -1 where there are none
+        const int kb = p0 - 64 + lane >= 0 ? keys[p0 - 64 + lane] : -1;
+        const int k0 = p0 + lane < n ? keys[p0 + lane] : -1, k1 = p0 + 64 + lane < n ? keys[p0 + 64 + lane] : -1;
+        const int t0 = p0 + lane < n ? tokens[p0 + lane] : 0, t1 = p0 + 64 + lane < n ? tokens[p0 + 64 + lane] : 0;
+        const int key_first = __builtin_amdgcn_readlane(k0, 0);
+        // bit i: the row of token i ends with it
+        const int behind0 = __shfl_down(k0, 1, 64), behind1 = __shfl_down(k1, 1, 64), k1_first = __builtin_amdgcn_readlane(k1, 0);
+        const unsigned long long ends0 = __ballot((lane == 63 ? k1_first : behind0) != k0);
+        const unsigned long long ends1 = __ballot((lane == 63 ? -2 : behind1) != k1);
+        // (an index of a row's last token from i on; the rows that are asked for end before token 127, or are long)
+        const auto end_of = [&](int i) {
+            const unsigned long long lo = i < 64 ? ends0 >> i : 0, hi = i < 64 ? ends1 : ends1 >> (i - 64);
+            return lo ? i + __ffsll(lo) - 1 : (i < 64 ? 64 : i) + (hi ? __ffsll(hi) - 1 : 63);
+        };
+        int begin = 0, end = min(part_len, n - p0), first_slot = -1, last_slot = -1;
+        const unsigned long long padded = __ballot(k0 < 0 || k0 >= vocab);
+        if (padded) end = min(end, __ffsll(padded) - 1);  // padding: behind all others
+        if (end > 0) {
+            const unsigned long long others = __ballot(kb != key_first);
+            const int back = others ? __clzll(others) : 64;  // tokens of the first row before the part
+            if (back > 0) {
+                const int last = end_of(0);
+                if (back + last + 1 > longest) first_slot = 0;
+                else begin = last + 1;
+            }
+            // the row of the part's last token, if it goes on and is not the first one cut above
+            const int last = end_of(end - 1);
+            if (last >= end) {
+                const int key = __builtin_amdgcn_readlane(k0, end - 1);
+                const unsigned long long same = __ballot(lane < end && k0 == key);
+                const int start = __ffsll(same) - 1;
+                if (start > 0 || back == 0) {
+                    if (last - start + 1 > longest) last_slot = 1;
+                    else end = last + 1;
+                }
+            }
+        }
+        if (tile == 0 && lane == 0) cut[part] = last_slot == 1;
         float s[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) s[e] = 0.f;
-        bool begins = __builtin_amdgcn_readlane(my_key, 0) != key_before;
-        for (int i = 0; i < count; ++i) {
-            const int key = __builtin_amdgcn_readlane(my_key, i);
-            if (key >= vocab) break;  // padding: behind all others
-            const int token = __builtin_amdgcn_readlane(my_token, i);
-            if (in) {
-                const vec v = *reinterpret_cast<const vec*>(dX + (long long)token * hidden + c);
+        // Read with all lanes running and before a choice is made: what lanes that a branch has switched off hold in a register that
+        // was written inside it is not defined, and a lane is read whether it is switched off or not.
+        const auto at = [&](int v0, int v1, int i) {
+            const int a = __builtin_amdgcn_readlane(v0, i & 63), b = __builtin_amdgcn_readlane(v1, i & 63);
+            return i < 64 ? a : b;
+        };
+        const auto ends_at = [&](int i) { return ((i < 64 ? ends0 : ends1) >> (i & 63) & 1) != 0; };
+        const auto load = [&](int g, vec (&row)[kBatch], vec (&old)[kBatch]) {
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) s[e] += (float)v[e];
+            for (int j = 0; j < kBatch; ++j) {
+                const int i = g + j;
+                if (i < end) {
+                    const int token = at(t0, t1, i), key = at(k0, k1, i);
+                    row[j] = in ? __builtin_nontemporal_load(reinterpret_cast<const vec*>(dX + (long long)token * hidden + c)) : vec{};
+                    if constexpr (kAccumulate)
+                        if (ends_at(i)) old[j] = in ? *reinterpret_cast<const vec*>(dW + (long long)key * hidden + c) : vec{};
+                }
             }
-            const int next = i + 1 < count ? __builtin_amdgcn_readlane(my_key, i + 1) : key_behind;
-            if (next != key || i + 1 == count) {
-                const bool ends = next != key;
-                if (in) {
-                    if (begins && ends) {
-                        store_row<T, kVec>(dW + (long long)key * hidden + c, s, scale, accumulate);
-                    } else {
-                        float* p = partial + ((long long)part * 2 + (begins ? 1 : 0)) * stride + c;
+        };
+        const auto sum = [&](int g, const vec (&row)[kBatch], const vec (&old)[kBatch]) {
 #pragma unroll
-                        for (int e = 0; e < kVec; ++e) p[e] = s[e];
+            for (int j = 0; j < kBatch; ++j) {
+                const int i = g + j;
+                if (i < end) {
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) s[e] += (float)row[j][e];
+                    const bool ends = ends_at(i);
+                    const int key = at(k0, k1, i);
+                    if (ends || i + 1 == end) {
+                        const int slot = first_slot >= 0 ? first_slot : !ends ? last_slot : -1;
+                        if (in && slot >= 0) {
+                            float* p = partial + ((long long)part * 2 + slot) * stride + c;
+#pragma unroll
+                            for (int e = 0; e < kVec; ++e)
+                                if (c + e >= own) p[e] = s[e];
+                        } else if (in) {
+                            vec o;
+#pragma unroll
+                            for (int e = 0; e < kVec; ++e) o[e] = (T)(kAccumulate ? (float)old[j][e] + scale * s[e] : scale * s[e]);
+                            store_own<T, kVec>(dW + (long long)key * hidden + c, o, own - c);
+                        }
+                        first_slot = -1;
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) s[e] = 0.f;
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) s[e] = 0.f;
-                begins = true;
             }
+        };
+        vec row_a[kBatch], row_b[kBatch], old_a[kBatch], old_b[kBatch];
+        load(begin, row_a, old_a);
+        for (int g = begin; g < end; g += 2 * kBatch) {
+            load(g + kBatch, row_b, old_b);
+            sum(g, row_a, old_a);
+            load(g + 2 * kBatch, row_a, old_a);
+            sum(g + kBatch, row_b, old_b);
         }
     }
 }
 
-// Rows that lie in several parts: the part in which a row begins adds what the parts behind it have of it, in their order.
-// One work-group a part and 256 columns, four wavefronts with a quarter of the parts each.
+// The rows that were cut: the part in which a row begins adds what the parts behind it have of it, in their order.  A work-group
+// looks at kJoinParts parts, in 256 columns; its four wavefronts take a quarter of a row's parts each.
+static constexpr int kJoinParts = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void k_embed_join(const int* __restrict__ keys, int n, int vocab, int hidden, float scale, int accumulate,
-                                                    T* __restrict__ dW, const float* __restrict__ partial, int stride, int parts) {
-    __shared__ float red[4][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = blockIdx.y * 256;
-    for (int part = blockIdx.x; part < parts - 1; part += gridDim.x) {
-        const int p0 = part * kPart, key = keys[p0 + kPart - 1];
-        if (key >= vocab || keys[p0 + kPart] != key) continue;                  // no row goes on
-        if (keys[p0] == key && p0 > 0 && keys[p0 - 1] == key) continue;          // it began before this part
-        int more = 0;                                                            // parts behind this one that it lies in
-        for (int base = part + 1; base < parts; base += 64) {
-            const unsigned long long other = __ballot(base + lane >= parts || keys[(long long)min(base + lane, parts - 1) * kPart] != key);
+__global__ __launch_bounds__(256) void k_embed_join(const int* __restrict__ keys, int n, int hidden, float scale, int accumulate, T* __restrict__ dW,
+                                                    const float* __restrict__ partial, const int* __restrict__ cut, int stride, int part_len, int parts) {
+    typedef float vec __attribute__((ext_vector_type(4)));
+    __shared__ vec red[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = blockIdx.y * 256, base = blockIdx.x * kJoinParts;
+    unsigned long long todo = __ballot(lane < kJoinParts && base + lane < parts && cut[base + lane]);
+    for (; todo; todo &= todo - 1) {
+        const int part = base + __ffsll(todo) - 1, key = keys[(part + 1) * part_len];  // (a cut row goes on behind its part)
+        int more = 0;                                                                  // parts behind this one that it lies in
+        for (int b = part + 1; b < parts; b += 64) {
+            const unsigned long long other = __ballot(b + lane >= parts || keys[(long long)min(b + lane, parts - 1) * part_len] != key);
             more += other ? __ffsll(other) - 1 : 64;
             if (other) break;
         }
         // pieces 0 .. more: the part's own, then theirs
-        const int pieces = more + 1, per = (pieces + 3) / 4, first = wave * per, last = min(pieces, first + per);
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int i = first; i < last; ++i) {
-            const float* p = partial + ((long long)(part + i) * 2 + (i == 0 ? 1 : 0)) * stride + c0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c0 + 64 * j + lane < hidden) s[j] += p[64 * j + lane];
+        const int per = (more + 4) / 4, first = wave * per, last = min(more + 1, first + per);
+        vec s = {0.f, 0.f, 0.f, 0.f};
+        const float* p = partial + (long long)part * 2 * stride + c0 + 4 * lane;
+        if (c0 + 4 * lane < stride) {
+#pragma unroll 8
+            for (int i = first; i < last; ++i) s += *reinterpret_cast<const vec*>(p + ((long long)i * 2 + (i == 0 ? 1 : 0)) * stride);
         }
         __syncthreads();  // (the sums of the row before have been read)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) red[wave][64 * j + lane] = s[j];
+        red[wave][lane] = s;
         __syncthreads();
         const int c = c0 + threadIdx.x;
         if (c < hidden) {
-            const float sum = red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+            const float* r = reinterpret_cast<const float*>(red) + threadIdx.x;
+            const float sum = (r[0] + r[256]) + (r[512] + r[768]);
             T* dst = dW + (long long)key * hidden + c;
             *dst = (T)(accumulate ? (float)*dst + scale * sum : scale * sum);
         }
     }
 }
 
-// Rows that no token has: zeros.  where[v] is whatever the workspace held unless a token has id v.
-template <typename T, int kVec>
-__global__ __launch_bounds__(256) void k_embed_zero(const int* __restrict__ ids, int n, const int* __restrict__ where, int vocab, int hidden,
-                                                    T* __restrict__ dW) {
-    typedef T vec __attribute__((ext_vector_type(kVec)));
-    for (int v = blockIdx.x; v < vocab; v += gridDim.x) {
-        const int t = n > 0 ? where[v] : -1;
-        if ((unsigned)t < (unsigned)n && ids[t] == v) continue;
-        const vec zero = {};
-        for (int c = threadIdx.x * kVec; c < hidden; c += 256 * kVec) *reinterpret_cast<vec*>(dW + (long long)v * hidden + c) = zero;
+// ---- backward of a few tokens: one launch --------------------------------------------------
+// A work-group a token and 64 * kVec columns: each of its wavefronts compares the token's id with a quarter of all others, and sums
+// the rows of those that have the same; nothing is done if one of them comes before the token.  The work-groups behind these zero
+// the rows that no token has, and find out from the ids which those are.
+static constexpr int kFewTokens = 2048;
+static bool few_tokens(int n, int tiles) { return n <= kFewTokens && (long long)n * n * tiles <= 1 << 23; }
+
+template <typename T, int kVec, bool kAccumulate>
+__global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, int n, int vocab, int hidden, const T* __restrict__ dX, float scale,
+                                                   T* __restrict__ dW, int tiles, int units, RowGrid g) {
+    typedef typename Piece<T, kVec>::type vec;
+    constexpr int kBatch = 16;
+    __shared__ unsigned short list[kFewTokens + 256];  // tokens of the row, ascending in every quarter
+    __shared__ float red[3][64 * kVec];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if constexpr (!kAccumulate) {
+        if ((int)blockIdx.x >= units) {
+            __shared__ unsigned present[256 / 32];  // of the work-group's rows
+            for (int b = blockIdx.x - units; b < g.blocks; b += gridDim.x - units) {
+                const int rows = 256 >> g.log_lanes;
+                int segment;
+                const long long row0 = first_row(g, b, &segment);
+                __syncthreads();  // (what the round before had here has been read)
+                if (tid < 256 / 32) present[tid] = 0;
+                __syncthreads();
+                for (int t = tid; t < n; t += 256) {
+                    const long long r = ids[t] - row0;
+                    if (r >= 0 && r < rows) atomicOr(&present[r >> 5], 1u << (r & 31));
+                }
+                __syncthreads();
+                zero_block<T, kVec>(dW, b, vocab, hidden, g, [&](long long row) { return (present[(row - row0) >> 5] >> ((row - row0) & 31) & 1) != 0; });
+            }
+            return;
+        }
     }
+    const int token = blockIdx.x / tiles, own = (blockIdx.x % tiles * 64 + lane) * kVec, id = ids[token];
+    if ((unsigned)id >= (unsigned)vocab) return;
+    const bool in = own < hidden;
+    const int c = min(own, hidden - kVec);  // (as in k_embed_sums)
+    const int quarter = (n + 255) / 256 * 64, begin = wave * quarter, end = min(n, begin + quarter);
+    unsigned short* mine = list + begin;
+    int count = 0;
+    bool earlier = false;
+#pragma unroll 4
+    for (int t0 = begin; t0 < end; t0 += 64) {
+        const int t = t0 + lane;
+        const bool same = t < end && ids[t] == id;
+        const unsigned long long set = __ballot(same);
+        earlier |= same && t < token;
+        if (same) mine[count + __popcll(set & ((1ull << lane) - 1))] = (unsigned short)t;
+        count += __popcll(set);
+    }
+    if (__syncthreads_or(earlier)) return;
+    vec old = {};
+    T* dst = dW + (long long)id * hidden + c;
+    if (kAccumulate && in && wave == 0) old = *reinterpret_cast<const vec*>(dst);
+    float s[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) s[e] = 0.f;
+    for (int i = 0; i < count; i += kBatch) {
+        vec row[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i + j < count && in) row[j] = *reinterpret_cast<const vec*>(dX + (long long)mine[i + j] * hidden + c);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i + j < count)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) s[e] += (float)row[j][e];
+    }
+    if (wave > 0)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) red[wave - 1][64 * e + lane] = s[e];
+    __syncthreads();
+    if (wave > 0 || !in) return;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+        const float sum = s[e] + ((red[0][64 * e + lane] + red[1][64 * e + lane]) + red[2][64 * e + lane]);
+        old[e] = (T)(kAccumulate ? (float)old[e] + scale * sum : scale * sum);
+    }
+    store_own<T, kVec>(dst, old, own - c);
 }
 
 struct EmbedPlan {
     SortPlan sort;
-    int *keys[2], *tokens[2], *counts, *where;
+    int *keys[2], *tokens[2], *counts, *where, *cut;
     float* partial;
-    int parts, stride;
-    size_t bytes;
+    int part_len, parts, stride;
+    size_t counts_a_pass, bytes;
 };
 static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_bytes) {
     Arena a(ws, ws_bytes);
@@ -329,9 +582,14 @@ static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_by
         p.keys[i] = static_cast<int*>(a.take((size_t)n * sizeof(int)));
         p.tokens[i] = static_cast<int*>(a.take((size_t)n * sizeof(int)));
     }
-    p.counts = static_cast<int*>(a.take(((size_t)p.sort.blocks << p.sort.digit) * sizeof(int)));
+    p.counts_a_pass = (size_t)p.sort.blocks << p.sort.digit;
+    p.counts = static_cast<int*>(a.take(p.counts_a_pass * p.sort.passes * sizeof(int)));
     p.where = static_cast<int*>(a.take((size_t)vocab * sizeof(int)));
-    p.parts = ceil_div(n, kPart);
+    // parts as long as leaves 2048 wavefronts (of 16-byte lanes): 
+    p.part_len = kPart;
+    while (p.part_len > 8 && (long long)ceil_div(n, p.part_len) * ceil_div(hidden, 512) < 2048) p.part_len /= 2;
+    p.parts = ceil_div(n, p.part_len);
+    p.cut = static_cast<int*>(a.take((size_t)p.parts * sizeof(int)));
     p.stride = (int)round_up((size_t)hidden, 8);
     p.partial = static_cast<float*>(a.take((size_t)p.parts * 2 * p.stride * sizeof(float)));
     p.bytes = round_up(a.used, 256);
@@ -340,51 +598,72 @@ static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_by
 
 size_t embed_backward_workspace_bytes(int vocab, int hidden, int n_tokens) { return plan_embed(vocab, hidden, n_tokens, nullptr, 0).bytes; }
 
-template <typename T>
+template <typename T, int kVec>
 static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* dX, int n, int vocab, int hidden, float scale, int accumulate,
                                   T* dW, hipStream_t stream) {
-    constexpr int kVec = 16 / sizeof(T);
-    const bool vec = hidden % kVec == 0;
+    const RowGrid table = row_grid(accumulate ? 0 : vocab, hidden, kVec);
+    ZeroRows z{n, vocab, table, 0, 0};
+    if (n <= 0) {
+        z.end = table.blocks;
+        if (z.end) k_embed_zero<T, kVec><<<std::min(z.end, kMaxBlocks), 256, 0, stream>>>(z, ids, p.where, dW, hidden);
+        return;
+    }
+    const int tiles = ceil_div(hidden, 64 * kVec);
+    if (few_tokens(n, tiles)) {
+        const int units = n * tiles;
+        if (accumulate)
+            k_embed_few<T, kVec, true><<<units, 256, 0, stream>>>(ids, n, vocab, hidden, dX, scale, dW, tiles, units, table);
+        else
+            k_embed_few<T, kVec, false><<<units + std::min(table.blocks, kMaxBlocks), 256, 0, stream>>>(ids, n, vocab, hidden, dX, scale, dW, tiles, units, table);
+        return;
+    }
     const int *keys = ids, *tokens = nullptr;
-    if (n > 0) {
-        const int bins = 1 << p.sort.digit;
-        for (int i = 0; i < p.sort.passes; ++i) {
-            const int shift = i * p.sort.digit;
-            k_sort_count<<<p.sort.blocks, 256, 0, stream>>>(keys, n, vocab, shift, bins, p.sort.per_block, p.counts);
-            k_sort_place<<<p.sort.blocks, 256, 0, stream>>>(keys, tokens, n, vocab, shift, p.sort.digit, p.sort.per_block, p.counts, p.sort.blocks,
-                                                            p.keys[i & 1], p.tokens[i & 1], i == 0 && !accumulate ? p.where : nullptr);
+    if (n <= kRankTokens) {
+        k_sort_rank<<<ceil_div(n, 64), 1024, 0, stream>>>(ids, n, vocab, p.keys[0], p.tokens[0], accumulate ? nullptr : p.where);
+        keys = p.keys[0];
+        tokens = p.tokens[0];
+    } else {
+        const SortPlan& o = p.sort;
+        const int bins = 1 << o.digit;
+        k_sort_count<<<o.blocks, 256, 0, stream>>>(ids, n, vocab, bins, o.per_block, p.counts, p.counts + p.counts_a_pass,
+                                                   (int)(p.counts_a_pass * (o.passes - 1)), accumulate ? nullptr : p.where);
+        for (int i = 0; i < o.passes; ++i) {
+            int* counts = p.counts + p.counts_a_pass * i;
+            const SortPass s{keys, tokens, p.keys[i & 1], p.tokens[i & 1], counts, i + 1 < o.passes ? counts + p.counts_a_pass : nullptr,
+                             n, vocab, i * o.digit, o.digit, o.per_block, o.blocks};
+            z.begin = z.end;  // every launch its share of the rows
+            z.end = (int)((long long)table.blocks * (i + 1) / o.passes);
+            const int grid = o.blocks + std::min(z.end - z.begin, kMaxBlocks);
+            if (o.digit == 10) k_sort_place<T, kVec, 4><<<grid, 256, 0, stream>>>(s, z, ids, p.where, dW, hidden);
+            else if (o.digit == 9) k_sort_place<T, kVec, 2><<<grid, 256, 0, stream>>>(s, z, ids, p.where, dW, hidden);
+            else k_sort_place<T, kVec, 1><<<grid, 256, 0, stream>>>(s, z, ids, p.where, dW, hidden);
             keys = p.keys[i & 1];
             tokens = p.tokens[i & 1];
         }
     }
-    if (!accumulate) {
-        const int grid = std::min(vocab, 1 << 20);
-        if (vec)
-            k_embed_zero<T, kVec><<<grid, 256, 0, stream>>>(ids, n, p.where, vocab, hidden, dW);
-        else
-            k_embed_zero<T, 1><<<grid, 256, 0, stream>>>(ids, n, p.where, vocab, hidden, dW);
-    }
-    if (n <= 0) return;
-    const int tiles = ceil_div(hidden, 64 * (vec ? kVec : 1));
+    z.begin = z.end;
+    z.end = table.blocks;
     const long long units = (long long)p.parts * tiles;
-    const int grid = (int)std::min<long long>((units + 3) / 4, 1 << 20);
-    if (vec)
-        k_embed_sums<T, kVec><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, accumulate, dW, p.partial, p.stride, tiles, units);
+    const int blocks = (int)std::min<long long>((units + 3) / 4, 1 << 20), grid = blocks + std::min(z.end - z.begin, kMaxBlocks);
+    if (accumulate)
+        k_embed_sums<T, kVec, true><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, dW, p.partial, p.cut, p.stride, p.part_len, tiles,
+                                                              units, blocks, z, ids, p.where);
     else
-        k_embed_sums<T, 1><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, accumulate, dW, p.partial, p.stride, tiles, units);
-    if (p.parts > 1)
-        k_embed_join<T><<<dim3(std::min(p.parts - 1, 1 << 16), ceil_div(hidden, 256)), 256, 0, stream>>>(keys, n, vocab, hidden, scale, accumulate, dW,
-                                                                                                        p.partial, p.stride, p.parts);
+        k_embed_sums<T, kVec, false><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, dW, p.partial, p.cut, p.stride, p.part_len, tiles,
+                                                               units, blocks, z, ids, p.where);
+    if (n > longest_whole(p.part_len))
+        k_embed_join<T><<<dim3(ceil_div(p.parts, kJoinParts), ceil_div(hidden, 256)), 256, 0, stream>>>(keys, n, hidden, scale, accumulate, dW, p.partial, p.cut,
+                                                                                                  p.stride, p.part_len, p.parts);
 }
 
 int launch_embed_backward(alch_dtype dt, const int* ids, const void* dX, int n_tokens, int vocab, int hidden, float scale, int accumulate,
                           void* dW, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     const EmbedPlan p = plan_embed(vocab, hidden, n_tokens, workspace, workspace_bytes);
     TraceScope ts(kTraceEmbed, (double)n_tokens * hidden, ((double)n_tokens + (accumulate ? 0 : vocab)) * hidden * dtype_size(dt), stream);
-    if (dt == ALCH_BF16)
-        embed_backward_launch<__bf16>(p, ids, (const __bf16*)dX, n_tokens, vocab, hidden, scale, accumulate, (__bf16*)dW, stream);
-    else
-        embed_backward_launch<float>(p, ids, (const float*)dX, n_tokens, vocab, hidden, scale, accumulate, (float*)dW, stream);
+    with_pieces(dt, hidden, [&](auto type, auto vec) {
+        typedef decltype(type) T;
+        embed_backward_launch<T, decltype(vec)::value>(p, ids, static_cast<const T*>(dX), n_tokens, vocab, hidden, scale, accumulate, static_cast<T*>(dW), stream);
+    });
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }

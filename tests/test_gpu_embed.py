@@ -34,7 +34,7 @@ def make_ids(kind, T, V, seed=0):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,H,V,scale", [(1, 4096, 1000, 1.0), (1, 1, 1, 0.3), (487, 487, 97, 22.06), (33, 8, 50, 1.0), (5003, 256, 1000, -16.0),
-                                         (70, 8200, 31, 64.0), (3, 20000, 5, 0.5)])
+                                         (70, 8200, 31, 64.0), (3, 20000, 5, 0.5), (999, 9, 20, 2.0), (5000, 3, 20, 1.0), (1000, 1029, 300, 1.0)])
 def test_forward(T, H, V, scale, dtype):
     import paper_2503_01066_amd as A
     ids, W = make_ids("mixed", T, V), randn((V, H), dtype, 1)
@@ -79,7 +79,9 @@ def check_backward(ids, dX, V, scale, dW, old):
 CASES = [(1, 4096, 1000, "mixed"), (31, 256, 64, "mixed"), (32, 256, 64, "one"), (33, 487, 64, "one"), (64, 64, 3, "runs"), (65, 8, 1, "one"),
          (487, 4096, 5000, "mixed"), (487, 130, 128256, "ascending"), (1025, 72, 1023, "runs"), (1500, 40, 1024, "mixed"), (5003, 256, 1000, "runs"),
          (16384, 64, 128256, "runs"), (9000, 520, 7, "mixed"), (70001, 24, 40000, "one"), (200, 64, 9, "padding"), (300, 1, 17, "mixed"),
-         (2049, 8200, 300, "runs"), (4097, 16, 4097, "ascending")]
+         (2049, 8200, 300, "runs"), (300, 8, 20, "runs"), (1024, 520, 40, "runs"), (777, 33, 2, "runs"), (16500, 2104, 500, "runs"),
+         (16384, 1032, 90, "mixed"), (1025, 8, 20, "runs"), (1100, 264, 1, "one"), (1200, 64, 9, "padding"), (2000, 9, 31, "runs"), (90, 9, 31, "runs"),
+         (3000, 515, 700, "mixed"), (4097, 16, 4097, "ascending")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -22,6 +22,7 @@ def test_embed_forward_refusals():
     assert call(dt=2) == INVALID and "dtype" in _err()
     assert call(V=0) == SHAPE and call(H=0) == SHAPE and call(H=-8) == SHAPE
     assert call(n=-1) == INVALID and call(n=(1 << 30) + 1) == UNSUPPORTED and call(H=(1 << 20) + 1) == UNSUPPORTED
+    assert call(V=1 << 30, H=1 << 11) == UNSUPPORTED and "2^40" in _err()
     assert call(ids=None) == INVALID and "token_ids" in _err()
     assert call(ids=P + 2) == INVALID and "4-byte" in _err()
     assert call(W=None) == INVALID and call(W=P + 8) == INVALID and "W_embed" in _err()
@@ -42,7 +43,8 @@ def test_embed_backward_refusals():
     q = L.alch_embed_backward_workspace_bytes
     assert q(1, 100, 64, 0) > 0 and q(0, 0, 64, 5) == 0 and q(3, 100, 64, 5) == 0 and q(1, 100, 64, -1) == 0
     assert q(1, 128256, 4096, 16384) >= 128256 * 4 + 16384 * 8
-    assert q(1, 2 ** 31 - 1, 1 << 20, 1 << 30) > 1 << 36  # (the largest of all: no overflow on the way)
+    assert q(1, 1 << 20, 1 << 20, 1 << 20) > 1 << 38 and q(1, 2 ** 31 - 1, 512, 1 << 30) > 1 << 36  # (the largest: no overflow on the way)
+    assert q(1, (1 << 20) + 1, 1 << 20, 5) == 0 and q(1, 5, 1 << 20, (1 << 20) + 1) == 0
 
 
 def _grads(*rows):
