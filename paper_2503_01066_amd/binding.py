@@ -635,26 +635,32 @@ def alch_attention_forward(shape, batch, Q, K, V, stream=None):
 
 
 def _code(dtype):
-    if dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError("dtype %s: bfloat16 or float32" % dtype)
-    return ALCH_BF16 if dtype == torch.bfloat16 else ALCH_F32
+    if dtype is torch.bfloat16:
+        return ALCH_BF16
+    if dtype is torch.float32:
+        return ALCH_F32
+    raise TypeError("dtype %s: bfloat16 or float32" % dtype)
+
+
+def _dense(t, dtype, device, shape=None):
+    return t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape)
 
 
 def _check_dense(t, name, dtype, device, shape=None):
-    """A library call takes the address of a tensor alone: what else it assumes of it is checked here."""
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    """A library call takes the address of a tensor alone: what else it assumes of it is checked here.  device: its index."""
+    if not _dense(t, dtype, device, shape):
         raise ValueError("%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s%s" % (
-            name, dtype, "" if shape is None else " of shape %s" % (tuple(shape),), device, t.dtype, tuple(t.shape), t.device,
-            "" if t.is_contiguous() else ", not contiguous"))
+            name, dtype, "" if shape is None else " of shape %s" % (tuple(shape),), "the CPU" if device < 0 else "cuda:%d" % device, t.dtype,
+            tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
 
 
-def _check_current(device, stream):
-    """Kernels go to the current device; a stream that is given belongs to it."""
-    if device.type != "cuda":
-        raise ValueError("tensors on %s" % device)
-    at = torch.cuda.current_device()
-    if device.index != at or (stream is not None and stream.device_index != at):
-        raise ValueError("tensors on %s%s, the current device is %d" % (device, "" if stream is None else ", a stream of %d" % stream.device_index, at))
+def _place(device, stream):
+    """The stream of a call whose tensors are on a device (its index): kernels go to the current device, a given stream belongs to it."""
+    at = torch.cuda.current_device() if device >= 0 else None
+    if device != at or (stream is not None and stream.device_index != at):
+        raise ValueError("tensors on %s%s, the current device is %s" % ("the cpu" if device < 0 else "cuda:%d" % device,
+                                                                       "" if stream is None else ", a stream of %d" % stream.device_index, at))
+    return _raw_stream(at) if stream is None and _raw_stream is not None else _stream_handle(stream)
 
 
 def _empty(shape, dtype, device, stream, fill=torch.empty):
@@ -673,16 +679,17 @@ def embed_backward_workspace_bytes(dtype, vocab, hidden, n_tokens):
 def alch_embed_forward(token_ids, W_embed, scale=1.0, X=None, stream=None):
     """Returns X [n_tokens, hidden], X[t] = scale * W_embed[token_ids[t]] (token_ids int32 [n_tokens]; a zero row where the id
     is no row of W_embed [vocab, hidden])."""
-    L = lib()
-    dev, (vocab, hidden), n = W_embed.device, W_embed.shape, token_ids.numel()
-    _check_current(dev, stream)
-    _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
-    _check_dense(W_embed, "W_embed", W_embed.dtype, dev)
+    (vocab, hidden), (n,), dev, dt = W_embed.shape, token_ids.shape, W_embed.get_device(), W_embed.dtype
+    handle = _place(dev, stream)
+    _check_dense(token_ids, "token_ids", torch.int32, dev)
+    _check_dense(W_embed, "W_embed", dt, dev)
     if X is None:
-        X = _empty((n, hidden), W_embed.dtype, dev, stream)
+        X = _empty((n, hidden), dt, W_embed.device, stream)
     else:
-        _check_dense(X, "X", W_embed.dtype, dev, (n, hidden))
-    _check(L.alch_embed_forward(_code(W_embed.dtype), vocab, hidden, n, _ptr(token_ids), _ptr(W_embed), scale, _ptr(X), _stream_handle(stream)))
+        _check_dense(X, "X", dt, dev, (n, hidden))
+    rc = lib().alch_embed_forward(_code(dt), vocab, hidden, n, token_ids.data_ptr(), W_embed.data_ptr(), scale, X.data_ptr(), handle)
+    if rc != 0:
+        _check(rc)
     return X
 
 
@@ -690,50 +697,64 @@ def alch_embed_backward(token_ids, dX, vocab, scale=1.0, dW_embed=None, accumula
     """Returns dW_embed [vocab, hidden], dW_embed[v] (+)= scale * the sum of dX[t] over the tokens with id v.  accumulate: adds to
     dW_embed, of which only the rows that occur are touched (the gradient of a head that shares the table, for one)."""
     L = lib()
-    dev, (n, hidden) = dX.device, dX.shape
-    _check_current(dev, stream)
+    (n, hidden), (n_ids,), dev, dt = dX.shape, token_ids.shape, dX.get_device(), dX.dtype
+    handle = _place(dev, stream)
     _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
-    _check_dense(dX, "dX", dX.dtype, dev)
+    _check_dense(dX, "dX", dt, dev)
     if dW_embed is None:
-        dW_embed = _empty((vocab, hidden), dX.dtype, dev, stream, torch.zeros if accumulate else torch.empty)
+        dW_embed = _empty((vocab, hidden), dt, dX.device, stream, torch.zeros if accumulate else torch.empty)
     else:
-        _check_dense(dW_embed, "dW_embed", dX.dtype, dev, (vocab, hidden))
-    code = _code(dX.dtype)
-    ws = workspace if workspace is not None else _empty((max(L.alch_embed_backward_workspace_bytes(code, vocab, hidden, n), 256),), torch.uint8, dev, stream)
-    _check_dense(ws, "workspace", torch.uint8, dev)
-    _check(L.alch_embed_backward(code, vocab, hidden, n, _ptr(token_ids), _ptr(dX), scale, _ptr(dW_embed), 1 if accumulate else 0, _ptr(ws),
-                                 ws.numel(), _stream_handle(stream)))
+        _check_dense(dW_embed, "dW_embed", dt, dev, (vocab, hidden))
+    code = _code(dt)
+    if workspace is None:
+        workspace = _empty((max(L.alch_embed_backward_workspace_bytes(code, vocab, hidden, n), 256),), torch.uint8, dX.device, stream)
+    else:
+        _check_dense(workspace, "workspace", torch.uint8, dev)
+    _check(L.alch_embed_backward(code, vocab, hidden, n, token_ids.data_ptr(), dX.data_ptr(), scale, dW_embed.data_ptr(), 1 if accumulate else 0,
+                                 workspace.data_ptr(), workspace.numel(), handle))
     return dW_embed
-
-
-def _check_apart(ranges):
-    """ranges: (first byte, byte behind the last, written, name).  What is written overlaps nothing else."""
-    ranges = sorted(r for r in ranges if r[1] > r[0])
-    end, last = 0, None      # of the ranges before, the one that reaches furthest, and the written one that does
-    wend, wlast = 0, None
-    for a, b, written, name in ranges:
-        if a < (end if written else wend):
-            raise ValueError("%s overlaps %s" % (name, last if written else wlast))
-        if b > end:
-            end, last = b, name
-        if written and b > wend:
-            wend, wlast = b, name
 
 
 class _TensorTable:
     """Pointers and lengths of many tensors: a host array for the library's checks, the same on the device for its kernels,
     uploaded once.  Keeps the tensors, which must stay where they are."""
 
-    def _make(self, row, rows, device, keep):
-        self.n, self.device, self.keep = len(rows), device, keep
-        self.host = (row * max(self.n, 1))(*[row(*r) for r in rows])
+    def __init__(self, row, first, device):
+        self.row, self.rows, self.ranges, self.keep = row, [], [], []
+        self.device = first[0].device if first else torch.zeros(0, device=device).device
+        self.index = -1 if self.device.type == "cpu" else self.device.index
+
+    def _take(self, t, name, i, dtype, shape=None, written=False, listed=True):
+        """The address of a tensor, checked; it is among those that may not overlap, if listed."""
+        if not _dense(t, dtype, self.index, shape):
+            _check_dense(t, "%s[%d]" % (name, i), dtype, self.index, shape)
+        at = t.data_ptr()
+        if listed:
+            self.ranges.append((at, at + t.numel() * t.element_size(), written, name, i))
+        self.keep.append(t)
+        return at
+
+    def _upload(self):
+        end, last = 0, None      # of the ranges so far the one that reaches furthest, and the written one that does
+        wend, wlast = 0, None
+        for r in sorted(r for r in self.ranges if r[1] > r[0]):
+            a, b, written = r[:3]
+            if a < (end if written else wend):
+                raise ValueError("%s[%d] overlaps %s[%d]" % (r[3:] + (last if written else wlast)[3:]))
+            if b > end:
+                end, last = b, r
+            if written and b > wend:
+                wend, wlast = b, r
+        self.n = len(self.rows)
+        self.host = (self.row * max(self.n, 1))(*self.rows)
         self.host_ptr = C.addressof(self.host)
-        self.dev = torch.frombuffer(bytearray(C.string_at(self.host_ptr, C.sizeof(self.host))), dtype=torch.uint8).to(device)
+        self.dev = torch.frombuffer(bytearray(self.host), dtype=torch.uint8).to(self.device)
         self.dev_ptr = self.dev.data_ptr()
+        del self.rows, self.ranges
 
-
-def _bytes_of(t, written, name):
-    return (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), written, name)
+    def _used(self, stream):
+        if stream is not None:  # (the table may be dropped behind the call: its memory is not handed out before the call has run)
+            self.dev.record_stream(stream)
 
 
 class GradList(_TensorTable):
@@ -745,18 +766,12 @@ class GradList(_TensorTable):
         outs = [None] * len(grads) if outs is None else list(outs)
         if len(outs) != len(grads):
             raise ValueError("%d outs for %d gradients" % (len(outs), len(grads)))
-        dev = grads[0].device if grads else torch.zeros(0, device=device).device
-        rows, ranges = [], []
+        super().__init__(GradTensor, grads, device)
         for i, (g, o) in enumerate(zip(grads, outs)):
-            _check_dense(g, "grads[%d]" % i, g.dtype, dev)
-            if o is not None:
-                _check_dense(o, "outs[%d]" % i, g.dtype, dev, g.shape)
-                ranges.append(_bytes_of(o, True, "outs[%d]" % i))
-            if o is None or o.data_ptr() != g.data_ptr():
-                ranges.append(_bytes_of(g, False, "grads[%d]" % i))
-            rows.append((g.data_ptr(), _ptr(o), g.numel(), _code(g.dtype), 0))
-        _check_apart(ranges)
-        self._make(GradTensor, rows, dev, (grads, outs))
+            dt = g.dtype
+            to = None if o is None else self._take(o, "outs", i, dt, g.shape, written=True)
+            self.rows.append((self._take(g, "grads", i, dt, listed=to != g.data_ptr()), to, g.numel(), _code(dt), 0))
+        self._upload()
 
 
 class AdamwList(_TensorTable):
@@ -764,27 +779,21 @@ class AdamwList(_TensorTable):
     master copy or None, and its weight decay (one number for all, or one each).  device: where a list without tensors belongs."""
 
     def __init__(self, params, grads, m, v, masters=None, weight_decay=0.0, device="cuda"):
-        params = list(params)
+        params, grads, m, v = list(params), list(grads), list(m), list(v)
         n = len(params)
         masters = [None] * n if masters is None else list(masters)
         decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
-        lists = dict(grads=list(grads), m=list(m), v=list(v), masters=masters, weight_decay=decay)
-        for name, l in lists.items():
+        for name, l in (("grads", grads), ("m", m), ("v", v), ("masters", masters), ("weight_decay", decay)):
             if len(l) != n:
                 raise ValueError("%d %s for %d parameters" % (len(l), name, n))
-        dev = params[0].device if params else torch.zeros(0, device=device).device
-        rows, ranges = [], []
+        super().__init__(AdamwTensor, params, device)
         for i, p in enumerate(params):
-            g, mi, vi, w = lists["grads"][i], lists["m"][i], lists["v"][i], masters[i]
-            _check_dense(p, "params[%d]" % i, p.dtype, dev)
-            _check_dense(g, "grads[%d]" % i, p.dtype, dev, p.shape)
-            ranges += [_bytes_of(p, True, "params[%d]" % i), _bytes_of(g, False, "grads[%d]" % i)]
-            for t, name in ((mi, "m"), (vi, "v")) + (((w, "masters"),) if w is not None else ()):
-                _check_dense(t, "%s[%d]" % (name, i), torch.float32, dev, p.shape)
-                ranges.append(_bytes_of(t, True, "%s[%d]" % (name, i)))
-            rows.append((p.data_ptr(), g.data_ptr(), _ptr(w), mi.data_ptr(), vi.data_ptr(), p.numel(), decay[i], _code(p.dtype)))
-        _check_apart(ranges)
-        self._make(AdamwTensor, rows, dev, (params, lists))
+            dt, shape, f32 = p.dtype, p.shape, torch.float32
+            self.rows.append((self._take(p, "params", i, dt, written=True), self._take(grads[i], "grads", i, dt, shape),
+                              None if masters[i] is None else self._take(masters[i], "masters", i, f32, shape, written=True),
+                              self._take(m[i], "m", i, f32, shape, written=True), self._take(v[i], "v", i, f32, shape, written=True),
+                              p.numel(), decay[i], _code(dt)))
+        self._upload()
 
 
 def grad_clip_workspace_bytes():
@@ -795,14 +804,18 @@ def alch_grad_clip(grads, max_norm, norm_out=None, workspace=None, stream=None):
     """grads: a GradList.  Returns the device float tensor [2] {norm over all gradients, factor they were multiplied with};
     norm_out[1:] is the grad_factor of alch_adamw_step."""
     L = lib()
-    _check_current(grads.device, stream)
+    dev = grads.index
+    handle = _place(dev, stream)
     if norm_out is None:
         norm_out = _empty((2,), torch.float32, grads.device, stream)
     else:
-        _check_dense(norm_out, "norm_out", torch.float32, grads.device, (2,))
-    ws = workspace if workspace is not None else _empty((L.alch_grad_clip_workspace_bytes(),), torch.uint8, grads.device, stream)
-    _check_dense(ws, "workspace", torch.uint8, grads.device)
-    _check(L.alch_grad_clip(grads.n, grads.dev_ptr, grads.host_ptr, max_norm, _ptr(norm_out), _ptr(ws), ws.numel(), _stream_handle(stream)))
+        _check_dense(norm_out, "norm_out", torch.float32, dev, (2,))
+    if workspace is None:
+        workspace = _empty((L.alch_grad_clip_workspace_bytes(),), torch.uint8, grads.device, stream)
+    else:
+        _check_dense(workspace, "workspace", torch.uint8, dev)
+    grads._used(stream)
+    _check(L.alch_grad_clip(grads.n, grads.dev_ptr, grads.host_ptr, max_norm, norm_out.data_ptr(), workspace.data_ptr(), workspace.numel(), handle))
     return norm_out
 
 
@@ -810,14 +823,15 @@ def alch_adamw_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, sched
     """One AdamW update of an AdamwList, in place.  schedule: device float tensor [2] {lr, step} that is read when the kernel
     runs, in place of lr and step (for captured steps).  grad_factor: device float tensor [1] that every gradient is multiplied
     with; where it is NaN or infinite nothing changes."""
-    L = lib()
-    _check_current(tensors.device, stream)
+    dev = tensors.index
+    handle = _place(dev, stream)
     if schedule is not None:
-        _check_dense(schedule, "schedule", torch.float32, tensors.device, (2,))
+        _check_dense(schedule, "schedule", torch.float32, dev, (2,))
     if grad_factor is not None:
-        _check_dense(grad_factor, "grad_factor", torch.float32, tensors.device, (1,))
+        _check_dense(grad_factor, "grad_factor", torch.float32, dev, (1,))
     p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
-    _check(L.alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), _stream_handle(stream)))
+    tensors._used(stream)
+    _check(lib().alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), handle))
 
 
 def alch_trace_enable(on):
