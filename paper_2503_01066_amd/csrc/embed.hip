@@ -483,22 +483,40 @@ __global__ __launch_bounds__(256) void k_embed_join(const int* __restrict__ keys
     }
 }
 
-// ---- backward of a few tokens: one launch --------------------------------------------------
-// A work-group a token and 64 * kVec columns: each of its wavefronts compares the token's id with a quarter of all others, and sums
-// the rows of those that have the same; nothing is done if one of them comes before the token.  The work-groups behind these zero
-// the rows that no token has, and find out from the ids which those are.
-static constexpr int kFewTokens = 2048;
-static bool few_tokens(int n, int tiles) { return n <= kFewTokens && (long long)n * n * tiles <= 1 << 23; }
+// ---- backward of few tokens: one launch ----------------------------------------------------
+// A work-group a token (or, kByRow, a row of a table that has fewer rows than there are tokens) and 64 * kVec columns.  Each of its
+// wavefronts compares the id with a part of all tokens' and sums the rows of those that have it.  By token nothing is done if one of
+// them comes before the token; its own row is on its way meanwhile, as is what it is added to.  The work-groups behind these zero the
+// rows that no token has, and find out from the ids which those are.
+static constexpr int kFewTokens = 2048, kFewTokensByRow = 8192;
+static constexpr int kTokenWaves = 4, kRowWaves = 8;
+static constexpr long long kFewPairs = 1 << 23, kFewUnits = 1 << 12;
+// Where comparing all ids with one another, once in every tile of columns, costs less than a sort and the launches behind it; ids as
+// texts have them, us by this kernel / with the sort:
+//   by token, table of 128,256 rows     1024 tokens    2048       3000
+//     hidden 256 (one tile), fp32         7.1 / 15.9   8.1 / 17.7   12.3 / 20.5
+//     1024 (two), bf16                    7.1 / 16.9  12.9 / 18.4   20.9 / 21.7
+//     4096 (eight)                       17.7 / 17.4  41.3 / 20.7
+//   by row, table of 1000 rows          1024           4096       8192
+//     hidden 256, fp32                    6.4 / 14.3   8.8 / 21.7   18.5 / 22.3
+//     1024                                8.4 / 15.4  15.3 / 22.9
+//     4096                               25.0 / 16.7
+// One id alone shared by 1024 tokens 20.5 / 14.9 by token, by 4096 50 / 27 by row: that is a chain of rows here.
+static bool few_tokens(int n, int tiles) { return n <= kFewTokens && (long long)n * n * tiles <= kFewPairs; }
+static bool few_rows(int n, int vocab, int tiles) {
+    return vocab < n && n <= kFewTokensByRow && (long long)vocab * tiles <= kFewUnits && (long long)n * vocab * tiles <= kFewPairs;
+}
 
-template <typename T, int kVec, bool kAccumulate>
-__global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, int n, int vocab, int hidden, const T* __restrict__ dX, float scale,
+template <typename T, int kVec, bool kAccumulate, bool kByRow>
+__global__ __launch_bounds__(kByRow ? 64 * kRowWaves : 64 * kTokenWaves) void k_embed_few(const int* __restrict__ ids, int n, int vocab, int hidden, const T* __restrict__ dX, float scale,
                                                    T* __restrict__ dW, int tiles, int units, RowGrid g) {
     typedef typename Piece<T, kVec>::type vec;
-    constexpr int kBatch = 16;
-    __shared__ unsigned short list[kFewTokens + 256];  // tokens of the row, ascending in every quarter
-    __shared__ float red[3][64 * kVec];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if constexpr (!kAccumulate) {
+    constexpr int kBatch = 16, kWaves = kByRow ? kRowWaves : kTokenWaves;
+    __shared__ unsigned short list[(kByRow ? kFewTokensByRow : kFewTokens) + 64 * kWaves];  // the tokens that have the id, ascending in every part
+    __shared__ float red[kWaves - 1][64 * kVec];
+    __shared__ int found[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if constexpr (!kAccumulate && !kByRow) {
         if ((int)blockIdx.x >= units) {
             __shared__ unsigned present[256 / 32];  // of the work-group's rows
             for (int b = blockIdx.x - units; b < g.blocks; b += gridDim.x - units) {
@@ -508,7 +526,7 @@ __global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, 
                 __syncthreads();  // (what the round before had here has been read)
                 if (tid < 256 / 32) present[tid] = 0;
                 __syncthreads();
-                for (int t = tid; t < n; t += 256) {
+                for (int t = tid; t < n; t += 64 * kWaves) {
                     const long long r = ids[t] - row0;
                     if (r >= 0 && r < rows) atomicOr(&present[r >> 5], 1u << (r & 31));
                 }
@@ -518,30 +536,41 @@ __global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, 
             return;
         }
     }
-    const int token = blockIdx.x / tiles, own = (blockIdx.x % tiles * 64 + lane) * kVec, id = ids[token];
-    if ((unsigned)id >= (unsigned)vocab) return;
+    const int unit = blockIdx.x / tiles, own = ((int)blockIdx.x % tiles * 64 + lane) * kVec, token = kByRow ? -1 : unit, id = kByRow ? unit : ids[unit];
+    if (!kByRow && (unsigned)id >= (unsigned)vocab) return;
     const bool in = own < hidden;
     const int c = min(own, hidden - kVec);  // (as in k_embed_sums)
-    const int quarter = (n + 255) / 256 * 64, begin = wave * quarter, end = min(n, begin + quarter);
+    T* dst = dW + (long long)id * hidden + c;
+    vec old = {}, row0 = {};
+    if (in && wave == 0) {
+        if (kAccumulate) old = *reinterpret_cast<const vec*>(dst);
+        if (!kByRow) row0 = *reinterpret_cast<const vec*>(dX + (long long)token * hidden + c);
+    }
+    const int part = (n + 64 * kWaves - 1) / (64 * kWaves) * 64, begin = wave * part, end = min(n, begin + part);
     unsigned short* mine = list + begin;
     int count = 0;
-    bool earlier = false;
+    unsigned long long earlier = 0;
 #pragma unroll 4
     for (int t0 = begin; t0 < end; t0 += 64) {
         const int t = t0 + lane;
-        const bool same = t < end && ids[t] == id;
+        const bool same = t < end && ids[t] == id && t != token;
         const unsigned long long set = __ballot(same);
-        earlier |= same && t < token;
+        if (!kByRow) earlier |= __ballot(same && t < token);
         if (same) mine[count + __popcll(set & ((1ull << lane) - 1))] = (unsigned short)t;
         count += __popcll(set);
     }
-    if (__syncthreads_or(earlier)) return;
-    vec old = {};
-    T* dst = dW + (long long)id * hidden + c;
-    if (kAccumulate && in && wave == 0) old = *reinterpret_cast<const vec*>(dst);
+    if (lane == 0) found[wave] = earlier ? -1 : count;
+    __syncthreads();
+    int others = 0;  // tokens of the other wavefronts
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (!kByRow && found[w] < 0) return;
+        if (w > 0) others += found[w];
+    }
+    if (kAccumulate && kByRow && found[0] + others == 0) return;
     float s[kVec];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) s[e] = 0.f;
+    for (int e = 0; e < kVec; ++e) s[e] = (float)row0[e];
     for (int i = 0; i < count; i += kBatch) {
         vec row[kBatch];
 #pragma unroll
@@ -553,15 +582,19 @@ __global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, 
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) s[e] += (float)row[j][e];
     }
-    if (wave > 0)
+    if (others) {
+        if (wave > 0)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) red[wave - 1][64 * e + lane] = s[e];
-    __syncthreads();
+            for (int e = 0; e < kVec; ++e) red[wave - 1][64 * e + lane] = s[e];
+        __syncthreads();
+    }
     if (wave > 0 || !in) return;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-        const float sum = s[e] + ((red[0][64 * e + lane] + red[1][64 * e + lane]) + red[2][64 * e + lane]);
-        old[e] = (T)(kAccumulate ? (float)old[e] + scale * sum : scale * sum);
+        if (others)
+#pragma unroll
+            for (int w = 0; w < kWaves - 1; ++w) s[e] += red[w][64 * e + lane];
+        old[e] = (T)(kAccumulate ? (float)old[e] + scale * s[e] : scale * s[e]);
     }
     store_own<T, kVec>(dst, old, own - c);
 }
@@ -609,12 +642,12 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
         return;
     }
     const int tiles = ceil_div(hidden, 64 * kVec);
-    if (few_tokens(n, tiles)) {
-        const int units = n * tiles;
-        if (accumulate)
-            k_embed_few<T, kVec, true><<<units, 256, 0, stream>>>(ids, n, vocab, hidden, dX, scale, dW, tiles, units, table);
-        else
-            k_embed_few<T, kVec, false><<<units + std::min(table.blocks, kMaxBlocks), 256, 0, stream>>>(ids, n, vocab, hidden, dX, scale, dW, tiles, units, table);
+    const bool by_row = few_rows(n, vocab, tiles);
+    if (by_row || few_tokens(n, tiles)) {
+        const int units = (by_row ? vocab : n) * tiles, grid = units + (by_row ? 0 : std::min(table.blocks, kMaxBlocks));
+        const auto launch = [&](auto kernel) { kernel<<<grid, 64 * (by_row ? kRowWaves : kTokenWaves), 0, stream>>>(ids, n, vocab, hidden, dX, scale, dW, tiles, units, table); };
+        if (by_row) accumulate ? launch(k_embed_few<T, kVec, true, true>) : launch(k_embed_few<T, kVec, false, true>);
+        else accumulate ? launch(k_embed_few<T, kVec, true, false>) : launch(k_embed_few<T, kVec, false, false>);
         return;
     }
     const int *keys = ids, *tokens = nullptr;

@@ -81,7 +81,8 @@ CASES = [(1, 4096, 1000, "mixed"), (31, 256, 64, "mixed"), (32, 256, 64, "one"),
          (16384, 64, 128256, "runs"), (9000, 520, 7, "mixed"), (70001, 24, 40000, "one"), (200, 64, 9, "padding"), (300, 1, 17, "mixed"),
          (2049, 8200, 300, "runs"), (300, 8, 20, "runs"), (1024, 520, 40, "runs"), (777, 33, 2, "runs"), (16500, 2104, 500, "runs"),
          (16384, 1032, 90, "mixed"), (1025, 8, 20, "runs"), (1100, 264, 1, "one"), (1200, 64, 9, "padding"), (2000, 9, 31, "runs"), (90, 9, 31, "runs"),
-         (3000, 515, 700, "mixed"), (4097, 16, 4097, "ascending")]
+         (3000, 515, 700, "mixed"), (8192, 100, 40, "runs"), (5000, 260, 999, "mixed"), (2500, 16, 2499, "ascending"), (3000, 70, 9, "padding"),
+         (3500, 1032, 20000, "runs"), (2100, 40, 100000, "mixed"), (4096, 72, 128256, "one"), (4097, 16, 4097, "ascending")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
