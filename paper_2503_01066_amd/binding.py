@@ -642,16 +642,13 @@ def _code(dtype):
     raise TypeError("dtype %s: bfloat16 or float32" % dtype)
 
 
-def _dense(t, dtype, device, shape=None):
-    return t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape)
-
-
 def _check_dense(t, name, dtype, device, shape=None):
     """A library call takes the address of a tensor alone: what else it assumes of it is checked here.  device: its index."""
-    if not _dense(t, dtype, device, shape):
-        raise ValueError("%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s%s" % (
-            name, dtype, "" if shape is None else " of shape %s" % (tuple(shape),), "the CPU" if device < 0 else "cuda:%d" % device, t.dtype,
-            tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (shape is None or t.shape == shape):
+        return
+    raise ValueError("%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s%s" % (
+        name if isinstance(name, str) else "%s[%d]" % name, dtype, "" if shape is None else " of shape %s" % (tuple(shape),),
+        "the CPU" if device < 0 else "cuda:%d" % device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
 
 
 def _place(device, stream):
@@ -726,8 +723,7 @@ class _TensorTable:
 
     def _take(self, t, name, i, dtype, shape=None, written=False, listed=True):
         """The address of a tensor, checked; it is among those that may not overlap, if listed."""
-        if not _dense(t, dtype, self.index, shape):
-            _check_dense(t, "%s[%d]" % (name, i), dtype, self.index, shape)
+        _check_dense(t, (name, i), dtype, self.index, shape)
         at = t.data_ptr()
         if listed:
             self.ranges.append((at, at + t.numel() * t.element_size(), written, name, i))

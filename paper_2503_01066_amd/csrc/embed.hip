@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256) void k_embed_zero(ZeroRows z, const int* __res
     zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x, gridDim.x);
 }
 
-// Up to kRankTokens tokens are sorted by one launch: a token's place is the number of tokens with a lower id, and of those with the
+// Up to kRankTokens tokens for every digit that their sort would have are sorted by one launch: a token's place is the number of tokens with a lower id, and of those with the
 // same one before it.  A work-group finds the places of 64 tokens, a token a lane; its wavefronts go over a sixteenth of all tokens
 // each, 64 of them with one load, and compare them with their own one after the other.
 static constexpr int kRankTokens = 4096;
@@ -618,9 +618,9 @@ static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_by
     p.counts_a_pass = (size_t)p.sort.blocks << p.sort.digit;
     p.counts = static_cast<int*>(a.take(p.counts_a_pass * p.sort.passes * sizeof(int)));
     p.where = static_cast<int*>(a.take((size_t)vocab * sizeof(int)));
-    // parts as long as leaves 2048 wavefronts (of 16-byte lanes): 
+    // parts as long as leaves 4096 wavefronts (of 512 columns)
     p.part_len = kPart;
-    while (p.part_len > 8 && (long long)ceil_div(n, p.part_len) * ceil_div(hidden, 512) < 2048) p.part_len /= 2;
+    while (p.part_len > 8 && (long long)ceil_div(n, p.part_len) * ceil_div(hidden, 512) < 4096) p.part_len /= 2;
     p.parts = ceil_div(n, p.part_len);
     p.cut = static_cast<int*>(a.take((size_t)p.parts * sizeof(int)));
     p.stride = (int)round_up((size_t)hidden, 8);
@@ -651,7 +651,7 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
         return;
     }
     const int *keys = ids, *tokens = nullptr;
-    if (n <= kRankTokens) {
+    if (n <= kRankTokens * p.sort.passes) {
         k_sort_rank<<<ceil_div(n, 64), 1024, 0, stream>>>(ids, n, vocab, p.keys[0], p.tokens[0], accumulate ? nullptr : p.where);
         keys = p.keys[0];
         tokens = p.tokens[0];

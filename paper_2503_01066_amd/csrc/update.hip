@@ -96,9 +96,22 @@ __device__ __forceinline__ ClipChunk clip_chunk(const alch_grad_tensor* __restri
     const long long begin = (long long)(c - first[t]) * chunk, at = begin * (a.dtype == ALCH_BF16 ? 2 : 4);
     return {static_cast<const char*>(a.grad) + at, a.out ? static_cast<char*>(a.out) + at : nullptr, (int)min((long long)chunk, (long long)a.n - begin), a.dtype};
 }
-__device__ __forceinline__ void clip_load(const ClipChunk& c, f32x4_u (&v)[kBatch]) {
+// The pieces of a thread.  Of a tensor's last chunk those that lie in it as a whole, the others are zero; behind them at most one
+// element a thread, *rest (its index, or -1), *r.  Returns whether the chunk is whole.
+__device__ __forceinline__ bool clip_load(const ClipChunk& c, f32x4_u (&v)[kBatch], int* rest, float* r) {
+    const f32x4_u* p = reinterpret_cast<const f32x4_u*>(c.grad) + threadIdx.x;
+    if (c.elements == clip_elements(c.dtype)) {
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) v[b] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(c.grad) + threadIdx.x + 256 * b);
+        for (int b = 0; b < kBatch; ++b) v[b] = __builtin_nontemporal_load(p + 256 * b);
+        return true;
+    }
+    const int n = c.dtype == ALCH_BF16 ? 8 : 4, pieces = c.elements / n;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) v[b] = (int)threadIdx.x + 256 * b < pieces ? __builtin_nontemporal_load(p + 256 * b) : f32x4_u{0.f, 0.f, 0.f, 0.f};
+    *rest = pieces * n + (int)threadIdx.x;
+    if (*rest >= c.elements) *rest = -1;
+    else *r = c.dtype == ALCH_BF16 ? (float)reinterpret_cast<const __bf16*>(c.grad)[*rest] : reinterpret_cast<const float*>(c.grad)[*rest];
+    return false;
 }
 
 // The squares are added in 64 bits: no gradient of finite numbers overflows there, none vanishes, and the order of the
@@ -114,28 +127,25 @@ __global__ __launch_bounds__(256) void k_norm(const alch_grad_tensor* __restrict
     if ((int)blockIdx.x < chunks) next = clip_chunk(tensors, first, n, blockIdx.x);
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         const ClipChunk a = next;
-        const bool full = a.elements == clip_elements(a.dtype);
         f32x4_u v[kBatch];
-        if (full) clip_load(a, v);
+        int rest = -1;
+        float r = 0.f;
+        clip_load(a, v, &rest, &r);
         if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
-        if (full && a.dtype == ALCH_BF16) {
+        if (a.dtype == ALCH_BF16) {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const bf16x8_u x = __builtin_bit_cast(bf16x8_u, v[b]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s += (double)(float)x[e] * (double)(float)x[e];
             }
-        } else if (full) {
+        } else {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s += (double)v[b][e] * (double)v[b][e];
-        } else {
-            for (int i = threadIdx.x; i < a.elements; i += 256) {
-                const double x = a.dtype == ALCH_BF16 ? (float)reinterpret_cast<const __bf16*>(a.grad)[i] : reinterpret_cast<const float*>(a.grad)[i];
-                s += x * x;
-            }
         }
+        if (rest >= 0) s += (double)r * (double)r;
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -174,14 +184,15 @@ __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict
     ClipChunk a = clip_chunk(tensors, first, n, blockIdx.x);  // (no more work-groups than chunks)
     float factor = 0.f;
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        bool used = a.out, full = used && a.elements == clip_elements(a.dtype);
         f32x4_u v[kBatch];
-        if (full) clip_load(a, v);
+        int rest = -1;
+        float r = 0.f;
+        const bool full = a.out && clip_load(a, v, &rest, &r);
         ClipChunk next = {};
         if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
         if (c == (int)blockIdx.x) factor = clip_factor(sums, max_norm, norm_out);
-        if (a.out == a.grad && factor == 1.f) used = full = false;
-        if (full) {
+        if (a.out && !(a.out == a.grad && factor == 1.f)) {
+            const int pieces = full ? 256 * kBatch : a.elements / (a.dtype == ALCH_BF16 ? 8 : 4);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 if (a.dtype == ALCH_BF16) {
@@ -192,14 +203,11 @@ __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict
                 } else {
                     v[b] *= factor;
                 }
-                __builtin_nontemporal_store(v[b], reinterpret_cast<f32x4_u*>(a.out) + threadIdx.x + 256 * b);
+                if (full || (int)threadIdx.x + 256 * b < pieces) __builtin_nontemporal_store(v[b], reinterpret_cast<f32x4_u*>(a.out) + threadIdx.x + 256 * b);
             }
-        } else if (used) {
-            for (int i = threadIdx.x; i < a.elements; i += 256) {
-                if (a.dtype == ALCH_BF16)
-                    reinterpret_cast<__bf16*>(a.out)[i] = (__bf16)((float)reinterpret_cast<const __bf16*>(a.grad)[i] * factor);
-                else
-                    reinterpret_cast<float*>(a.out)[i] = reinterpret_cast<const float*>(a.grad)[i] * factor;
+            if (rest >= 0) {
+                if (a.dtype == ALCH_BF16) reinterpret_cast<__bf16*>(a.out)[rest] = (__bf16)(r * factor);
+                else reinterpret_cast<float*>(a.out)[rest] = r * factor;
             }
         }
         a = next;
@@ -291,40 +299,48 @@ __device__ __forceinline__ void adamw(const AdamwChunk& k, const AdamwArgs& a, c
     T* param = static_cast<T*>(k.t.param) + k.at;
     const T* grad = static_cast<const T*>(k.t.grad) + k.at;
     float *m = k.t.m + k.at, *v = k.t.v + k.at, *master = kMaster ? k.t.master + k.at : nullptr;
-    if (k.elements == kAdamwChunk) {
-        f32x4_u gv[kAdamwBatch], mv[kAdamwBatch], vv[kAdamwBatch], wv[kAdamwBatch];
+    f32x4_u gv[kAdamwBatch], mv[kAdamwBatch], vv[kAdamwBatch], wv[kAdamwBatch];
+    const int whole = k.elements / 4 - (int)threadIdx.x;  // (of the pieces of four elements, those from this thread's first one on)
+    const bool full = k.elements == kAdamwChunk;
+    const auto load = [&](int b) {
+        const int i = (threadIdx.x + 256 * b) * 4;
+        gv[b] = load4(grad + i);
+        mv[b] = load4(m + i);
+        vv[b] = load4(v + i);
+        if constexpr (kMaster) wv[b] = load4(master + i);
+        else wv[b] = load4(param + i);
+    };
+    if (full) {
 #pragma unroll
-        for (int b = 0; b < kAdamwBatch; ++b) {
-            const int i = (threadIdx.x + 256 * b) * 4;
-            gv[b] = load4(grad + i);
-            mv[b] = load4(m + i);
-            vv[b] = load4(v + i);
-            if constexpr (kMaster) wv[b] = load4(master + i);
-            else wv[b] = load4(param + i);
-        }
-#pragma unroll
-        for (int b = 0; b < kAdamwBatch; ++b) {
-            const int i = (threadIdx.x + 256 * b) * 4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float me = mv[b][e], ve = vv[b][e], we = wv[b][e];
-                adamw_element(a, r, k.t.weight_decay, gv[b][e], me, ve, we);
-                mv[b][e] = me; vv[b][e] = ve; wv[b][e] = we;
-            }
-            store4(m + i, mv[b]);
-            store4(v + i, vv[b]);
-            if constexpr (kMaster) store4(master + i, wv[b]);
-            store4(param + i, wv[b]);
-        }
+        for (int b = 0; b < kAdamwBatch; ++b) load(b);
     } else {
-        for (int i = threadIdx.x; i < k.elements; i += 256) {
-            float me = m[i], ve = v[i], we = kMaster ? master[i] : (float)param[i];
-            adamw_element(a, r, k.t.weight_decay, (float)grad[i], me, ve, we);
-            m[i] = me;
-            v[i] = ve;
-            if constexpr (kMaster) master[i] = we;
-            param[i] = (T)we;
+#pragma unroll
+        for (int b = 0; b < kAdamwBatch; ++b)
+            if (256 * b < whole) load(b);
+    }
+#pragma unroll
+    for (int b = 0; b < kAdamwBatch; ++b) {
+        if (!full && 256 * b >= whole) continue;
+        const int i = (threadIdx.x + 256 * b) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float me = mv[b][e], ve = vv[b][e], we = wv[b][e];
+            adamw_element(a, r, k.t.weight_decay, gv[b][e], me, ve, we);
+            mv[b][e] = me; vv[b][e] = ve; wv[b][e] = we;
         }
+        store4(m + i, mv[b]);
+        store4(v + i, vv[b]);
+        if constexpr (kMaster) store4(master + i, wv[b]);
+        store4(param + i, wv[b]);
+    }
+    const int i = (k.elements & ~3) + (int)threadIdx.x;  // behind the last whole piece
+    if (i < k.elements) {
+        float me = m[i], ve = v[i], we = kMaster ? master[i] : (float)param[i];
+        adamw_element(a, r, k.t.weight_decay, (float)grad[i], me, ve, we);
+        m[i] = me;
+        v[i] = ve;
+        if constexpr (kMaster) master[i] = we;
+        param[i] = (T)we;
     }
 }
 
