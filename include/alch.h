@@ -458,7 +458,8 @@ int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t 
  *   dW_embed   [vocab, hidden] out.  accumulate == 0: every row is written, zeros where no token has the id.
  *              accumulate != 0: only rows of ids that occur are read and written (sum in fp32, one rounding), for
  *              micro-batches and for a table shared with the head, whose dW_lm it may be.
- *   workspace  alch_embed_backward_workspace_bytes() bytes, 16-byte aligned
+ *   workspace  alch_embed_backward_workspace_bytes() bytes, 16-byte aligned; what it holds is not read.  As everywhere, two calls
+ *              that may run at the same time need one each.
  * Sums are in fp32, in an order that the token ids alone determine: results repeat bit for bit.
  */
 int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids,
@@ -510,7 +511,7 @@ typedef struct {
     double lr, beta1, beta2, eps;
     int32_t step;             /* of this update, the first one is 1 */
     const float* schedule;    /* device float [2] or NULL: { lr, step } in place of the two above, read when the kernel runs, so that
-                                 a captured step can be replayed with other values */
+                                 a captured step can be replayed with other values; a step below 1 is none: nothing is written */
     const float* grad_factor; /* device float [1] or NULL: multiplies every gradient (norm_out + 1 of alch_grad_clip) */
 } alch_adamw;
 

@@ -1422,6 +1422,12 @@ static int check_embed(alch_dtype dtype, int vocab, int hidden, int n_tokens) {
     return ALCH_OK;
 }
 
+// Whether two buffers share memory.
+static bool overlap(const void* a, unsigned long long a_bytes, const void* b, unsigned long long b_bytes) {
+    const unsigned long long x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
 #define REQUIRE_WORDS(p, name)                                                                                                \
     do {                                                                                                                      \
         if (!(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is NULL", name);                                                      \
@@ -1435,6 +1441,8 @@ int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t 
     if (n_tokens == 0) return ALCH_OK;
     REQUIRE_WORDS(token_ids, "token_ids");
     REQUIRE_PTR(W_embed, "W_embed"); REQUIRE_PTR(X, "X");
+    const unsigned long long row = (unsigned long long)hidden * dtype_size(dtype);
+    if (overlap(X, n_tokens * row, W_embed, vocab * row)) return fail(ALCH_ERR_INVALID_ARG, "X overlaps W_embed");
     return launch_embed(dtype, token_ids, W_embed, X, n_tokens, vocab, hidden, scale, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -1453,6 +1461,8 @@ int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t
         REQUIRE_PTR(dX, "dX");
     }
     REQUIRE_PTR(dW_embed, "dW_embed");
+    const unsigned long long row = (unsigned long long)hidden * dtype_size(dtype);
+    if (n_tokens > 0 && overlap(dW_embed, vocab * row, dX, n_tokens * row)) return fail(ALCH_ERR_INVALID_ARG, "dW_embed overlaps dX");
     const size_t need = embed_backward_workspace_bytes(vocab, hidden, n_tokens);
     if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
     if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
@@ -1472,9 +1482,8 @@ int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alc
         ALCH_TRY(check_tensor_ptr(t.grad, i, "grad"));
         if (!t.out || t.out == t.grad) continue;
         ALCH_TRY(check_tensor_ptr(t.out, i, "out"));
-        const uintptr_t g = reinterpret_cast<uintptr_t>(t.grad), o = reinterpret_cast<uintptr_t>(t.out);
-        const uintptr_t bytes = (uintptr_t)t.n * dtype_size((alch_dtype)t.dtype);
-        if (g < o ? o - g < bytes : g - o < bytes) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: out overlaps grad", i);
+        const unsigned long long bytes = (unsigned long long)t.n * dtype_size((alch_dtype)t.dtype);
+        if (overlap(t.grad, bytes, t.out, bytes)) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: out overlaps grad", i);
     }
     if (!(max_norm >= 0.f)) return fail(ALCH_ERR_INVALID_ARG, "max_norm %g", (double)max_norm);
     REQUIRE_WORDS(norm_out, "norm_out");

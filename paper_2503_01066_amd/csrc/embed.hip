@@ -567,7 +567,8 @@ __global__ __launch_bounds__(kByRow ? 64 * kRowWaves : 64 * kTokenWaves) void k_
         if (!kByRow && found[w] < 0) return;
         if (w > 0) others += found[w];
     }
-    if (kAccumulate && kByRow && found[0] + others == 0) return;
+    const bool absent = kByRow && found[0] + others == 0;
+    if (kAccumulate && absent) return;
     float s[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) s[e] = (float)row0[e];
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(kByRow ? 64 * kRowWaves : 64 * kTokenWaves) void k_
         if (others)
 #pragma unroll
             for (int w = 0; w < kWaves - 1; ++w) s[e] += red[w][64 * e + lane];
-        old[e] = (T)(kAccumulate ? (float)old[e] + scale * s[e] : scale * s[e]);
+        old[e] = (T)(kAccumulate ? (float)old[e] + scale * s[e] : absent ? 0.f : scale * s[e]);
     }
     store_own<T, kVec>(dst, old, own - c);
 }

@@ -250,14 +250,14 @@ static constexpr int kAdamwBlocks = 1 << 22;  // one work-group a chunk: 1061 us
 struct AdamwArgs {
     const alch_adamw_tensor* tensors;
     int n;
-    float lr, c1, c2;        // c = 1 / (1 - b^step)
+    float lr, c1, c2;        // 1 / (1 - b1^step), sqrt(1 / (1 - b2^step))
     float b1, b2, d1, d2, eps;  // d = 1 - b
     double beta1, beta2;     // for a step that is known on the device only
     const float *schedule, *grad_factor;
 };
 
 // 1 / (1 - b^t), in 64 bits: for b = 0.999 and t = 1 three of seven digits are lost in 32.
-__host__ __device__ inline float correction(double beta, double step) { return (float)(1.0 / (1.0 - pow(beta, step))); }
+__host__ __device__ inline double correction(double beta, double step) { return 1.0 / (1.0 - pow(beta, step)); }
 
 // Four elements a lane, so that the 64 lanes of a load of fp32 read 1 KB without a gap (eight a lane, as two loads of every other
 // 16 bytes, cost 10 % with non-temporal loads).
@@ -291,7 +291,7 @@ __device__ __forceinline__ void adamw_element(const AdamwArgs& a, const AdamwRat
     const float x = g * r.factor;
     m = a.b1 * m + a.d1 * x;
     v = a.b2 * v + a.d2 * x * x;
-    w -= r.lr * (m * r.c1 / (sqrtf(v * r.c2) + a.eps) + decay * w);
+    w -= r.lr * (m * r.c1 / (sqrtf(v) * r.c2 + a.eps) + decay * w);
 }
 
 template <typename T, bool kMaster>
@@ -348,12 +348,13 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
     __shared__ int first[kMaxTensors + 1];
     __shared__ float shared_c[3];
     const float factor = a.grad_factor ? *a.grad_factor : 1.f;
-    if (!(fabsf(factor) < INFINITY)) return;  // (the gradients are of no use: nothing changes)
+    if (!(fabsf(factor) < INFINITY)) return;            // (the gradients are of no use: nothing changes)
+    if (a.schedule && !(a.schedule[1] >= 1.f)) return;  // (nor is this a step)
     if (a.schedule && threadIdx.x == 0) {
         const double step = a.schedule[1];
         shared_c[0] = a.schedule[0];
-        shared_c[1] = correction(a.beta1, step);
-        shared_c[2] = correction(a.beta2, step);
+        shared_c[1] = (float)correction(a.beta1, step);
+        shared_c[2] = (float)sqrt(correction(a.beta2, step));
     }
     chunk_table(a.tensors, a.n, [](int) { return kAdamwChunk; }, first);
     const int chunks = first[a.n];
@@ -380,7 +381,8 @@ int launch_adamw(int n_tensors, const alch_adamw_tensor* tensors, const alch_ada
     }
     if (chunks == 0) return ALCH_OK;
     TraceScope ts(kTraceUpdate, 0.0, bytes, stream);
-    const AdamwArgs a{tensors, n_tensors, (float)p.lr, p.schedule ? 0.f : correction(p.beta1, p.step), p.schedule ? 0.f : correction(p.beta2, p.step),
+    const AdamwArgs a{tensors, n_tensors, (float)p.lr, p.schedule ? 0.f : (float)correction(p.beta1, p.step),
+                      p.schedule ? 0.f : (float)sqrt(correction(p.beta2, p.step)),
                       (float)p.beta1, (float)p.beta2, (float)(1.0 - p.beta1), (float)(1.0 - p.beta2), (float)p.eps, p.beta1, p.beta2,
                       p.schedule, p.grad_factor};
     k_adamw<<<(int)std::min<long long>(chunks, kAdamwBlocks), 256, 0, stream>>>(a);

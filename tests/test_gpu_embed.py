@@ -121,6 +121,21 @@ def test_backward_without_tokens_writes_zeros():
     assert bool((dW == 5).all())
 
 
+@pytest.mark.parametrize("scale", [-2.0, float("inf"), float("nan")])
+@pytest.mark.parametrize("T,V", [(40, 1000), (300, 50), (6000, 20000), (9000, 3000), (0, 9)])
+def test_rows_without_a_token_are_zero_whatever_the_scale(T, V, scale):
+    import paper_2503_01066_amd as A
+    ids = (make_ids("mixed", T, V // 2, T) * 2) if T else np.empty(0, np.int32)  # (odd rows have no token)
+    dev = torch.from_numpy(ids.astype(np.int32)).cuda()
+    X = A.alch_embed_forward(dev, torch.ones(V, 72, device="cuda"), scale=scale)
+    bad = torch.from_numpy((ids < 0) | (ids >= V)).cuda()
+    assert X.shape == (T, 72) and bool((X[bad].view(torch.int32) == 0).all())
+    dW = A.alch_embed_backward(dev, torch.ones(T, 72, device="cuda"), V, scale=scale, dW_embed=torch.full((V, 72), 5.0, device="cuda"))
+    met = torch.zeros(V, dtype=torch.bool, device="cuda")
+    met[dev[~bad].long()] = True
+    assert bool((dW[~met].view(torch.int32) == 0).all()) and not bool((dW[met] == 0).any())
+
+
 def test_infinities_and_nan_reach_their_own_row_alone():
     import paper_2503_01066_amd as A
     ids = np.array([3, 1, 3, 2, 1] * 20, np.int32)

@@ -166,6 +166,29 @@ def test_adamw_schedule_on_the_device_is_the_same_update():
         assert bool(((a - b).abs().double() <= 2 * (half(a) + 4 * U) * b.abs().double()).all())
 
 
+@pytest.mark.parametrize("step", [0.0, -1.0, math.nan])
+def test_adamw_schedule_that_is_no_step_changes_nothing(step):
+    import paper_2503_01066_amd as A
+    p, g, m, v = (tensors([5000, 3], ["f32"], k) for k in range(4))
+    old = [x.clone() for x in p + m + v]
+    A.alch_adamw_step(A.AdamwList(p, g, m, v), 1.0, schedule=torch.tensor([1.0, step], device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(p + m + v, old))
+
+
+def test_lists_dropped_behind_calls_on_another_stream():
+    import paper_2503_01066_amd as A
+    s = torch.cuda.Stream()
+    g = tensors([300000, 77], ["bf16"], 1)
+    want = A.alch_grad_clip(A.GradList(g), 1.0)
+    torch.cuda.synchronize()
+    norms = []
+    for _ in range(20):
+        norms.append(A.alch_grad_clip(A.GradList(g), 1.0, stream=s))
+        torch.full((4096,), 0x7f, dtype=torch.uint8, device="cuda")  # (memory that was just freed is written again)
+    torch.cuda.synchronize()
+    assert all(torch.equal(n, want) for n in norms)
+
+
 def test_captured_step_follows_its_schedule_and_gradients():
     import paper_2503_01066_amd as A
     sizes = [3000, 9, 70000]

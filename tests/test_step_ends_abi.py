@@ -18,7 +18,7 @@ def _err():
 
 
 def test_embed_forward_refusals():
-    call = lambda dt=1, V=100, H=64, n=5, ids=P, W=P, X=P: A.lib().alch_embed_forward(dt, V, H, n, ids, W, 1.0, X, None)
+    call = lambda dt=1, V=100, H=64, n=5, ids=P, W=P, X=2 * P: A.lib().alch_embed_forward(dt, V, H, n, ids, W, 1.0, X, None)
     assert call(dt=2) == INVALID and "dtype" in _err()
     assert call(V=0) == SHAPE and call(H=0) == SHAPE and call(H=-8) == SHAPE
     assert call(n=-1) == INVALID and call(n=(1 << 30) + 1) == UNSUPPORTED and call(H=(1 << 20) + 1) == UNSUPPORTED
@@ -27,17 +27,20 @@ def test_embed_forward_refusals():
     assert call(ids=P + 2) == INVALID and "4-byte" in _err()
     assert call(W=None) == INVALID and call(W=P + 8) == INVALID and "W_embed" in _err()
     assert call(X=None) == INVALID and call(X=P + 2) == INVALID
+    assert call(X=P) == INVALID and "overlaps" in _err()
+    assert call(X=P + 99 * 128) == INVALID and call(X=P - 4 * 128) == INVALID
     assert call(n=0, ids=None, W=None, X=None) == 0  # nothing to do, nothing is launched
 
 
 def test_embed_backward_refusals():
     L = A.lib()
     need = L.alch_embed_backward_workspace_bytes(1, 100, 64, 5)
-    call = lambda dt=1, V=100, H=64, n=5, ids=P, dX=P, dW=P, acc=0, ws=P, wsb=need: L.alch_embed_backward(
+    call = lambda dt=1, V=100, H=64, n=5, ids=P, dX=2 * P, dW=P, acc=0, ws=P, wsb=need: L.alch_embed_backward(
         dt, V, H, n, ids, dX, 1.0, dW, acc, ws, wsb, None)
     assert call(dt=-1) == INVALID and call(V=-1) == SHAPE and call(n=-1) == INVALID and call(n=(1 << 30) + 1) == UNSUPPORTED
     assert call(ids=None) == INVALID and call(ids=P + 1) == INVALID and call(dX=None) == INVALID and call(dX=P + 4) == INVALID
     assert call(dW=None) == INVALID and call(dW=P + 8) == INVALID and "dW_embed" in _err()
+    assert call(dX=P + 99 * 128) == INVALID and "overlaps" in _err() and call(dX=P - 4 * 128) == INVALID
     assert call(wsb=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE and call(ws=P + 8) == INVALID
     assert call(n=0, acc=1, ids=None, dX=None, dW=None, ws=None) == 0
     q = L.alch_embed_backward_workspace_bytes
