@@ -48,6 +48,8 @@ def parse():
                     help="pack / keep only X, Q, K, V; the backward recomputes O, LSE, X2, G and U")
     ap.add_argument("--scan-once", action="store_true",
                     help="config3: scan the mask for the first layer only, alch_capture_gather for the other 31")
+    ap.add_argument("--update", action="store_true",
+                    help="config4: the step also holds the embedding gradient, clipping by the global norm and the AdamW update")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-baseline-full", action="store_true",
                     help="time the oracle on the whole workload (config 3: all 32 layers; config 5: 2 x 4096 tokens) "
@@ -334,6 +336,42 @@ def run_layer(args, torch, A):
     return out
 
 
+def with_update(args, torch, A, backward, Ws, loras, lora_grads, base_grads, emb, ids, W_lm, g_final):
+    """`backward` followed by what a training step does with its gradients.  The learning rate is 0: the update is the same
+    work, and the records stay those of the weights."""
+    params, grads = [], []
+    for l, W in enumerate(Ws):
+        for k, w in W.items():
+            if base_grads[l].get("d" + k) is not None:
+                params.append(w)
+                grads.append(base_grads[l]["d" + k])
+        if loras is not None:
+            for p, ab in loras[l].items():
+                params += ab
+                grads += [lora_grads[l]["dA" + p], lora_grads[l]["dB" + p]]
+    head, d_emb = None, None
+    if not args.frozen_base:
+        head, d_emb = (torch.empty_like(g_final), torch.empty_like(W_lm)), torch.empty_like(emb)
+        params += [g_final, W_lm, emb]
+        grads += [head[0], head[1], d_emb]
+        ws_emb = torch.empty(A.embed_backward_workspace_bytes(emb.dtype, emb.shape[0], emb.shape[1], ids.numel()), dtype=torch.uint8, device=emb.device)
+    if not params:
+        raise SystemExit("--update: nothing is trained (--frozen-base needs --lora-rank)")
+    masters = [p.float() for p in params]
+    zeros = lambda: [torch.zeros_like(w) for w in masters]
+    clip, tensors = A.GradList(grads, grads), A.AdamwList(params, grads, zeros(), zeros(), masters=masters, weight_decay=0.1)
+    norm, ws = torch.empty(2, device=emb.device), torch.empty(A.grad_clip_workspace_bytes(), dtype=torch.uint8, device=emb.device)
+
+    def step(xf, rs, hooks=None):
+        out = backward(xf, rs, hooks, head)
+        if d_emb is not None:
+            A.alch_embed_backward(ids, out["dX_embed"], emb.shape[0], dW_embed=d_emb, workspace=ws_emb)
+        A.alch_grad_clip(clip, 1.0, norm_out=norm, workspace=ws)
+        A.alch_adamw_step(tensors, 0.0, grad_factor=norm[1:])
+        return out
+    return step
+
+
 def run_config4(args, torch, A):
     """32-layer 8B-shaped stack, 8 x 4096 tokens, vocab 128256: loss + backward from reused records
     (Section 1 of the paper) against forward recompute + the same backward (its separate-cluster baseline)."""
@@ -352,8 +390,10 @@ def run_config4(args, torch, A):
     W_lm, g_final = rnd((V, H), 0.02), torch.ones(H, device=dev, dtype=bf)
     ids = torch.randint(0, V, (T,), generator=g, device=dev)
     emb = rnd((V, H), 0.02)
-    X0 = emb[ids]
-    del emb
+    ids32 = ids.to(torch.int32)
+    X0 = A.alch_embed_forward(ids32, emb)
+    if not args.update:
+        del emb
     labels = torch.full((T,), -1, dtype=torch.int32, device=dev)
     lab2 = labels.view(B, S)
     lab2[:, :-1] = ids.view(B, S)[:, 1:].to(torch.int32)
@@ -390,19 +430,24 @@ def run_config4(args, torch, A):
         bgrads = [({} if args.frozen_base else {"d" + k: torch.empty_like(v) for k, v in W.items()}) for W in Ws]
         mode = "rank-%d adapter gradients on a %s base" % (r, "frozen" if args.frozen_base else "trained")
 
-        def backward(xf, rs, hooks=None):
+        def backward(xf, rs, hooks=None, head_grads=None):
             return A.alch_stack_backward_lora(shape, batch, rs, Ws, loras, r, 2.0, xf, g_final, W_lm, labels,
                                               loss_mask=loss_mask, grads_layers=bgrads, want_head=not args.frozen_base,
-                                              lora_grads_layers=lgrads, hooks=hooks, workspace=ws)
+                                              lora_grads_layers=lgrads, hooks=hooks, workspace=ws, head_grads=head_grads)
     else:
         grads = [({} if args.frozen_base else {"d" + k: torch.empty_like(v) for k, v in W.items()}) for W in Ws]
         ws = torch.empty(A.stack_backward_workspace_bytes(shape, L, V, T, S), dtype=torch.uint8, device=dev)
         if args.frozen_base:
             mode = "data gradients only (frozen base and head)"
 
-        def backward(xf, rs, hooks=None):
+        def backward(xf, rs, hooks=None, head_grads=None):
             return A.alch_stack_backward(shape, batch, rs, Ws, xf, g_final, W_lm, labels, loss_mask=loss_mask,
-                                         grads_layers=grads, want_head=not args.frozen_base, hooks=hooks, workspace=ws)
+                                         grads_layers=grads, want_head=not args.frozen_base, hooks=hooks, workspace=ws, head_grads=head_grads)
+
+    if args.update:
+        backward = with_update(args, torch, A, backward, Ws, loras if r else None, lgrads if r else None, bgrads if r else grads,
+                               emb, ids32, W_lm, g_final)
+        mode += ", clipping and AdamW update" + ("" if args.frozen_base else " behind the embedding gradient")
 
     def timed(fn, steps, warmup):
         for _ in range(warmup):

@@ -51,6 +51,10 @@ class Step:
         self.masters = [p.float() for p in self.params] if dtype == "bf16" else None
         self.m, self.v = [torch.zeros(p.shape, device="cuda") for p in self.params], [torch.full(p.shape, 1e-6, device="cuda") for p in self.params]
         self.norm = torch.empty(2, device="cuda")
+        self.head_grads = (torch.empty_like(self.g), torch.empty_like(self.E))
+        g = [self.grads[l]["d" + k] for l in range(L) for k in WEIGHT_KEYS] + list(self.head_grads)
+        self.all_grads, self.clip = g, A.GradList(g, g)
+        self.adamw = A.AdamwList(self.params, g, self.m, self.v, masters=self.masters, weight_decay=[0.0 if p.dim() == 1 else 0.1 for p in self.params])
 
     def gradients(self):
         A = self.A
@@ -58,19 +62,13 @@ class Step:
         for l in range(self.L):
             A.alch_layer_forward(self.shape, self.batch, self.acts[l], self.W[l], workspace=self.ws[0], rec=self.recs[l], Y=self.acts[l + 1])
         out = A.alch_stack_backward(self.shape, self.batch, self.recs, self.W, self.acts[-1], self.g, self.E, self.dev_labels,
-                                    grads_layers=self.grads, workspace=self.ws[1])
+                                    grads_layers=self.grads, workspace=self.ws[1], head_grads=self.head_grads)
         A.alch_embed_backward(self.dev_ids, out["dX_embed"], self.V, scale=SCALE, dW_embed=out["dW_lm"], accumulate=True, workspace=self.ws[2])
         return out
 
-    def tables(self, out):
-        """Of the gradients that this call's `out` holds; made once for buffers that stay."""
-        g = [self.grads[l]["d" + k] for l in range(self.L) for k in WEIGHT_KEYS] + [out["dg_final"], out["dW_lm"]]
-        decay = [0.0 if p.dim() == 1 else 0.1 for p in self.params]
-        return g, self.A.GradList(g, g), self.A.AdamwList(self.params, g, self.m, self.v, masters=self.masters, weight_decay=decay)
-
-    def update(self, clip, adamw):
-        self.A.alch_grad_clip(clip, MAX_NORM, norm_out=self.norm, workspace=self.ws[3])
-        self.A.alch_adamw_step(adamw, **HYPER)
+    def update(self):
+        self.A.alch_grad_clip(self.clip, MAX_NORM, norm_out=self.norm, workspace=self.ws[3])
+        self.A.alch_adamw_step(self.adamw, **HYPER)
 
     def reset(self):
         for p, s in zip(self.params, self.start):
@@ -90,9 +88,10 @@ class Step:
 def test_step_against_oracle_and_differences(dtype, shape_name, lens, V, wstd):
     s = Step(shape_name, dtype, lens, V, 2, wstd)
     out = s.gradients()
-    g, clip, adamw = s.tables(out)
+    g = s.all_grads
+    assert out["dg_final"].data_ptr() == g[-2].data_ptr() and out["dW_lm"].data_ptr() == g[-1].data_ptr()
     raw = [x.clone() for x in g]
-    s.update(clip, adamw)
+    s.update()
     torch.cuda.synchronize()
 
     osh, Ws, E, gain = oracle_shape(s.shp), [f64(W) for W in s.host], s.table.astype(np.float64), s.gain.astype(np.float64)
@@ -128,15 +127,9 @@ def test_step_against_oracle_and_differences(dtype, shape_name, lens, V, wstd):
 
 def test_captured_step_replays():
     s = Step("medium", "bf16", [100, 37], 300, 2, 0.05)
-    # the head's gradients come from the binding: the tables are made for copies at a fixed place
-    fixed = dict(dg_final=torch.empty_like(s.g), dW_lm=torch.empty_like(s.E))
-    _, clip, adamw = s.tables(fixed)
-
     def captured():
-        out = s.gradients()
-        for k, v in fixed.items():
-            v.copy_(out[k])
-        s.update(clip, adamw)
+        s.gradients()
+        s.update()
 
     eager = []
     for _ in range(3):
