@@ -392,7 +392,8 @@ def run_config4(args, torch, A):
     emb = rnd((V, H), 0.02)
     ids32 = ids.to(torch.int32)
     X0 = A.alch_embed_forward(ids32, emb)
-    if not args.update:
+    update = getattr(args, "update", False)
+    if not update:
         del emb
     labels = torch.full((T,), -1, dtype=torch.int32, device=dev)
     lab2 = labels.view(B, S)
@@ -444,7 +445,7 @@ def run_config4(args, torch, A):
             return A.alch_stack_backward(shape, batch, rs, Ws, xf, g_final, W_lm, labels, loss_mask=loss_mask,
                                          grads_layers=grads, want_head=not args.frozen_base, hooks=hooks, workspace=ws, head_grads=head_grads)
 
-    if args.update:
+    if update:
         backward = with_update(args, torch, A, backward, Ws, loras if r else None, lgrads if r else None, bgrads if r else grads,
                                emb, ids32, W_lm, g_final)
         mode += ", clipping and AdamW update" + ("" if args.frozen_base else " behind the embedding gradient")
