@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256) void k_sort_place(SortPass a, ZeroRows z, cons
 
 // ---- backward: sums ----------------------------------------------------------------------
 // A wavefront takes the rows whose tokens begin among its `part` sorted tokens (at most kPart), in 64 * kVec columns, and sums
-// each to its end, also past its own tokens.  The work-groups from `blocks` on zero rows.  Only rows of more than two parts' tokens are cut: every wavefront sums those among its
+// each to its end, also past its own tokens.  (A work-group of its own each: they end at different times.)  Only rows of more than two parts' tokens are cut: every wavefront sums those among its
 // own tokens and leaves them in fp32, [part][1] where the row begins here, [part][0] where it came from the part before.
 static constexpr int kPart = 32;
 __host__ __device__ inline int longest_whole(int part_len) { return 2 * part_len; }  // at most 64: the keys that a wavefront looks at
@@ -326,18 +326,13 @@ __device__ __forceinline__ void store_own(T* p, const V& v, int skip) {
 }
 
 template <typename T, int kVec, bool kAccumulate>
-__global__ __launch_bounds__(256) void k_embed_sums(const int* __restrict__ keys, const int* __restrict__ tokens, int n, int vocab, int hidden,
+__global__ __launch_bounds__(64) void k_embed_sums(const int* __restrict__ keys, const int* __restrict__ tokens, int n, int vocab, int hidden,
                                                     const T* __restrict__ dX, float scale, T* __restrict__ dW, float* __restrict__ partial,
-                                                    int* __restrict__ cut, int stride, int part_len, int tiles, long long units, int blocks, ZeroRows z,
-                                                    const int* __restrict__ ids, const int* __restrict__ where) {
-    if ((int)blockIdx.x >= blocks) {
-        zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x - blocks, gridDim.x - blocks);
-        return;
-    }
+                                                    int* __restrict__ cut, int stride, int part_len, int tiles, long long units) {
     typedef typename Piece<T, kVec>::type vec;
     constexpr int kBatch = 8;  // rows that are on their way while as many are summed
-    const int lane = threadIdx.x & 63;
-    for (long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (long long)blocks * 4) {
+    const int lane = threadIdx.x;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
         const int part = __builtin_amdgcn_readfirstlane((int)(u / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(u % tiles));
         const int p0 = part * part_len, own = (tile * 64 + lane) * kVec;
         const int longest = longest_whole(part_len);
@@ -445,14 +440,20 @@ __global__ __launch_bounds__(256) void k_embed_sums(const int* __restrict__ keys
 }
 
 // The rows that were cut: the part in which a row begins adds what the parts behind it have of it, in their order.  A work-group
-// looks at kJoinParts parts, in 256 columns; its four wavefronts take a quarter of a row's parts each.
+// looks at kJoinParts parts, in 256 columns; its four wavefronts take a quarter of a row's parts each.  The work-groups from `blocks`
+// on zero rows, where the sort has left that to this launch.
 static constexpr int kJoinParts = 16;
-template <typename T>
+template <typename T, int kVec>
 __global__ __launch_bounds__(256) void k_embed_join(const int* __restrict__ keys, int n, int hidden, float scale, int accumulate, T* __restrict__ dW,
-                                                    const float* __restrict__ partial, const int* __restrict__ cut, int stride, int part_len, int parts) {
+                                                    const float* __restrict__ partial, const int* __restrict__ cut, int stride, int part_len, int parts,
+                                                    int slices, int blocks, ZeroRows z, const int* __restrict__ ids, const int* __restrict__ where) {
+    if ((int)blockIdx.x >= blocks) {
+        zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x - blocks, gridDim.x - blocks);
+        return;
+    }
     typedef float vec __attribute__((ext_vector_type(4)));
     __shared__ vec red[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = blockIdx.y * 256, base = blockIdx.x * kJoinParts;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = (int)blockIdx.x % slices * 256, base = (int)blockIdx.x / slices * kJoinParts;
     unsigned long long todo = __ballot(lane < kJoinParts && base + lane < parts && cut[base + lane]);
     for (; todo; todo &= todo - 1) {
         const int part = base + __ffsll(todo) - 1, key = keys[(part + 1) * part_len];  // (a cut row goes on behind its part)
@@ -678,16 +679,14 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
     z.begin = z.end;
     z.end = table.blocks;
     const long long units = (long long)p.parts * tiles;
-    const int blocks = (int)std::min<long long>((units + 3) / 4, 1 << 20), grid = blocks + std::min(z.end - z.begin, kMaxBlocks);
-    if (accumulate)
-        k_embed_sums<T, kVec, true><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, dW, p.partial, p.cut, p.stride, p.part_len, tiles,
-                                                              units, blocks, z, ids, p.where);
-    else
-        k_embed_sums<T, kVec, false><<<grid, 256, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, dW, p.partial, p.cut, p.stride, p.part_len, tiles,
-                                                               units, blocks, z, ids, p.where);
-    if (n > longest_whole(p.part_len))
-        k_embed_join<T><<<dim3(ceil_div(p.parts, kJoinParts), ceil_div(hidden, 256)), 256, 0, stream>>>(keys, n, hidden, scale, accumulate, dW, p.partial, p.cut,
-                                                                                                  p.stride, p.part_len, p.parts);
+    const int grid = (int)std::min<long long>(units, kMaxBlocks);
+    const auto sums = accumulate ? k_embed_sums<T, kVec, true> : k_embed_sums<T, kVec, false>;
+    sums<<<grid, 64, 0, stream>>>(keys, tokens, n, vocab, hidden, dX, scale, dW, p.partial, p.cut, p.stride, p.part_len, tiles, units);
+    const int slices = ceil_div(hidden, 256), joins = n > longest_whole(p.part_len) ? ceil_div(p.parts, kJoinParts) * slices : 0;
+    const int zeros = std::min(z.end - z.begin, kMaxBlocks);
+    if (joins + zeros > 0)
+        k_embed_join<T, kVec><<<joins + zeros, 256, 0, stream>>>(keys, n, hidden, scale, accumulate, dW, p.partial, p.cut, p.stride, p.part_len, p.parts,
+                                                                 slices, joins, z, ids, p.where);
 }
 
 int launch_embed_backward(alch_dtype dt, const int* ids, const void* dX, int n_tokens, int vocab, int hidden, float scale, int accumulate,
