@@ -82,7 +82,7 @@ CASES = [(1, 4096, 1000, "mixed"), (31, 256, 64, "mixed"), (32, 256, 64, "one"),
          (2049, 8200, 300, "runs"), (300, 8, 20, "runs"), (1024, 520, 40, "runs"), (777, 33, 2, "runs"), (16500, 2104, 500, "runs"),
          (16384, 1032, 90, "mixed"), (1025, 8, 20, "runs"), (1100, 264, 1, "one"), (1200, 64, 9, "padding"), (2000, 9, 31, "runs"), (90, 9, 31, "runs"),
          (3000, 515, 700, "mixed"), (8192, 100, 40, "runs"), (5000, 260, 999, "mixed"), (2500, 16, 2499, "ascending"), (3000, 70, 9, "padding"),
-         (3500, 1032, 20000, "runs"), (2100, 40, 100000, "mixed"), (4096, 72, 128256, "one"), (4097, 16, 4097, "ascending")]
+         (3500, 1032, 20000, "runs"), (2100, 40, 100000, "mixed"), (4096, 72, 128256, "one"), (1048581, 24, 3000, "runs"), (20000, 8, 3000000, "mixed"), (8193, 40, 30000, "mixed"), (4097, 16, 4097, "ascending")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -159,6 +159,26 @@ def test_table_beyond_32_bit_offsets():
     assert dW[-1, 0] == 6 and dW[-2, 0] == 3 and bool((dW[-2:] == dW[-2:, :1]).all()) and bool((dW[:V - 2] == 0).all())
     dW = A.alch_embed_backward(ids, X, V, dW_embed=W)
     assert dW[-1, 0] == 3 and dW[-2, 0] == 1 and bool((dW[-2:] == dW[-2:, :1]).all()) and bool((dW[:V - 2] == 0).all())
+
+
+def test_ids_of_31_bits():
+    import paper_2503_01066_amd as A
+    V, T = (1 << 30) + 77, 17000  # four digits
+    r = np.random.default_rng(1)
+    ids = np.concatenate([r.integers(0, V, T - 4000), np.full(2000, V - 1), r.choice([V, -1, 2 ** 31 - 1], 2000)]).astype(np.int32)
+    r.shuffle(ids)
+    dev = torch.from_numpy(ids).cuda()
+    dX = torch.ones((T, 1), device="cuda")
+    dW = torch.full((V, 1), 3.0, device="cuda")
+    A.alch_embed_backward(dev, dX, V, dW_embed=dW)
+    met, n = np.unique(ids[(ids >= 0) & (ids < V)], return_counts=True)
+    at = torch.from_numpy(met).long().cuda()
+    assert torch.equal(dW[at, 0], torch.from_numpy(n).float().cuda()) and int((dW != 0).sum()) == len(met)
+    A.alch_embed_backward(dev, dX, V, dW_embed=dW, accumulate=True)
+    assert torch.equal(dW[at, 0], torch.from_numpy(2 * n).float().cuda()) and int((dW != 0).sum()) == len(met)
+    X = A.alch_embed_forward(dev, dW)
+    ok = torch.from_numpy((ids >= 0) & (ids < V)).cuda()
+    assert torch.equal(X[ok], dW[dev[ok].long()]) and bool((X[~ok] == 0).all())
 
 
 def test_other_streams_and_two_calls_at_once():
