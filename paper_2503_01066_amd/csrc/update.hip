@@ -4,8 +4,8 @@
 //   m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  w -= lr (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + decay w)
 //
 // Both are bound by memory: one pass over the gradients for the norm, one for what uses the factor.  All tensors of a call share
-// its launches: they are cut into chunks, and every work-group finds the tensor of a chunk in a table of the tensors' first
-// chunks, which it makes in LDS from the tensors' lengths.
+// its launches: they are cut into chunks, and every work-group finds the tensor of a chunk in a table that it makes of the tensors'
+// lengths.
 #include <algorithm>
 #include <math.h>
 
@@ -15,57 +15,96 @@ namespace alch {
 
 static constexpr int kMaxTensors = ALCH_MAX_TENSORS;
 static constexpr int kNormBlocks = 1024;
+static constexpr int kMaxChunkBlocks = 1 << 22;  // of a launch; chunks behind them are gone over in rounds
 
 typedef float f32x4_u __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_u __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_u __attribute__((ext_vector_type(4)));
 
-// first[i] = chunks of the tensors before i, first[n] = all of them; chunk_of(tensor): its elements a chunk.  Work-groups of 256 threads.
-template <typename Tensor, typename F>
-__device__ __forceinline__ void chunk_table(const Tensor* __restrict__ tensors, int n, F chunk_of, int* first /*[n + 1]*/) {
-    __shared__ int wave_total[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int carry = 0;
-    for (int base = 0; base < n; base += 256) {
-        const int i = base + tid;
-        int own = 0;
-        if (i < n) {
-            const int chunk = chunk_of(tensors[i].dtype);  // (a power of two)
-            own = (int)((tensors[i].n + chunk - 1) >> (31 - __clz(chunk)));
-        }
-        int inc = own;
+// Which tensor a chunk belongs to, and which of its chunks it is.  Up to 64 tensors (kFew) every wavefront holds the table in
+// registers, a tensor a lane, so that a chunk's address is one load behind the launch; more of them have their first chunks in LDS.
+// Work-groups of 256 threads, all of which make the table and look chunks up together.
+template <typename Tensor, bool kFew>
+struct ChunkTable {
+    struct Chunk {
+        Tensor t;
+        int index;
+    };
+    static constexpr int kWords = sizeof(Tensor) / 4;
+    const Tensor* tensors;
+    int n, chunks;
+    int* first;         // [kMaxTensors + 1]: chunks of the tensors before, of all of them behind the last
+    int words[kWords];  // kFew: the lane's tensor,
+    int before;         // the chunks of those before it
+
+    template <typename F>
+    static __device__ __forceinline__ int count(const Tensor& t, F chunk_of) {
+        const int chunk = chunk_of(t.dtype);  // (a power of two)
+        return (int)((t.n + chunk - 1) >> (31 - __clz(chunk)));
+    }
+    static __device__ __forceinline__ int inclusive(int v) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(inc, d, 64);
-            if (lane >= d) inc += o;
+            const int o = __shfl_up(v, d, 64);
+            if (lane >= d) v += o;
         }
-        if (lane == 63) wave_total[wave] = inc;
-        __syncthreads();
-        int before = carry;
+        return v;
+    }
+    template <typename F>
+    __device__ __forceinline__ ChunkTable(const Tensor* __restrict__ tensors_, int n_, F chunk_of, int* first_) : tensors(tensors_), n(n_), first(first_) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        if constexpr (kFew) {
+            Tensor t = {};
+            if (lane < n) t = tensors[lane];
+            __builtin_memcpy(words, &t, sizeof(Tensor));
+            const int own = lane < n ? count(t, chunk_of) : 0, inc = inclusive(own);
+            before = inc - own;
+            chunks = __builtin_amdgcn_readlane(inc, 63);
+        } else {
+            __shared__ int wave_total[4];
+            int carry = 0;
+            for (int base = 0; base < n; base += 256) {
+                const int i = base + tid, own = i < n ? count(tensors[i], chunk_of) : 0, inc = inclusive(own);
+                if (lane == 63) wave_total[wave] = inc;
+                __syncthreads();
+                int ahead = carry;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) before += wave_total[w];
-            carry += wave_total[w];
+                for (int w = 0; w < 4; ++w) {
+                    if (w < wave) ahead += wave_total[w];
+                    carry += wave_total[w];
+                }
+                if (i < n) first[i] = ahead + inc - own;
+                __syncthreads();
+            }
+            chunks = carry;
         }
-        if (i < n) first[i] = before + inc - own;
-        __syncthreads();
     }
-    if (tid == 0) first[n] = carry;
-    __syncthreads();
-}
-
-// The tensor of a chunk: the last one whose first chunk is not behind it (of empty ones, which begin where the next one does,
-// the last, which is not empty).  64 candidates at a time.
-__device__ __forceinline__ int tensor_of(const int* first, int n, int chunk) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, step = 1;
-    while (step * 64 < n) step *= 64;
-    for (; step >= 1; step /= 64) {
-        const int i = lo + lane * step;
-        lo += (__popcll(__ballot(i < n && first[i] <= chunk)) - 1) * step;
+    // The last tensor whose first chunk is not behind it (of empty ones, which begin where the next one does, the last, which is not
+    // empty), among 64 at a time.
+    __device__ __forceinline__ Chunk find(int c) const {
+        const int lane = threadIdx.x & 63;
+        if constexpr (kFew) {
+            const int at = __popcll(__ballot(lane < n && before <= c)) - 1;
+            int w[kWords];
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = __builtin_amdgcn_readlane(words[i], at);
+            Chunk r;
+            __builtin_memcpy(&r.t, w, sizeof(Tensor));
+            r.index = c - __builtin_amdgcn_readlane(before, at);
+            return r;
+        } else {
+            int at = 0, step = 1;
+            while (step * 64 < n) step *= 64;
+            for (; step >= 1; step /= 64) {
+                const int i = at + lane * step;
+                at += (__popcll(__ballot(i < n && first[i] <= c)) - 1) * step;
+            }
+            at = __builtin_amdgcn_readfirstlane(at);
+            return {tensors[at], c - first[at]};
+        }
     }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
+};
 
 __device__ __forceinline__ double block_sum(double v, double* red /*[4]*/) {
 #pragma unroll
@@ -89,12 +128,13 @@ struct ClipChunk {
     int elements, dtype;
 };
 __host__ __device__ inline int clip_elements(int dtype) { return 256 * kBatch * (dtype == ALCH_BF16 ? 8 : 4); }
-__device__ __forceinline__ ClipChunk clip_chunk(const alch_grad_tensor* __restrict__ tensors, const int* first, int n, int c) {
-    const int t = tensor_of(first, n, c);
-    const alch_grad_tensor a = tensors[t];
-    const int chunk = clip_elements(a.dtype);
-    const long long begin = (long long)(c - first[t]) * chunk, at = begin * (a.dtype == ALCH_BF16 ? 2 : 4);
-    return {static_cast<const char*>(a.grad) + at, a.out ? static_cast<char*>(a.out) + at : nullptr, (int)min((long long)chunk, (long long)a.n - begin), a.dtype};
+template <bool kFew>
+__device__ __forceinline__ ClipChunk clip_chunk(const ChunkTable<alch_grad_tensor, kFew>& table, int c) {
+    const auto k = table.find(c);
+    const int chunk = clip_elements(k.t.dtype);
+    const long long begin = (long long)k.index * chunk, at = begin * (k.t.dtype == ALCH_BF16 ? 2 : 4);
+    return {static_cast<const char*>(k.t.grad) + at, k.t.out ? static_cast<char*>(k.t.out) + at : nullptr, (int)min((long long)chunk, (long long)k.t.n - begin),
+            k.t.dtype};
 }
 // The pieces of a thread.  Of a tensor's last chunk those that lie in it as a whole, the others are zero; behind them at most one
 // element a thread, *rest (its index, or -1), *r.  Returns whether the chunk is whole.
@@ -117,21 +157,22 @@ __device__ __forceinline__ bool clip_load(const ClipChunk& c, f32x4_u (&v)[kBatc
 // The squares are added in 64 bits: no gradient of finite numbers overflows there, none vanishes, and the order of the
 // additions (which differs with the lengths of the tensors) is not seen in a norm of 32 bits.  They cost nothing beside the
 // loads (436 MB: 73.9 us, 73.1 with sums in fp32).
+template <bool kFew>
 __global__ __launch_bounds__(256) void k_norm(const alch_grad_tensor* __restrict__ tensors, int n, double* __restrict__ partial) {
-    __shared__ int first[kMaxTensors + 1];
+    __shared__ int first[kFew ? 1 : kMaxTensors + 1];
     __shared__ double red[4];
-    chunk_table(tensors, n, clip_elements, first);
-    const int chunks = first[n];
+    const ChunkTable<alch_grad_tensor, kFew> table(tensors, n, clip_elements, first);
+    const int chunks = table.chunks;
     double s = 0.0;
     ClipChunk next = {};
-    if ((int)blockIdx.x < chunks) next = clip_chunk(tensors, first, n, blockIdx.x);
+    if ((int)blockIdx.x < chunks) next = clip_chunk(table, blockIdx.x);
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         const ClipChunk a = next;
         f32x4_u v[kBatch];
         int rest = -1;
         float r = 0.f;
         clip_load(a, v, &rest, &r);
-        if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);  // (while these are on their way)
         if (a.dtype == ALCH_BF16) {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
@@ -175,13 +216,14 @@ __device__ __forceinline__ float clip_factor(const NormSums& sums, float max_nor
     return factor;
 }
 
+template <bool kFew>
 __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict__ tensors, int n, const double* __restrict__ partial, int blocks,
                                               float max_norm, float* __restrict__ norm_out) {
-    __shared__ int first[kMaxTensors + 1];
+    __shared__ int first[kFew ? 1 : kMaxTensors + 1];
     const NormSums sums = norm_sums(partial, blocks);
-    chunk_table(tensors, n, clip_elements, first);
-    const int chunks = first[n];
-    ClipChunk a = clip_chunk(tensors, first, n, blockIdx.x);  // (no more work-groups than chunks)
+    const ChunkTable<alch_grad_tensor, kFew> table(tensors, n, clip_elements, first);
+    const int chunks = table.chunks;
+    ClipChunk a = clip_chunk(table, blockIdx.x);  // (no more work-groups than chunks)
     float factor = 0.f;
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         f32x4_u v[kBatch];
@@ -189,10 +231,9 @@ __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict
         float r = 0.f;
         const bool full = a.out && clip_load(a, v, &rest, &r);
         ClipChunk next = {};
-        if (c + (int)gridDim.x < chunks) next = clip_chunk(tensors, first, n, c + gridDim.x);  // (while these are on their way)
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);  // (while these are on their way)
         if (c == (int)blockIdx.x) factor = clip_factor(sums, max_norm, norm_out);
         if (a.out && !(a.out == a.grad && factor == 1.f)) {
-            const int pieces = full ? 256 * kBatch : a.elements / (a.dtype == ALCH_BF16 ? 8 : 4);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 if (a.dtype == ALCH_BF16) {
@@ -203,7 +244,16 @@ __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict
                 } else {
                     v[b] *= factor;
                 }
-                if (full || (int)threadIdx.x + 256 * b < pieces) __builtin_nontemporal_store(v[b], reinterpret_cast<f32x4_u*>(a.out) + threadIdx.x + 256 * b);
+            }
+            f32x4_u* out = reinterpret_cast<f32x4_u*>(a.out) + threadIdx.x;
+            if (full) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) __builtin_nontemporal_store(v[b], out + 256 * b);
+            } else {
+                const int pieces = a.elements / (a.dtype == ALCH_BF16 ? 8 : 4);
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    if ((int)threadIdx.x + 256 * b < pieces) __builtin_nontemporal_store(v[b], out + 256 * b);
             }
             if (rest >= 0) {
                 if (a.dtype == ALCH_BF16) reinterpret_cast<__bf16*>(a.out)[rest] = (__bf16)(r * factor);
@@ -234,9 +284,14 @@ int launch_grad_clip(int n_tensors, const alch_grad_tensor* tensors, const alch_
     TraceScope ts(kTraceUpdate, 0.0, bytes * (any_out ? 3 : 1), stream);
     double* partial = static_cast<double*>(workspace);
     const int blocks = (int)std::min<long long>(std::max<long long>(chunks, 1), kNormBlocks);
-    k_norm<<<blocks, 256, 0, stream>>>(tensors, n_tensors, partial);
+    const bool few = n_tensors <= 64;
+    const auto norm = few ? k_norm<true> : k_norm<false>;
+    const auto clip = few ? k_clip<true> : k_clip<false>;
+    norm<<<blocks, 256, 0, stream>>>(tensors, n_tensors, partial);
+    // a work-group a chunk where the table costs little: 436 MB of nine tensors 204 us, 215 with 1024 work-groups that walk the chunks;
+    // 42 MB of 448 tensors 27.9 and 26.3
     if (any_out)
-        k_clip<<<blocks, 256, 0, stream>>>(tensors, n_tensors, partial, blocks, max_norm, norm_out);
+        clip<<<few ? (int)std::min<long long>(chunks, kMaxChunkBlocks) : blocks, 256, 0, stream>>>(tensors, n_tensors, partial, blocks, max_norm, norm_out);
     else
         k_norm_finish<<<1, 256, 0, stream>>>(partial, blocks, max_norm, norm_out);
     ALCH_HIP_TRY(hipGetLastError());
@@ -244,8 +299,9 @@ int launch_grad_clip(int n_tensors, const alch_grad_tensor* tensors, const alch_
 }
 
 // ---- AdamW --------------------------------------------------------------------------------
-static constexpr int kAdamwBatch = 2, kAdamwChunk = 1024 * kAdamwBatch;  // elements
-static constexpr int kAdamwBlocks = 1 << 22;  // one work-group a chunk: 1061 us for 218 M elements, 1192 with 2048 work-groups that walk them
+// Elements of a chunk, four a thread, and a work-group a chunk: 218 M elements 1054 us, 1079 with two pieces a thread, 1192 with 2048
+// work-groups that walk the chunks.
+static constexpr int kAdamwChunk = 1024;
 
 struct AdamwArgs {
     const alch_adamw_tensor* tensors;
@@ -275,13 +331,11 @@ struct AdamwChunk {
     long long at;
     int elements;
 };
-__device__ __forceinline__ AdamwChunk adamw_chunk(const alch_adamw_tensor* __restrict__ tensors, const int* first, int n, int c) {
-    const int i = tensor_of(first, n, c);
-    AdamwChunk a;
-    a.t = tensors[i];
-    a.at = (long long)(c - first[i]) * kAdamwChunk;
-    a.elements = (int)min((long long)kAdamwChunk, (long long)a.t.n - a.at);
-    return a;
+template <bool kFew>
+__device__ __forceinline__ AdamwChunk adamw_chunk(const ChunkTable<alch_adamw_tensor, kFew>& table, int c) {
+    const auto k = table.find(c);
+    const long long at = (long long)k.index * kAdamwChunk;
+    return {k.t, at, (int)min((long long)kAdamwChunk, (long long)k.t.n - at)};
 }
 
 struct AdamwRates {
@@ -299,39 +353,22 @@ __device__ __forceinline__ void adamw(const AdamwChunk& k, const AdamwArgs& a, c
     T* param = static_cast<T*>(k.t.param) + k.at;
     const T* grad = static_cast<const T*>(k.t.grad) + k.at;
     float *m = k.t.m + k.at, *v = k.t.v + k.at, *master = kMaster ? k.t.master + k.at : nullptr;
-    f32x4_u gv[kAdamwBatch], mv[kAdamwBatch], vv[kAdamwBatch], wv[kAdamwBatch];
-    const int whole = k.elements / 4 - (int)threadIdx.x;  // (of the pieces of four elements, those from this thread's first one on)
-    const bool full = k.elements == kAdamwChunk;
-    const auto load = [&](int b) {
-        const int i = (threadIdx.x + 256 * b) * 4;
-        gv[b] = load4(grad + i);
-        mv[b] = load4(m + i);
-        vv[b] = load4(v + i);
-        if constexpr (kMaster) wv[b] = load4(master + i);
-        else wv[b] = load4(param + i);
-    };
-    if (full) {
-#pragma unroll
-        for (int b = 0; b < kAdamwBatch; ++b) load(b);
-    } else {
-#pragma unroll
-        for (int b = 0; b < kAdamwBatch; ++b)
-            if (256 * b < whole) load(b);
-    }
-#pragma unroll
-    for (int b = 0; b < kAdamwBatch; ++b) {
-        if (!full && 256 * b >= whole) continue;
-        const int i = (threadIdx.x + 256 * b) * 4;
+    const int at = threadIdx.x * 4;
+    if (at + 4 <= k.elements) {
+        const f32x4_u g4 = load4(grad + at);
+        f32x4_u m4 = load4(m + at), v4 = load4(v + at), w4;
+        if constexpr (kMaster) w4 = load4(master + at);
+        else w4 = load4(param + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float me = mv[b][e], ve = vv[b][e], we = wv[b][e];
-            adamw_element(a, r, k.t.weight_decay, gv[b][e], me, ve, we);
-            mv[b][e] = me; vv[b][e] = ve; wv[b][e] = we;
+            float me = m4[e], ve = v4[e], we = w4[e];
+            adamw_element(a, r, k.t.weight_decay, g4[e], me, ve, we);
+            m4[e] = me; v4[e] = ve; w4[e] = we;
         }
-        store4(m + i, mv[b]);
-        store4(v + i, vv[b]);
-        if constexpr (kMaster) store4(master + i, wv[b]);
-        store4(param + i, wv[b]);
+        store4(m + at, m4);
+        store4(v + at, v4);
+        if constexpr (kMaster) store4(master + at, w4);
+        store4(param + at, w4);
     }
     const int i = (k.elements & ~3) + (int)threadIdx.x;  // behind the last whole piece
     if (i < k.elements) {
@@ -344,8 +381,9 @@ __device__ __forceinline__ void adamw(const AdamwChunk& k, const AdamwArgs& a, c
     }
 }
 
+template <bool kFew>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
-    __shared__ int first[kMaxTensors + 1];
+    __shared__ int first[kFew ? 1 : kMaxTensors + 1];
     __shared__ float shared_c[3];
     const float factor = a.grad_factor ? *a.grad_factor : 1.f;
     if (!(fabsf(factor) < INFINITY)) return;            // (the gradients are of no use: nothing changes)
@@ -356,11 +394,11 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
         shared_c[1] = (float)correction(a.beta1, step);
         shared_c[2] = (float)sqrt(correction(a.beta2, step));
     }
-    chunk_table(a.tensors, a.n, [](int) { return kAdamwChunk; }, first);
-    const int chunks = first[a.n];
+    const ChunkTable<alch_adamw_tensor, kFew> table(a.tensors, a.n, [](int) { return kAdamwChunk; }, first);
+    if (a.schedule) __syncthreads();  // (its rates have been written)
     const AdamwRates r{factor, a.schedule ? shared_c[0] : a.lr, a.schedule ? shared_c[1] : a.c1, a.schedule ? shared_c[2] : a.c2};
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const AdamwChunk k = adamw_chunk(a.tensors, first, a.n, c);
+    for (int c = blockIdx.x; c < table.chunks; c += gridDim.x) {
+        const AdamwChunk k = adamw_chunk(table, c);
         if (k.t.dtype == ALCH_BF16) {
             if (k.t.master) adamw<__bf16, true>(k, a, r);
             else adamw<__bf16, false>(k, a, r);
@@ -385,7 +423,8 @@ int launch_adamw(int n_tensors, const alch_adamw_tensor* tensors, const alch_ada
                       p.schedule ? 0.f : (float)sqrt(correction(p.beta2, p.step)),
                       (float)p.beta1, (float)p.beta2, (float)(1.0 - p.beta1), (float)(1.0 - p.beta2), (float)p.eps, p.beta1, p.beta2,
                       p.schedule, p.grad_factor};
-    k_adamw<<<(int)std::min<long long>(chunks, kAdamwBlocks), 256, 0, stream>>>(a);
+    const auto kernel = n_tensors <= 64 ? k_adamw<true> : k_adamw<false>;
+    kernel<<<(int)std::min<long long>(chunks, kMaxChunkBlocks), 256, 0, stream>>>(a);
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }
