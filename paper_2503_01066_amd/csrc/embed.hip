@@ -21,17 +21,21 @@ struct Piece {
 };
 
 // A work-group goes over 8 KB of rows that lie behind one another, two pieces a thread: `1 << log_lanes` threads to a row, one row
-// in `segments` work-groups where it is longer.  Work-groups with more, or with fewer that have more of them under way, are slower:
-// 70,001 rows of 8 KB copied in 134 us, with two rows a work-group 143, with four 146; 1.05 GB zeroed in 154, with four rows 190.
+// in `segments` work-groups where it is longer, with three pieces a thread where that saves one (50,000 rows of 10 KB copied in 130 us
+// with two, 120 with three).  Work-groups with more, or with fewer that have more of them under way, are slower: 70,001 rows of 8 KB
+// copied in 131 us, with two rows a work-group 143, with four 146.
 struct RowGrid {
-    int log_lanes, segments, blocks;
+    int log_lanes, per, segments, blocks;
+    bool pairs;  // of zeros: see zero_block
 };
 static RowGrid row_grid(long long rows, int hidden, int vec) {
     RowGrid g;
     const int pieces = ceil_div(hidden, vec);
     g.log_lanes = 0;
     while (g.log_lanes < 8 && (2 << g.log_lanes) < pieces) ++g.log_lanes;
-    g.segments = ceil_div(pieces, 2 << g.log_lanes);
+    g.per = ceil_div(pieces, 3 << g.log_lanes) < ceil_div(pieces, 2 << g.log_lanes) ? 3 : 2;
+    g.segments = ceil_div(pieces, g.per << g.log_lanes);
+    g.pairs = false;
     g.blocks = (int)((rows + (256 >> g.log_lanes) - 1) / (256 >> g.log_lanes) * g.segments);  // (at most 2^30: 2^40 elements)
     return g;
 }
@@ -55,19 +59,20 @@ __global__ __launch_bounds__(256) void k_embed(const int* __restrict__ ids, cons
         long long t = first_row(g, b, &segment) + (threadIdx.x >> g.log_lanes);
         if (kWide) t = __builtin_amdgcn_readfirstlane((int)t);
         if (t >= n_tokens) continue;
-        const int id = ids[t], c0 = ((segment << (g.log_lanes + 1)) + lane) * kVec, step = kVec << g.log_lanes;
+        const int id = ids[t], c0 = ((segment * g.per << g.log_lanes) + lane) * kVec, step = kVec << g.log_lanes;
+        const int end = min(hidden, c0 + g.per * step);
         const bool valid = (unsigned)id < (unsigned)vocab;
         const T* src = W + (long long)(valid ? id : 0) * hidden;
-        vec v[2] = {};
+        vec v[3] = {};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (valid && c0 + j * step < hidden) v[j] = *reinterpret_cast<const vec*>(src + min(c0 + j * step, hidden - kVec));
+        for (int j = 0; j < 3; ++j)
+            if (valid && c0 + j * step < end) v[j] = *reinterpret_cast<const vec*>(src + min(c0 + j * step, hidden - kVec));
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < 3; ++j) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[j][e] = (T)((float)v[j][e] * scale);
             if (!valid) v[j] = vec{};  // (also where the scale is negative or no number)
-            if (c0 + j * step < hidden) __builtin_nontemporal_store(v[j], reinterpret_cast<vec*>(X + t * hidden + min(c0 + j * step, hidden - kVec)));
+            if (c0 + j * step < end) __builtin_nontemporal_store(v[j], reinterpret_cast<vec*>(X + t * hidden + min(c0 + j * step, hidden - kVec)));
         }
     }
 }
@@ -141,7 +146,8 @@ __global__ __launch_bounds__(256) void k_sort_count(const int* __restrict__ ids,
     for (int b = threadIdx.x; b < bins; b += 256) counts[(long long)blockIdx.x * bins + b] = hist[b];
 }
 
-// Zeros a work-group's rows of a table, the block-th of the grid; present(row): whether a token has it.
+// Zeros a work-group's rows of a table, the block-th of the grid; present(row): whether a token has it.  g.pairs: a thread's first two
+// pieces lie next to one another, instead of a row of threads' first pieces before their second ones.
 template <typename T, int kVec, typename F>
 __device__ __forceinline__ void zero_block(T* __restrict__ dW, int block, int vocab, int hidden, const RowGrid& g, F present) {
     typedef typename Piece<T, kVec>::type vec;
@@ -149,14 +155,23 @@ __device__ __forceinline__ void zero_block(T* __restrict__ dW, int block, int vo
     const long long row = first_row(g, block, &segment) + (threadIdx.x >> g.log_lanes);
     const auto zero = [&](long long r) {
         if (r >= vocab || present(r)) return;
-        // (a thread's two pieces next to one another: 154 us for 1.05 GB, 171 with the second 4 KB behind the first)
-        const int c0 = ((segment << (g.log_lanes + 1)) + 2 * (threadIdx.x & ((1 << g.log_lanes) - 1))) * kVec;
+        const int lane = threadIdx.x & ((1 << g.log_lanes) - 1), first = segment * g.per << g.log_lanes;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (c0 + j * kVec < hidden) *reinterpret_cast<vec*>(dW + r * hidden + min(c0 + j * kVec, hidden - kVec)) = vec{};
+        for (int j = 0; j < 3; ++j) {
+            const int c = (first + (g.pairs && j < 2 ? 2 * lane + j : (j << g.log_lanes) + lane)) * kVec;
+            if (j < g.per && c < hidden) *reinterpret_cast<vec*>(dW + r * hidden + min(c, hidden - kVec)) = vec{};
+        }
     };
     if (g.log_lanes >= 6) zero(__builtin_amdgcn_readfirstlane((int)row));  // (one row a wavefront: looked up as scalars)
     else zero(row);
+}
+
+// Whether a launch that mostly zeros does so in pairs: tables beyond the last-level cache (256 MB) whose rows fill their work-groups.
+// us of a whole backward pass of 9000 tokens, in pairs / not: rows of 8 KB 82 MB 57.4 / 53.6, 246 MB 72.7 / 64.6, 492 MB 114 / 119, 1.05 GB
+// 198 / 212; of 4 KB 1.05 GB 191 / 202; of 16 KB 983 MB 209 / 216; of 2 KB 614 MB 118 / 119; of 10 KB 1.02 GB 229 / 224, of 7 KB 919 MB 194 / 183.
+// Beside the sums of few tokens or the joins not in pairs serves better (1.05 GB, 64 tokens 160 / 166, 487 tokens 184 / 172, 1000 tokens 212 / 164).
+static bool zero_in_pairs(const RowGrid& g, long long rows, int hidden, int vec, size_t size) {
+    return rows * hidden * (long long)size > 256LL << 20 && hidden % (vec * (g.per << g.log_lanes)) == 0;
 }
 
 // Blocks begin .. end-1 of the table's grid.
@@ -638,6 +653,7 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
                                   T* dW, hipStream_t stream) {
     const RowGrid table = row_grid(accumulate ? 0 : vocab, hidden, kVec);
     ZeroRows z{n, vocab, table, 0, 0};
+    z.grid.pairs = zero_in_pairs(table, vocab, hidden, kVec, sizeof(T));
     if (n <= 0) {
         z.end = table.blocks;
         if (z.end) k_embed_zero<T, kVec><<<std::min(z.end, kMaxBlocks), 256, 0, stream>>>(z, ids, p.where, dW, hidden);
@@ -676,8 +692,9 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
             tokens = p.tokens[i & 1];
         }
     }
-    z.begin = z.end;
+    z.begin = z.end;  // what is left goes beside the joins
     z.end = table.blocks;
+    z.grid.pairs = false;
     const long long units = (long long)p.parts * tiles;
     const int grid = (int)std::min<long long>(units, kMaxBlocks);
     const auto sums = accumulate ? k_embed_sums<T, kVec, true> : k_embed_sums<T, kVec, false>;
