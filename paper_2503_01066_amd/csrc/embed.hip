@@ -171,7 +171,7 @@ __device__ __forceinline__ void zero_block(T* __restrict__ dW, int block, int vo
 // 198 / 212; of 4 KB 1.05 GB 191 / 202; of 16 KB 983 MB 209 / 216; of 2 KB 614 MB 118 / 119; of 10 KB 1.02 GB 229 / 224, of 7 KB 919 MB 194 / 183.
 // Beside the sums of few tokens or the joins not in pairs serves better (1.05 GB, 64 tokens 160 / 166, 487 tokens 184 / 172, 1000 tokens 212 / 164).
 static bool zero_in_pairs(const RowGrid& g, long long rows, int hidden, int vec, size_t size) {
-    return rows * hidden * (long long)size > 256LL << 20 && hidden % (vec * (g.per << g.log_lanes)) == 0;
+    return g.per == 2 && rows * hidden * (long long)size > 256LL << 20 && hidden % (vec * (2 << g.log_lanes)) == 0;
 }
 
 // Blocks begin .. end-1 of the table's grid.
@@ -194,10 +194,15 @@ __global__ __launch_bounds__(256) void k_embed_zero(ZeroRows z, const int* __res
     zero_rows<T, kVec>(z, ids, where, dW, hidden, blockIdx.x, gridDim.x);
 }
 
-// Up to kRankTokens tokens for every digit that their sort would have are sorted by one launch: a token's place is the number of tokens with a lower id, and of those with the
-// same one before it.  A work-group finds the places of 64 tokens, a token a lane; its wavefronts go over a sixteenth of all tokens
-// each, 64 of them with one load, and compare them with their own one after the other.
+// Up to kRankTokens tokens for every digit that their sort would have are sorted by one launch: a token's place is the number of
+// tokens with a lower id, and of those with the same one before it.  A work-group finds the places of 64 tokens, a token a lane; its
+// wavefronts go over a sixteenth of all tokens each, 64 of them with one load, and compare them with their own one after the other.
+// us of a backward pass with this sort / the radix sort, rows of 8 KB: 17 bits of id, accumulated 2500 tokens 23.6 / 32.8, 8192 52.8 / 55.3,
+// 12,000 67.4 / 64.0; 10 bits (rows of 4 KB) 4096 26.5 / 25.9, 6000 30.5 / 27.8.  A table that is written can be zeroed beside the launches of
+// the radix sort, which is more where it is large: 2300 and 8192 tokens, 82 MB 28.7 / 36.5 and 49.6 / 49.9, 330 MB 66 / 72 and 87.1 / 86.9, 600 MB
+// 125 / 116 and 147 / 132, 1.05 GB 199 / 180 and 229 / 199.
 static constexpr int kRankTokens = 4096;
+static constexpr long long kRankTable = 384LL << 20;  // bytes
 __global__ __launch_bounds__(1024) void k_sort_rank(const int* __restrict__ ids, int n, int vocab, int* __restrict__ keys_out, int* __restrict__ tokens_out,
                                                     int* __restrict__ where) {
     __shared__ int counts[16][64];
@@ -324,8 +329,9 @@ __global__ __launch_bounds__(256) void k_sort_place(SortPass a, ZeroRows z, cons
 
 // ---- backward: sums ----------------------------------------------------------------------
 // A wavefront takes the rows whose tokens begin among its `part` sorted tokens (at most kPart), in 64 * kVec columns, and sums
-// each to its end, also past its own tokens.  (A work-group of its own each: they end at different times.)  Only rows of more than two parts' tokens are cut: every wavefront sums those among its
-// own tokens and leaves them in fp32, [part][1] where the row begins here, [part][0] where it came from the part before.
+// each to its end, also past its own tokens.  (A work-group of its own each: they end at different times.)  Only rows of more than
+// two parts' tokens are cut: every wavefront sums those among its own tokens and leaves them in fp32, [part][1] where the row begins
+// here, [part][0] where it came from the part before.
 static constexpr int kPart = 32;
 __host__ __device__ inline int longest_whole(int part_len) { return 2 * part_len; }  // at most 64: the keys that a wavefront looks at
 
@@ -635,7 +641,8 @@ static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_by
     p.counts_a_pass = (size_t)p.sort.blocks << p.sort.digit;
     p.counts = static_cast<int*>(a.take(p.counts_a_pass * p.sort.passes * sizeof(int)));
     p.where = static_cast<int*>(a.take((size_t)vocab * sizeof(int)));
-    // parts as long as leaves 4096 wavefronts (of 512 columns)
+    // parts as long as leaves 4096 wavefronts (of 512 columns): shorter ones are more loads of keys and more cut rows, longer ones too few
+    // wavefronts for the memory; us with parts of 8 / 32, rows of 8 KB: 3000 tokens 25.7 / 36.9, 10,000 62 / 61, 70,001 249 / 207
     p.part_len = kPart;
     while (p.part_len > 8 && (long long)ceil_div(n, p.part_len) * ceil_div(hidden, 512) < 4096) p.part_len /= 2;
     p.parts = ceil_div(n, p.part_len);
@@ -669,7 +676,7 @@ static void embed_backward_launch(const EmbedPlan& p, const int* ids, const T* d
         return;
     }
     const int *keys = ids, *tokens = nullptr;
-    if (n <= kRankTokens * p.sort.passes) {
+    if (n <= kRankTokens * p.sort.passes && (accumulate || (long long)vocab * hidden * (long long)sizeof(T) <= kRankTable)) {
         k_sort_rank<<<ceil_div(n, 64), 1024, 0, stream>>>(ids, n, vocab, p.keys[0], p.tokens[0], accumulate ? nullptr : p.where);
         keys = p.keys[0];
         tokens = p.tokens[0];

@@ -111,6 +111,18 @@ def test_backward(T, H, V, kind, dtype):
     assert torch.equal(again, first)
 
 
+@pytest.mark.parametrize("T,H,V", [(2100, 256, 800000), (5000, 256, 800000), (8000, 512, 410001), (3000, 2048, 100003), (5000, 5120, 40001), (2100, 6144, 40000)])
+def test_few_tokens_of_a_large_table(T, H, V):
+    """Most of the call writes zeros: rows of every width, and not a byte behind the table."""
+    import paper_2503_01066_amd as A
+    ids, dX = make_ids("mixed", T, V, 3), randn((T, H), "bf16", 4)
+    ids[:700] = V - 1  # the last row, over many parts
+    memory = torch.full((V + 1, H), 3.0, dtype=torch.bfloat16, device="cuda")
+    dW = A.alch_embed_backward(torch.from_numpy(ids).cuda(), dX.cuda(), V, scale=0.5, dW_embed=memory[:V])
+    check_backward(ids, dX, V, 0.5, dW, None)
+    assert bool((memory[V] == 3).all())
+
+
 def test_backward_without_tokens_writes_zeros():
     import paper_2503_01066_amd as A
     dW = torch.full((37, 24), 5.0, device="cuda")
