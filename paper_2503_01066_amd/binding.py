@@ -120,12 +120,12 @@ def library_path():
 
 
 _LIB = None
-_PACK = 0  # address of alch_capture_pack
+_PACK = _EMBED = 0  # addresses of alch_capture_pack and alch_embed_forward
 
 
 def lib():
     """Loads libalch.so (built by paper_2503_01066_amd.build); raises if it is missing."""
-    global _LIB, _PACK
+    global _LIB, _PACK, _EMBED
     if _LIB is not None:
         return _LIB
     path = library_path()
@@ -217,6 +217,7 @@ def lib():
     L.alch_trace_enable.argtypes = [C.c_int32]
     L.alch_trace_collect.argtypes = [C.POINTER(CTraceRecord), C.c_int32, C.POINTER(C.c_int32)]
     _PACK = C.cast(L.alch_capture_pack, C.c_void_p).value
+    _EMBED = C.cast(L.alch_embed_forward, C.c_void_p).value
     _LIB = L
     return L
 
@@ -667,6 +668,11 @@ def _place(device, stream):
     return _raw_stream(at) if stream is None and _raw_stream is not None else _stream_handle(stream)
 
 
+def _check_counts(n_tokens, vocab):
+    if n_tokens > 0x7fffffff or vocab > 0x7fffffff:
+        raise ValueError("%d tokens, a table of %d rows: more than 2^31 - 1" % (n_tokens, vocab))
+
+
 def _empty(shape, dtype, device, stream, fill=torch.empty):
     """Memory of the stream that the call goes to: what was freed on another one may still be in use there, and what is freed
     behind the call is not handed out elsewhere while it runs."""
@@ -677,13 +683,23 @@ def _empty(shape, dtype, device, stream, fill=torch.empty):
 
 
 def embed_backward_workspace_bytes(dtype, vocab, hidden, n_tokens):
+    _check_counts(n_tokens, vocab)
     return lib().alch_embed_backward_workspace_bytes(_code(dtype), vocab, hidden, n_tokens)
 
 
 def alch_embed_forward(token_ids, W_embed, scale=1.0, X=None, stream=None):
     """Returns X [n_tokens, hidden], X[t] = scale * W_embed[token_ids[t]] (token_ids int32 [n_tokens]; a zero row where the id
     is no row of W_embed [vocab, hidden])."""
+    if _marshal is not None and stream is None and _raw_stream is not None and token_ids.is_cuda:
+        lib()
+        at = torch.cuda.current_device()
+        out = _marshal.embed_forward(_EMBED, token_ids, W_embed, scale, X, at, _raw_stream(at))
+        if out is not None:
+            if out[0] != 0:
+                _check(out[0])
+            return out[1]
     (vocab, hidden), (n,), dev, dt = W_embed.shape, token_ids.shape, W_embed.get_device(), W_embed.dtype
+    _check_counts(n, vocab)
     handle = _place(dev, stream)
     _check_dense(token_ids, "token_ids", torch.int32, dev)
     _check_dense(W_embed, "W_embed", dt, dev)
@@ -702,6 +718,7 @@ def alch_embed_backward(token_ids, dX, vocab, scale=1.0, dW_embed=None, accumula
     dW_embed, of which only the rows that occur are touched (the gradient of a head that shares the table, for one)."""
     L = lib()
     (n, hidden), (n_ids,), dev, dt = dX.shape, token_ids.shape, dX.get_device(), dX.dtype
+    _check_counts(n, vocab)
     handle = _place(dev, stream)
     _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
     _check_dense(dX, "dX", dt, dev)

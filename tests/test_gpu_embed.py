@@ -223,3 +223,53 @@ def test_gradient_against_differences():
     measured, formula = (f(W + h * E) - f(W)) / h, (dW.double() * E.double()).sum()
     # X and X(W + hE) are rounded twice (2^-24 of at most ~5 * 3 each), 33600 products with |R| ~ 1, over h: about 1e-4 of ~ 540
     assert abs(float(measured - formula)) <= 2.0 ** -23 * 2 / h * float((A.alch_embed_forward(dev, W.abs() + h * E.abs(), scale=scale) * R.abs()).double().sum()) + 1e-9
+
+
+FORMS = ["plain", "fp32", "X", "no tokens", "whole scale", "64-bit ids", "ids of two dims", "spaced ids", "host ids", "host table", "half table", "table by columns",
+         "X too short", "X of another type", "X by columns", "X on the host", "X off 16 bytes", "no table", "tensor scale", "another stream", "stream given"]
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_rows_marshalled_by_the_extension_and_in_python(monkeypatch, form):
+    import paper_2503_01066_amd as A
+    from paper_2503_01066_amd import binding
+    assert binding._marshal is not None
+    T, V, H = 5, 40, 64
+    ids, W = torch.from_numpy(make_ids("mixed", T, V)).cuda(), randn((V, H), "bf16", 2).cuda()
+    X, scale, stream, out = None, 0.75, None, []
+    if form == "fp32": W = W.float()
+    if form.startswith("X"): X = torch.full((T + 1, H), 9.0, dtype=W.dtype, device="cuda")[:T]
+    if form == "no tokens": ids = ids[:0]
+    if form == "whole scale": scale = 3
+    if form == "64-bit ids": ids = ids.long()
+    if form == "ids of two dims": ids = ids[None]
+    if form == "spaced ids": ids = torch.stack([ids, ids], 1)[:, 0]
+    if form == "host ids": ids = ids.cpu()
+    if form == "host table": W = W.cpu()
+    if form == "half table": W = W.half()
+    if form == "table by columns": W = W.t().contiguous().t()
+    if form == "X too short": X = X[:T - 1]
+    if form == "X of another type": X = X.float()
+    if form == "X by columns": X = X.t().contiguous().t()
+    if form == "X on the host": X = X.cpu()
+    if form == "X off 16 bytes": X = torch.zeros(T * H + 1, dtype=W.dtype, device="cuda")[1:].view(T, H)
+    if form == "no table": W = None
+    if form == "tensor scale": scale = torch.tensor(0.75)
+    if form == "stream given": stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for ext in (binding._marshal, None):
+        monkeypatch.setattr(binding, "_marshal", ext)
+        try:
+            with torch.cuda.stream(torch.cuda.Stream() if form == "another stream" else None):
+                got = A.alch_embed_forward(ids, W, scale=scale, X=X, stream=stream)
+            torch.cuda.synchronize()
+            out.append((got is X, got.dtype, got.tolist()))
+        except Exception as e:  # noqa: BLE001 (compared below)
+            out.append((type(e), str(e)))
+    assert out[0] == out[1]
+    fine = form in ("plain", "fp32", "X", "no tokens", "whole scale", "tensor scale", "another stream", "stream given")
+    assert isinstance(out[0][0], bool) == fine
+    if fine and form != "no tokens":
+        ok = (ids >= 0) & (ids < V)
+        want = torch.where(ok[:, None], (W[ids.long().clamp(0, V - 1)].float() * float(scale)).to(W.dtype), torch.zeros((), dtype=W.dtype, device="cuda"))
+        assert out[0][2] == want.tolist()

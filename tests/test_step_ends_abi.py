@@ -165,3 +165,14 @@ def test_calls_refuse_tensors_that_are_not_on_the_current_device():
                  lambda: A.alch_adamw_step(A.AdamwList([W], [W.clone()], [W.clone()], [W.clone()]), 1e-3)):
         with pytest.raises(ValueError, match="cpu"):
             call()
+
+
+def test_counts_beyond_32_bits_are_refused():
+    """The library takes 32 bits: a count that a conversion would cut to a small one is refused in front of it."""
+    import torch
+    ids, many = torch.zeros(3, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).expand(2 ** 32 + 3)
+    for call in (lambda: A.alch_embed_forward(many, torch.zeros(4, 8)), lambda: A.alch_embed_backward(ids, torch.zeros(3, 8), 2 ** 32 + 4),
+                 lambda: A.alch_embed_backward(many, torch.zeros(1, 1).expand(2 ** 32 + 3, 1), 4),
+                 lambda: A.embed_backward_workspace_bytes(torch.float32, 2 ** 32 + 4, 8, 3), lambda: A.embed_backward_workspace_bytes(torch.float32, 4, 8, 2 ** 31)):
+        with pytest.raises(ValueError, match="more than 2.31 - 1"):
+            call()
