@@ -439,6 +439,7 @@ int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batc
  * The two ends of a training step: the embedding rows in front of layer 0 (Section 4.1: the prefill starts
  * from the token ids), their gradient behind dX_embed, and what is done with the gradients (Section 3: the
  * weights are updated every iteration while they serve).
+ * Memory that a call writes, its workspace included, may not overlap other memory of the call, except where it says so.
  */
 
 /*
@@ -470,8 +471,7 @@ size_t alch_embed_backward_workspace_bytes(alch_dtype dtype, int32_t vocab, int3
 /* The tensors of the two calls below come as a table that the caller makes once, for as long as they stay where they
  * are: a device array that the kernels read, and a host copy of the same values for validation and launch planning.
  * Tensors are dense, of any number of elements (0 too: pointers may be NULL then), 2^40 elements in all, at most
- * ALCH_MAX_TENSORS of them, each of its own type.  Memory that a call writes may not overlap other memory of the call,
- * except where it says so. */
+ * ALCH_MAX_TENSORS of them, each of its own type. */
 #define ALCH_MAX_TENSORS 4096
 
 typedef struct {

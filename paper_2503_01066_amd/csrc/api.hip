@@ -1443,6 +1443,7 @@ int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t 
     REQUIRE_PTR(W_embed, "W_embed"); REQUIRE_PTR(X, "X");
     const unsigned long long row = (unsigned long long)hidden * dtype_size(dtype);
     if (overlap(X, n_tokens * row, W_embed, vocab * row)) return fail(ALCH_ERR_INVALID_ARG, "X overlaps W_embed");
+    if (overlap(X, n_tokens * row, token_ids, 4ull * n_tokens)) return fail(ALCH_ERR_INVALID_ARG, "X overlaps token_ids");
     return launch_embed(dtype, token_ids, W_embed, X, n_tokens, vocab, hidden, scale, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -1466,6 +1467,12 @@ int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t
     const size_t need = embed_backward_workspace_bytes(vocab, hidden, n_tokens);
     if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
     if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+    if (overlap(workspace, need, dW_embed, vocab * row)) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps dW_embed");
+    if (n_tokens > 0) {
+        if (overlap(workspace, need, dX, n_tokens * row)) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps dX");
+        if (overlap(workspace, need, token_ids, 4ull * n_tokens)) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps token_ids");
+        if (overlap(dW_embed, vocab * row, token_ids, 4ull * n_tokens)) return fail(ALCH_ERR_INVALID_ARG, "dW_embed overlaps token_ids");
+    }
     return launch_embed_backward(dtype, token_ids, dX, n_tokens, vocab, hidden, scale, accumulate != 0, dW_embed, workspace, workspace_bytes,
                                  static_cast<hipStream_t>(hip_stream));
 }
@@ -1490,6 +1497,7 @@ int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alc
     const size_t need = grad_clip_workspace_bytes();
     if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
     if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+    if (overlap(workspace, need, norm_out, 2 * sizeof(float))) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps norm_out");
     return launch_grad_clip(n_tensors, tensors, tensors_host, max_norm, norm_out, workspace, static_cast<hipStream_t>(hip_stream));
 }
 

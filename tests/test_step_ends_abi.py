@@ -176,3 +176,19 @@ def test_counts_beyond_32_bits_are_refused():
                  lambda: A.embed_backward_workspace_bytes(torch.float32, 2 ** 32 + 4, 8, 3), lambda: A.embed_backward_workspace_bytes(torch.float32, 4, 8, 2 ** 31)):
         with pytest.raises(ValueError, match="more than 2.31 - 1"):
             call()
+
+
+def test_scratch_and_ids_that_outputs_share_are_refused():
+    """Sorted tokens that something else writes over would be followed to wherever they point."""
+    L, far = A.lib(), 1 << 40
+    need = L.alch_embed_backward_workspace_bytes(1, 100, 64, 5)
+    call = lambda ids=far, dX=2 * far, dW=3 * far, ws=4 * far, acc=0: L.alch_embed_backward(1, 100, 64, 5, ids, dX, 1.0, dW, acc, ws, need, None)
+    for acc in (0, 1):
+        assert call(ws=3 * far + 99 * 128, acc=acc) == INVALID and "workspace overlaps dW_embed" in _err()
+        assert call(ws=2 * far + 4 * 128, acc=acc) == INVALID and "workspace overlaps dX" in _err()
+        assert call(ids=4 * far + need - 4, acc=acc) == INVALID and "workspace overlaps token_ids" in _err()
+        assert call(ids=3 * far - 16, acc=acc) == INVALID and "dW_embed overlaps token_ids" in _err()
+    assert L.alch_embed_backward(1, 100, 64, 0, None, None, 1.0, far, 0, far, need, None) == INVALID and "workspace overlaps dW_embed" in _err()
+    assert L.alch_embed_forward(1, 100, 64, 5, far + 4 * 128 + 124, 2 * far, 1.0, far, None) == INVALID and "X overlaps token_ids" in _err()
+    rows, size = _grads((far, None, 64, 1, 0)), L.alch_grad_clip_workspace_bytes()
+    assert L.alch_grad_clip(1, P, C.addressof(rows), 1.0, 2 * far + size - 4, 2 * far, size, None) == INVALID and "workspace overlaps norm_out" in _err()
