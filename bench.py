@@ -359,7 +359,8 @@ def with_update(args, torch, A, backward, Ws, loras, lora_grads, base_grads, emb
         raise SystemExit("--update: nothing is trained (--frozen-base needs --lora-rank)")
     masters = [p.float() for p in params]
     zeros = lambda: [torch.zeros_like(w) for w in masters]
-    clip, tensors = A.GradList(grads, grads), A.AdamwList(params, grads, zeros(), zeros(), masters=masters, weight_decay=0.1)
+    # (measured only: the update multiplies with the factor, so that the gradients are neither written nor scaled twice)
+    clip, tensors = A.GradList(grads), A.AdamwList(params, grads, zeros(), zeros(), masters=masters, weight_decay=0.1)
     norm, ws = torch.empty(2, device=emb.device), torch.empty(A.grad_clip_workspace_bytes(), dtype=torch.uint8, device=emb.device)
 
     def step(xf, rs, hooks=None):

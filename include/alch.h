@@ -486,7 +486,7 @@ typedef struct {
  * alch_grad_clip: the 2-norm over all elements of all tensors, and the gradients scaled so that it does not exceed max_norm:
  *   norm = sqrt(sum g^2);  factor = max_norm / norm where norm > max_norm, else 1;  out = factor * grad
  * A norm that is no finite number (an infinity or NaN among the gradients) gives factor NaN: clipped gradients are NaN
- * then, and alch_adamw_step leaves everything as it was.  The sum is held in 64 bits: finite gradients of any size have
+ * then, and alch_adamw_step that is given this factor leaves everything as it was.  The sum is held in 64 bits: finite gradients of any size have
  * a finite sum (the norm is rounded to fp32 when it is written).
  *   max_norm   >= 0; an infinity only measures
  *   norm_out   device float [2] out: { norm, factor }, 4-byte aligned
@@ -512,7 +512,8 @@ typedef struct {
     int32_t step;             /* of this update, the first one is 1 */
     const float* schedule;    /* device float [2] or NULL: { lr, step } in place of the two above, read when the kernel runs, so that
                                  a captured step can be replayed with other values; a step below 1 is none: nothing is written */
-    const float* grad_factor; /* device float [1] or NULL: multiplies every gradient (norm_out + 1 of alch_grad_clip) */
+    const float* grad_factor; /* device float [1] or NULL: multiplies every gradient.  norm_out + 1 of alch_grad_clip where that call only
+                                 measured them (out NULL); gradients that it has clipped are not to be multiplied again */
 } alch_adamw;
 
 /*

@@ -821,8 +821,9 @@ def grad_clip_workspace_bytes():
 
 
 def alch_grad_clip(grads, max_norm, norm_out=None, workspace=None, stream=None):
-    """grads: a GradList.  Returns the device float tensor [2] {norm over all gradients, factor they were multiplied with};
-    norm_out[1:] is the grad_factor of alch_adamw_step."""
+    """grads: a GradList.  Returns the device float tensor [2] {norm over all gradients, clipping factor}.  The factor is applied
+    once: here, to the gradients that the list has outs for (alch_adamw_step on these takes no grad_factor), or by alch_adamw_step with
+    grad_factor=norm_out[1:] on gradients that were only measured, which saves a pass over them."""
     L = lib()
     dev = grads.index
     handle = _place(dev, stream)
