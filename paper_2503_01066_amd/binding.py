@@ -738,7 +738,8 @@ def alch_embed_backward(token_ids, dX, vocab, scale=1.0, dW_embed=None, accumula
 
 class _TensorTable:
     """Pointers and lengths of many tensors: a host array for the library's checks, the same on the device for its kernels,
-    uploaded once.  Keeps the tensors, which must stay where they are."""
+    uploaded once.  Keeps the tensors, which must stay where they are.  A captured call reads the table at every replay: a list lives as
+    long as the graphs that hold calls with it."""
 
     def __init__(self, row, first, device):
         self.row, self.rows, self.ranges, self.keep = row, [], [], []
@@ -770,11 +771,14 @@ class _TensorTable:
         self.host_ptr = C.addressof(self.host)
         self.dev = torch.frombuffer(bytearray(self.host), dtype=torch.uint8).to(self.device)
         self.dev_ptr = self.dev.data_ptr()
+        self.made_on = None if self.index < 0 else torch.cuda.current_stream(self.device).cuda_stream
         del self.rows, self.ranges
 
-    def _used(self, stream):
-        if stream is not None:  # (the table may be dropped behind the call: its memory is not handed out before the call has run)
-            self.dev.record_stream(stream)
+    def _used(self, stream, handle):
+        """Before a call on a stream (None: the current one; its handle): the table may be dropped behind the call, and its memory is not
+        handed out before the call has run."""
+        if handle != self.made_on:
+            self.dev.record_stream(torch.cuda.current_stream() if stream is None else stream)
 
 
 class GradList(_TensorTable):
@@ -835,7 +839,7 @@ def alch_grad_clip(grads, max_norm, norm_out=None, workspace=None, stream=None):
         workspace = _empty((L.alch_grad_clip_workspace_bytes(),), torch.uint8, grads.device, stream)
     else:
         _check_dense(workspace, "workspace", torch.uint8, dev)
-    grads._used(stream)
+    grads._used(stream, handle)
     _check(L.alch_grad_clip(grads.n, grads.dev_ptr, grads.host_ptr, max_norm, norm_out.data_ptr(), workspace.data_ptr(), workspace.numel(), handle))
     return norm_out
 
@@ -851,7 +855,7 @@ def alch_adamw_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, sched
     if grad_factor is not None:
         _check_dense(grad_factor, "grad_factor", torch.float32, dev, (1,))
     p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
-    tensors._used(stream)
+    tensors._used(stream, handle)
     _check(lib().alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), handle))
 
 
