@@ -43,3 +43,25 @@ def test_a_list_is_kept_for_the_stream_that_a_call_goes_to(monkeypatch, call):
         tensors.dev.streams, current.cuda_stream = [], at
         run(stream)
         assert tensors.dev.streams == kept, (at, stream)
+
+
+def test_hidden_sizes_beyond_32_bits_are_refused():
+    """They would be cut to a small one, which has a workspace and rows of its own."""
+    ids, wide = torch.zeros(3, dtype=torch.int32), torch.zeros(1, 1)
+    for call in (lambda: A.alch_embed_forward(ids, wide.expand(4, 2 ** 32 + 8)), lambda: A.alch_embed_backward(ids, wide.expand(3, 2 ** 32 + 8), 4),
+                 lambda: A.embed_backward_workspace_bytes(torch.float32, 4, 2 ** 32 + 8, 3),
+                 lambda: A.embed_backward_workspace_bytes(torch.float32, 8 - 2 ** 32, 8, 3)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+
+
+def test_steps_beyond_32_bits_are_refused(monkeypatch):
+    z = lambda: torch.zeros(8)
+    tensors, steps = A.AdamwList([z()], [z()], [z()], [z()]), []
+    monkeypatch.setattr(B, "lib", lambda: SimpleNamespace(alch_adamw_step=lambda n, d, h, p, s: steps.append(p._obj.step) or 0))
+    monkeypatch.setattr(B, "_place", lambda device, stream: tensors.made_on)
+    for step in (2 ** 32 + 1, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="32 bits"):
+            A.alch_adamw_step(tensors, 1e-3, step=step)
+    A.alch_adamw_step(tensors, 1e-3, step=2 ** 31 - 1)
+    assert steps == [2 ** 31 - 1]
