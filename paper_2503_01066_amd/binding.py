@@ -668,11 +668,11 @@ def _place(device, stream):
     return _raw_stream(at) if stream is None and _raw_stream is not None else _stream_handle(stream)
 
 
-def _check_int32(**counts):
-    """The library takes 32 bits: what does not fit would be cut to another number on the way."""
-    for name, n in counts.items():
-        if not -0x80000000 <= n <= 0x7fffffff:
-            raise ValueError("%s = %d: more than 2^31 - 1, or otherwise no number of 32 bits" % (name, n))
+def _check_int32(what, a, b=0, c=0):
+    """The library takes 32 bits: what does not fit would be cut to another number on the way.  what: the numbers' names."""
+    if -0x80000000 <= a <= 0x7fffffff and -0x80000000 <= b <= 0x7fffffff and -0x80000000 <= c <= 0x7fffffff:
+        return
+    raise ValueError("%s = %s: more than 2^31 - 1, or otherwise no numbers of 32 bits" % (what, (a, b, c)[:what.count(",") + 1]))
 
 
 def _empty(shape, dtype, device, stream, fill=torch.empty):
@@ -685,7 +685,7 @@ def _empty(shape, dtype, device, stream, fill=torch.empty):
 
 
 def embed_backward_workspace_bytes(dtype, vocab, hidden, n_tokens):
-    _check_int32(n_tokens=n_tokens, vocab=vocab, hidden=hidden)
+    _check_int32("n_tokens, vocab, hidden", n_tokens, vocab, hidden)
     return lib().alch_embed_backward_workspace_bytes(_code(dtype), vocab, hidden, n_tokens)
 
 
@@ -701,7 +701,7 @@ def alch_embed_forward(token_ids, W_embed, scale=1.0, X=None, stream=None):
                 _check(out[0])
             return out[1]
     (vocab, hidden), (n,), dev, dt = W_embed.shape, token_ids.shape, W_embed.get_device(), W_embed.dtype
-    _check_int32(n_tokens=n, vocab=vocab, hidden=hidden)
+    _check_int32("n_tokens, vocab, hidden", n, vocab, hidden)
     handle = _place(dev, stream)
     _check_dense(token_ids, "token_ids", torch.int32, dev)
     _check_dense(W_embed, "W_embed", dt, dev)
@@ -720,7 +720,7 @@ def alch_embed_backward(token_ids, dX, vocab, scale=1.0, dW_embed=None, accumula
     dW_embed, of which only the rows that occur are touched (the gradient of a head that shares the table, for one)."""
     L = lib()
     (n, hidden), (n_ids,), dev, dt = dX.shape, token_ids.shape, dX.get_device(), dX.dtype
-    _check_int32(n_tokens=n, vocab=vocab, hidden=hidden)
+    _check_int32("n_tokens, vocab, hidden", n, vocab, hidden)
     handle = _place(dev, stream)
     _check_dense(token_ids, "token_ids", torch.int32, dev, (n,))
     _check_dense(dX, "dX", dt, dev)
@@ -856,7 +856,7 @@ def alch_adamw_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, sched
         _check_dense(schedule, "schedule", torch.float32, dev, (2,))
     if grad_factor is not None:
         _check_dense(grad_factor, "grad_factor", torch.float32, dev, (1,))
-    _check_int32(step=step)
+    _check_int32("step", step)
     p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
     tensors._used(stream, handle)
     _check(lib().alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), handle))
