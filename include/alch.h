@@ -459,8 +459,9 @@ int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t 
  *   dW_embed   [vocab, hidden] out.  accumulate == 0: every row is written, zeros where no token has the id.
  *              accumulate != 0: only rows of ids that occur are read and written (sum in fp32, one rounding), for
  *              micro-batches and for a table shared with the head, whose dW_lm it may be.
- *   workspace  alch_embed_backward_workspace_bytes() bytes, 16-byte aligned; what it holds is not read.  As everywhere, two calls
- *              that may run at the same time need one each.
+ *   workspace  alch_embed_backward_workspace_bytes() bytes, 16-byte aligned; what it holds makes no difference.  As everywhere, two
+ *              calls that may run at the same time need one each.  The size never falls with n_tokens: a workspace for the largest batch
+ *              serves all others of the same table.
  * Sums are in fp32, in an order that the token ids alone determine: results repeat bit for bit.
  */
 int alch_embed_backward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids,

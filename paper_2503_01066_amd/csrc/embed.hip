@@ -332,7 +332,7 @@ __global__ __launch_bounds__(256) void k_sort_place(SortPass a, ZeroRows z, cons
 // each to its end, also past its own tokens.  (A work-group of its own each: they end at different times.)  Only rows of more than
 // two parts' tokens are cut: every wavefront sums those among its own tokens and leaves them in fp32, [part][1] where the row begins
 // here, [part][0] where it came from the part before.
-static constexpr int kPart = 32;
+static constexpr int kPart = 32, kPartMin = 8;
 __host__ __device__ inline int longest_whole(int part_len) { return 2 * part_len; }  // at most 64: the keys that a wavefront looks at
 
 template <typename T, int kVec, typename V>
@@ -629,6 +629,8 @@ struct EmbedPlan {
     int part_len, parts, stride;
     size_t counts_a_pass, bytes;
 };
+// A workspace for n tokens serves every smaller batch too: blocks of the sort and parts are longer, and therefore fewer, behind some n,
+// so that room is taken for the most that any batch of up to n tokens has.
 static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_bytes) {
     Arena a(ws, ws_bytes);
     EmbedPlan p;
@@ -639,16 +641,21 @@ static EmbedPlan plan_embed(int vocab, int hidden, int n, void* ws, size_t ws_by
         p.tokens[i] = static_cast<int*>(a.take((size_t)n * sizeof(int)));
     }
     p.counts_a_pass = (size_t)p.sort.blocks << p.sort.digit;
-    p.counts = static_cast<int*>(a.take(p.counts_a_pass * p.sort.passes * sizeof(int)));
+    const size_t most_blocks = std::min(ceil_div(n, kSortBlockMin), kSortBlocks);
+    p.counts = static_cast<int*>(a.take((most_blocks << p.sort.digit) * p.sort.passes * sizeof(int)));
     p.where = static_cast<int*>(a.take((size_t)vocab * sizeof(int)));
     // parts as long as leaves 4096 wavefronts (of 512 columns): shorter ones are more loads of keys and more cut rows, longer ones too few
     // wavefronts for the memory; us with parts of 8 / 32, rows of 8 KB: 3000 tokens 25.7 / 36.9, 10,000 62 / 61, 70,001 249 / 207
+    constexpr int kWavefronts = 4096;
+    const int tiles = ceil_div(hidden, 512);
     p.part_len = kPart;
-    while (p.part_len > 8 && (long long)ceil_div(n, p.part_len) * ceil_div(hidden, 512) < 4096) p.part_len /= 2;
+    while (p.part_len > kPartMin && (long long)ceil_div(n, p.part_len) * tiles < kWavefronts) p.part_len /= 2;
     p.parts = ceil_div(n, p.part_len);
-    p.cut = static_cast<int*>(a.take((size_t)p.parts * sizeof(int)));
+    // (parts shorter than kPart are taken where there are fewer than kWavefronts / tiles of twice their length)
+    const size_t most_parts = std::max(ceil_div(n, kPart), std::min(ceil_div(n, kPartMin), 2 * ((kWavefronts - 1) / tiles)));
+    p.cut = static_cast<int*>(a.take(most_parts * sizeof(int)));
     p.stride = (int)round_up((size_t)hidden, 8);
-    p.partial = static_cast<float*>(a.take((size_t)p.parts * 2 * p.stride * sizeof(float)));
+    p.partial = static_cast<float*>(a.take(most_parts * 2 * p.stride * sizeof(float)));
     p.bytes = round_up(a.used, 256);
     return p;
 }

@@ -65,3 +65,21 @@ def test_steps_beyond_32_bits_are_refused(monkeypatch):
             A.alch_adamw_step(tensors, 1e-3, step=step)
     A.alch_adamw_step(tensors, 1e-3, step=2 ** 31 - 1)
     assert steps == [2 ** 31 - 1]
+
+
+@pytest.mark.parametrize("hidden", [1, 8, 256, 487, 512, 513, 4096, 8192, 8200, 20000, 1 << 17, 1 << 20])
+@pytest.mark.parametrize("vocab", [1, 1000, 1023, 128256, 2 ** 20])
+def test_a_workspace_for_a_batch_serves_every_smaller_one(hidden, vocab):
+    """A program sizes it once, for its largest batch: the size never falls with the number of tokens, over all lengths of parts and blocks."""
+    tiles = -(-hidden // 512)
+    at = {0, 1, 2, 511, 512, 513}
+    for part in (8, 16, 32):  # parts of a length end where 4096 wavefronts have their own
+        at |= {part * k + d for k in (4095 // tiles, 4096 // tiles, -(-4096 // tiles)) for d in (-1, 0, 1)}
+    for blocks in (512,):     # blocks of the sort become longer
+        at |= {blocks * size + d for size in (512, 768, 1024, 1280) for d in (-1, 0, 1)}
+    at |= {1 << k for k in range(31)} | {(1 << k) - 24 for k in range(6, 31)} | {8176, 8192, 16000, 16352, 16384}
+    at = sorted(n for n in at if n >= 0 and n * hidden <= 1 << 40)
+    for dtype in (torch.bfloat16, torch.float32):
+        sizes = [A.embed_backward_workspace_bytes(dtype, vocab, hidden, n) for n in at]
+        falls = [(n, m) for n, m, a, b in zip(at, at[1:], sizes, sizes[1:]) if b < a]
+        assert not falls and sizes[0] > 0
