@@ -439,7 +439,10 @@ int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batc
  * The two ends of a training step: the embedding rows in front of layer 0 (Section 4.1: the prefill starts
  * from the token ids), their gradient behind dX_embed, and what is done with the gradients (Section 3: the
  * weights are updated every iteration while they serve).
- * Memory that a call writes, its workspace included, may not overlap other memory of the call, except where it says so.
+ * Memory that a call writes, its workspace included, may not overlap other memory of the call, except where it says so.  That is
+ * refused where it is seen at once: all of it for the embedding rows; for the tables of tensors what else a call takes (workspace,
+ * norm_out, schedule, grad_factor, the table itself) against every tensor, and a tensor's out against its grad.  Tensors are not
+ * compared with one another.
  */
 
 /*

@@ -1428,6 +1428,32 @@ static bool overlap(const void* a, unsigned long long a_bytes, const void* b, un
     return x < y ? y - x < a_bytes : x - y < b_bytes;
 }
 
+// What a call takes beside its tensors (p NULL: not given), none of which may share memory with theirs.
+struct Beside {
+    struct Memory {
+        const void* p;
+        unsigned long long bytes;
+        const char* name;
+    };
+    Memory of[3];
+    uintptr_t low = ~(uintptr_t)0, high = 0;  // of all three
+    Beside(Memory a, Memory b, Memory c) : of{a, b, c} {
+        for (const Memory& m : of)
+            if (m.p) {
+                low = std::min(low, reinterpret_cast<uintptr_t>(m.p));
+                high = std::max(high, reinterpret_cast<uintptr_t>(m.p) + (uintptr_t)m.bytes);
+            }
+    }
+    // memory of tensor i.  (Hundreds of tensors are looked at, most of them outside that span: 1 ns each, 4 inside)
+    int apart(int i, const void* p, unsigned long long bytes, const char* name) const {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (!p || at >= high || at + bytes <= low) return ALCH_OK;
+        for (const Memory& m : of)
+            if (m.p && overlap(m.p, m.bytes, p, bytes)) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: %s overlaps %s", i, m.name, name);
+        return ALCH_OK;
+    }
+};
+
 #define REQUIRE_WORDS(p, name)                                                                                                \
     do {                                                                                                                      \
         if (!(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is NULL", name);                                                      \
@@ -1498,6 +1524,19 @@ int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alc
     if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
     if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
     if (overlap(workspace, need, norm_out, 2 * sizeof(float))) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps norm_out");
+    // (the sums of the norm are read by every work-group, beside others that write clipped values, and the table by all of them)
+    const unsigned long long table = (unsigned long long)n_tensors * sizeof(*tensors);
+    const Beside::Memory scratch{workspace, need, "workspace"}, result{norm_out, 2 * sizeof(float), "norm_out"};
+    const Beside written(scratch, result, {}), all(scratch, result, {tensors, table, "tensors"});
+    if (n_tensors > 0 && overlap(workspace, need, tensors, table)) return fail(ALCH_ERR_INVALID_ARG, "workspace overlaps tensors");
+    if (n_tensors > 0 && overlap(norm_out, 2 * sizeof(float), tensors, table)) return fail(ALCH_ERR_INVALID_ARG, "norm_out overlaps tensors");
+    for (int i = 0; i < n_tensors; ++i) {
+        const alch_grad_tensor& t = tensors_host[i];
+        if (t.n == 0) continue;
+        const unsigned long long bytes = (unsigned long long)t.n * dtype_size((alch_dtype)t.dtype);
+        ALCH_TRY(all.apart(i, t.out, bytes, "out"));
+        ALCH_TRY(written.apart(i, t.grad, bytes, "grad"));
+    }
     return launch_grad_clip(n_tensors, tensors, tensors_host, max_norm, norm_out, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -1519,6 +1558,18 @@ int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const a
         ALCH_TRY(check_tensor_ptr(t.m, i, "m"));
         ALCH_TRY(check_tensor_ptr(t.v, i, "v"));
         if (t.master) ALCH_TRY(check_tensor_ptr(t.master, i, "master"));
+    }
+    // (read by every work-group, beside others that write)
+    const Beside read({p->schedule, 2 * sizeof(float), "schedule"}, {p->grad_factor, sizeof(float), "grad_factor"},
+                      {tensors, (unsigned long long)n_tensors * sizeof(*tensors), "tensors"});
+    for (int i = 0; i < n_tensors; ++i) {
+        const alch_adamw_tensor& t = tensors_host[i];
+        if (t.n == 0) continue;
+        const unsigned long long f32 = 4ull * t.n;
+        ALCH_TRY(read.apart(i, t.param, (unsigned long long)t.n * dtype_size((alch_dtype)t.dtype), "param"));
+        ALCH_TRY(read.apart(i, t.master, f32, "master"));
+        ALCH_TRY(read.apart(i, t.m, f32, "m"));
+        ALCH_TRY(read.apart(i, t.v, f32, "v"));
     }
     return launch_adamw(n_tensors, tensors, tensors_host, *p, static_cast<hipStream_t>(hip_stream));
 }

@@ -83,3 +83,51 @@ def test_a_workspace_for_a_batch_serves_every_smaller_one(hidden, vocab):
         sizes = [A.embed_backward_workspace_bytes(dtype, vocab, hidden, n) for n in at]
         falls = [(n, m) for n, m, a, b in zip(at, at[1:], sizes, sizes[1:]) if b < a]
         assert not falls and sizes[0] > 0
+
+
+FAR = 1 << 40  # (addresses that are compared, never followed)
+INVALID = -1
+
+
+def _err():
+    return A.lib().alch_last_error().decode()
+
+
+def test_clipping_refuses_scratch_and_results_inside_its_gradients():
+    """Work-groups read the sums for themselves while others store clipped values already."""
+    L = A.lib()
+    need = L.alch_grad_clip_workspace_bytes()
+
+    def call(norm_out=3 * FAR, ws=4 * FAR, rows=((FAR, None, 0, 1, 0), (FAR, 2 * FAR, 1000, 1, 0), (FAR + 4096, None, 1000, 0, 0)), dev=64):
+        h = (B.GradTensor * len(rows))(*[B.GradTensor(*r) for r in rows])
+        return L.alch_grad_clip(len(rows), dev, C.addressof(h), 1.0, norm_out, ws, need, None)
+
+    for at in (2 * FAR, 2 * FAR + 1984, 2 * FAR - need + 16):
+        assert call(ws=at) == INVALID and "tensor 1: workspace overlaps out" in _err()
+    assert call(ws=FAR + 1984) == INVALID and "tensor 1: workspace overlaps grad" in _err()
+    assert call(ws=FAR + 4096 + 3984) == INVALID and "tensor 2: workspace overlaps grad" in _err()
+    assert call(norm_out=2 * FAR + 1996) == INVALID and "tensor 1: norm_out overlaps out" in _err()
+    assert call(norm_out=FAR - 4) == INVALID and "tensor 1: norm_out overlaps grad" in _err()
+    assert call(norm_out=FAR + 8092) == INVALID and "tensor 2: norm_out overlaps grad" in _err()
+    # the table, which all work-groups read
+    assert call(dev=4 * FAR + need - 8) == INVALID and "workspace overlaps tensors" in _err()
+    assert call(dev=3 * FAR - 88) == INVALID and "norm_out overlaps tensors" in _err()
+    assert call(dev=2 * FAR + 1992) == INVALID and "tensor 1: tensors overlaps out" in _err()
+
+
+def test_the_update_refuses_a_factor_or_schedule_inside_what_it_writes():
+    L = A.lib()
+    good = dict(param=FAR, grad=2 * FAR, master=3 * FAR, m=4 * FAR, v=5 * FAR, n=1000, weight_decay=0.0, dtype=1)
+
+    def call(dev=64, **kw):
+        rows = [B.AdamwTensor(**dict(good, n=0)), B.AdamwTensor(**good)]
+        h = (B.AdamwTensor * 2)(*rows)
+        p = B.CAdamw(**dict(dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1), **kw))
+        return L.alch_adamw_step(2, dev, C.addressof(h), C.byref(p), None)
+
+    for name, at, size in (("param", FAR, 2000), ("master", 3 * FAR, 4000), ("m", 4 * FAR, 4000), ("v", 5 * FAR, 4000)):
+        for inside in (at, at + size - 4):
+            assert call(grad_factor=inside) == INVALID and "tensor 1: grad_factor overlaps %s" % name in _err()
+            assert call(schedule=inside) == INVALID and "tensor 1: schedule overlaps %s" % name in _err()
+        assert call(dev=at - 104) == INVALID and "tensor 1: tensors overlaps %s" % name in _err()
+        assert call(schedule=at - 4) == INVALID and "tensor 1: schedule overlaps %s" % name in _err()
