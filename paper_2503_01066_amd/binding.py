@@ -353,6 +353,11 @@ def _wgrads_struct(grads, accumulate):
                      ("d" + w for w in WEIGHT_KEYS)], 1 if accumulate else 0)
 
 
+def _gradient(like, accumulate, stream):
+    """A gradient that a call makes itself: zeros where the call adds to it."""
+    return _empty(like.shape, like.dtype, like.device, stream, torch.zeros) if accumulate else torch.empty_like(like)
+
+
 def layer_backward_workspace_bytes(shape, total_tokens, max_seqlen):
     return lib().alch_layer_backward_workspace_bytes(C.byref(shape), total_tokens, max_seqlen)
 
@@ -367,7 +372,7 @@ def alch_layer_backward(shape, batch, saved, weights, dY, loss_mask=None, want=W
     L = lib()
     dev = dY.device
     if grads is None:
-        grads = {"d" + k: torch.empty_like(weights[k]) for k in want}
+        grads = {"d" + k: _gradient(weights[k], accumulate, stream) for k in want}
     if dX is None:
         dX = torch.empty_like(dY)
     need = L.alch_layer_backward_workspace_bytes(C.byref(shape), batch.total_tokens, batch.max_seqlen)
@@ -389,12 +394,12 @@ def alch_layer_backward_lora(shape, batch, saved, weights, lora, rank, scale, dY
     L = lib()
     dev = dY.device
     if grads is None:
-        grads = {"d" + k: torch.empty_like(weights[k]) for k in want}
+        grads = {"d" + k: _gradient(weights[k], accumulate, stream) for k in want}
     if lora_grads is None:
         lora_grads = {}
         for p_, (A_, B_) in lora.items():
-            lora_grads["dA" + p_] = torch.empty_like(A_)
-            lora_grads["dB" + p_] = torch.empty_like(B_)
+            lora_grads["dA" + p_] = _gradient(A_, accumulate, stream)
+            lora_grads["dB" + p_] = _gradient(B_, accumulate, stream)
     if dX is None:
         dX = torch.empty_like(dY)
     cl, cg = _lora_structs(lora, lora_grads, rank, scale, accumulate)
@@ -436,13 +441,13 @@ def alch_layer_forward(shape, batch, X, weights, workspace=None, stream=None, se
     return Y, rec
 
 
-def _head_grads(given, want, g_final, W_lm):
+def _head_grads(given, want, g_final, W_lm, accumulate, stream):
     if given is not None:
         for t, like, name in zip(given, (g_final, W_lm), ("dg_final", "dW_lm")):
             if t is not None:
                 _check_dense(t, "head_grads: " + name, like.dtype, like.get_device(), like.shape)
         return given
-    return (torch.empty_like(g_final), torch.empty_like(W_lm)) if want else (None, None)
+    return tuple(_gradient(t, accumulate, stream) for t in (g_final, W_lm)) if want else (None, None)
 
 
 def alch_stack_backward(shape, batch, saved_layers, weights_layers, X_final, g_final, W_lm, labels, loss_mask=None,
@@ -455,11 +460,11 @@ def alch_stack_backward(shape, batch, saved_layers, weights_layers, X_final, g_f
     n_layers = len(saved_layers)
     vocab = W_lm.shape[0]
     if grads_layers is None:
-        grads_layers = [{"d" + k: torch.empty_like(w[k]) for k in want} for w in weights_layers]
+        grads_layers = [{"d" + k: _gradient(w[k], accumulate, stream) for k in want} for w in weights_layers]
     SA = (CSaved * max(n_layers, 1))(*[_saved_struct(s, 0) for s in saved_layers])
     WA = (CWeights * max(n_layers, 1))(*[_weights_struct(w, 0) for w in weights_layers])
     GA = (CWgrads * max(n_layers, 1))(*[_wgrads_struct(g, accumulate) for g in grads_layers])
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     need = L.alch_stack_backward_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen)
@@ -498,13 +503,13 @@ def alch_stack_backward_lora(shape, batch, saved_layers, weights_layers, lora_la
     n_layers = len(saved_layers)
     vocab = W_lm.shape[0]
     if grads_layers is None:
-        grads_layers = [{"d" + k: torch.empty_like(w[k]) for k in want} for w in weights_layers]
+        grads_layers = [{"d" + k: _gradient(w[k], accumulate, stream) for k in want} for w in weights_layers]
     if lora_grads_layers is None:
         lora_grads_layers = []
         for lo in lora_layers:
             g = {}
             for p_, (A_, B_) in lo.items():
-                g["dA" + p_], g["dB" + p_] = torch.empty_like(A_), torch.empty_like(B_)
+                g["dA" + p_], g["dB" + p_] = _gradient(A_, accumulate, stream), _gradient(B_, accumulate, stream)
             lora_grads_layers.append(g)
     n = max(n_layers, 1)
     SA = (CSaved * n)(*[_saved_struct(s, 0) for s in saved_layers])
@@ -513,7 +518,7 @@ def alch_stack_backward_lora(shape, batch, saved_layers, weights_layers, lora_la
     pairs = [_lora_structs(lo, lg, rank, scale, accumulate) for lo, lg in zip(lora_layers, lora_grads_layers)]
     LA = (CLora * n)(*[p_[0] for p_ in pairs])
     LG = (CLoraGrads * n)(*[p_[1] for p_ in pairs])
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     need = L.alch_stack_backward_lora_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens,
@@ -574,7 +579,7 @@ def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final,
     dpo = CDpo(it.n_items, n_pairs, it.row.data_ptr(), it.label.data_ptr(), it.slot.data_ptr(), it.rows_host.ctypes.data,
                it.ref.data_ptr(), beta, z.data_ptr())
     if grads_layers is None:
-        grads_layers = [{"d" + k: torch.empty_like(w[k]) for k in want} for w in weights_layers]
+        grads_layers = [{"d" + k: _gradient(w[k], accumulate, stream) for k in want} for w in weights_layers]
     n = max(n_layers, 1)
     SA = (CSaved * n)(*[_saved_struct(s_, 0) for s_ in saved_layers])
     WA = (CWeights * n)(*[_weights_struct(w, 0) for w in weights_layers])
@@ -586,7 +591,7 @@ def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final,
             for lo in lora_layers:
                 g = {}
                 for p_, (A_, B_) in lo.items():
-                    g["dA" + p_], g["dB" + p_] = torch.empty_like(A_), torch.empty_like(B_)
+                    g["dA" + p_], g["dB" + p_] = _gradient(A_, accumulate, stream), _gradient(B_, accumulate, stream)
                 lora_grads_layers.append(g)
         pairs = [_lora_structs(lo, lg, rank, scale, accumulate) for lo, lg in zip(lora_layers, lora_grads_layers)]
         LA = (CLora * n)(*[p_[0] for p_ in pairs])
@@ -595,7 +600,7 @@ def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final,
                                                           batch.max_seqlen, rank)
     else:
         need = L.alch_stack_backward_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen)
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     ws = workspace if workspace is not None else _workspace(need, dev)
