@@ -441,20 +441,28 @@ def alch_layer_forward(shape, batch, X, weights, workspace=None, stream=None, se
     return Y, rec
 
 
-def _head_grads(given, want, g_final, W_lm, accumulate, stream):
+def _head_grads(given, want, default, g_final, W_lm, accumulate, stream):
+    """(dg_final, dW_lm).  given: the caller's tensors or None; want: None (the call's default, and given tensors), or whether there
+    are any."""
     if given is not None:
+        given = tuple(given)
+        if len(given) != 2:
+            raise ValueError("head_grads: 2 (dg_final, dW_lm) are needed, got %d" % len(given))
+        if want is not None and not want and any(t is not None for t in given):
+            raise ValueError("head_grads are given, and want_head is False")
         for t, like, name in zip(given, (g_final, W_lm), ("dg_final", "dW_lm")):
             if t is not None:
                 _check_dense(t, "head_grads: " + name, like.dtype, like.get_device(), like.shape)
         return given
-    return tuple(_gradient(t, accumulate, stream) for t in (g_final, W_lm)) if want else (None, None)
+    return tuple(_gradient(t, accumulate, stream) for t in (g_final, W_lm)) if (default if want is None else want) else (None, None)
 
 
 def alch_stack_backward(shape, batch, saved_layers, weights_layers, X_final, g_final, W_lm, labels, loss_mask=None,
-                        want=WEIGHT_KEYS, grads_layers=None, accumulate=False, want_head=True, hooks=None,
+                        want=WEIGHT_KEYS, grads_layers=None, accumulate=False, want_head=None, hooks=None,
                         workspace=None, stream=None, head_grads=None):
     """Returns dict: loss (device float tensor [1]), dX_embed, dg_final, dW_lm, layers=[grad dicts].  head_grads: the tensors
-    (dg_final, dW_lm) that the head's gradients go to, where a program keeps them."""
+    (dg_final, dW_lm) that the head's gradients go to, where a program keeps them; None for one that is not computed.  Without them the
+    call makes both, unless want_head is False."""
     L = lib()
     dev = X_final.device
     n_layers = len(saved_layers)
@@ -464,7 +472,7 @@ def alch_stack_backward(shape, batch, saved_layers, weights_layers, X_final, g_f
     SA = (CSaved * max(n_layers, 1))(*[_saved_struct(s, 0) for s in saved_layers])
     WA = (CWeights * max(n_layers, 1))(*[_weights_struct(w, 0) for w in weights_layers])
     GA = (CWgrads * max(n_layers, 1))(*[_wgrads_struct(g, accumulate) for g in grads_layers])
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, True, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     need = L.alch_stack_backward_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen)
@@ -493,10 +501,10 @@ def _lora_structs(lora, lora_grads, rank, scale, accumulate):
 
 
 def alch_stack_backward_lora(shape, batch, saved_layers, weights_layers, lora_layers, rank, scale, X_final, g_final,
-                             W_lm, labels, loss_mask=None, want=(), want_head=False, lora_grads_layers=None,
+                             W_lm, labels, loss_mask=None, want=(), want_head=None, lora_grads_layers=None,
                              grads_layers=None, accumulate=False, hooks=None, workspace=None, stream=None, head_grads=None):
     """Stack backward with adapters.  lora_layers: list of dicts projection -> (A, B).  Defaults: frozen base and
-    frozen head (want=(), want_head=False), gradients of every adapter.  Returns the dict of alch_stack_backward;
+    frozen head (want=(), no head gradients unless want_head or head_grads ask for them), gradients of every adapter.  Returns the dict of alch_stack_backward;
     the per-layer dicts hold the adapter gradients ('dAq', 'dBq', ...) and any base gradients asked for."""
     L = lib()
     dev = X_final.device
@@ -518,7 +526,7 @@ def alch_stack_backward_lora(shape, batch, saved_layers, weights_layers, lora_la
     pairs = [_lora_structs(lo, lg, rank, scale, accumulate) for lo, lg in zip(lora_layers, lora_grads_layers)]
     LA = (CLora * n)(*[p_[0] for p_ in pairs])
     LG = (CLoraGrads * n)(*[p_[1] for p_ in pairs])
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, False, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     need = L.alch_stack_backward_lora_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens,
@@ -564,7 +572,7 @@ class DpoItems:
 
 def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final, g_final, W_lm, item_row, item_label,
                             item_slot, ref_logp, beta, lora_layers=None, rank=0, scale=1.0, want=WEIGHT_KEYS,
-                            want_head=True, lora_grads_layers=None, grads_layers=None, accumulate=False, hooks=None,
+                            want_head=None, lora_grads_layers=None, grads_layers=None, accumulate=False, hooks=None,
                             workspace=None, stream=None, head_grads=None):
     """Stack backward under the DPO loss.  item_row / item_label / item_slot: int32 numpy arrays, one entry per
     scored token, rows ascending; ref_logp: float32 [2 * n_pairs] (numpy or device tensor); or item_row = a DpoItems
@@ -600,7 +608,7 @@ def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final,
                                                           batch.max_seqlen, rank)
     else:
         need = L.alch_stack_backward_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen)
-    dg_final, dW_lm = _head_grads(head_grads, want_head, g_final, W_lm, accumulate, stream)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, True, g_final, W_lm, accumulate, stream)
     dX_embed = torch.empty_like(X_final)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     ws = workspace if workspace is not None else _workspace(need, dev)

@@ -66,3 +66,30 @@ def test_gradients_that_are_added_to_begin_as_zeros(library, name):
     written = gradients(run(name, **kw))
     assert written.keys() == made.keys()  # (nothing is cleared where all of it is written)
     assert all(bool(torch.isnan(g).all()) for g in written.values())
+
+
+HEADS = [c for c in CALLS if "stack" in c]
+
+
+@pytest.mark.parametrize("name", HEADS)
+def test_head_gradients_that_are_given_and_not_wanted_are_refused(library, name):
+    head = torch.zeros(H), torch.zeros(V, H)
+    for given in (head, (None, head[1]), (head[0], None)):
+        with pytest.raises(ValueError, match="head_grads"):
+            run(name, head_grads=given, want_head=False)
+    for kw in (dict(), dict(want_head=True)):  # (given tensors are wanted ones, whatever the call does without any)
+        out = run(name, head_grads=head, **kw)
+        assert out["dg_final"] is head[0] and out["dW_lm"] is head[1]
+    assert run(name, head_grads=(None, head[1]))["dg_final"] is None
+    out = run(name, want_head=False)
+    assert out["dg_final"] is None and out["dW_lm"] is None
+    assert run(name, head_grads=(None, None), want_head=False)["dW_lm"] is None
+    without = run(name)
+    assert (without["dW_lm"] is None) == (name == "alch_stack_backward_lora")
+
+
+@pytest.mark.parametrize("given", [(torch.zeros(H),), (torch.zeros(H), torch.zeros(V, H), torch.zeros(1))])
+def test_head_gradients_are_two(library, given):
+    for name in HEADS:
+        with pytest.raises(ValueError, match="head_grads: 2"):
+            run(name, head_grads=given)
