@@ -449,8 +449,8 @@ int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batc
  * alch_embed_forward: X[t] = scale * W_embed[token_ids[t]]; a token id outside 0..vocab-1 marks a position without
  * a token (padding): its row is zero.
  *   token_ids  device int32 [n_tokens], 4-byte aligned;  W_embed [vocab, hidden];  X [n_tokens, hidden] out
- * The product is rounded once; scale = 1 copies the rows' bits.  Supported: n_tokens <= 2^30, hidden <= 2^20, 2^40
- * elements of W_embed and of X.
+ * The product is rounded once; scale = 1 copies the rows (bit for bit, but that signalling NaNs become quiet ones).
+ * Supported: n_tokens <= 2^30, hidden <= 2^20, 2^40 elements of W_embed and of X.
  */
 int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids,
                        const void* W_embed, float scale, void* X, void* hip_stream);

@@ -5,7 +5,8 @@
 //
 // Both are bound by memory.  The backward pass needs the tokens of a row next to one another: they are sorted by id (stable,
 // so that every sum runs over ascending tokens and results repeat bit for bit; no float atomics), and the sorted tokens are
-// cut into parts of equal length, so that one id that half of a batch shares is no longer a chain than any other.
+// cut into parts of equal length, so that one id that half of a batch shares is summed by as many wavefronts as its tokens need.  What
+// stays a chain is the sum of these pieces: a quarter of an id's parts behind one another, for every 256 columns.
 #include <algorithm>
 #include <type_traits>
 
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(256) void k_embed(const int* __restrict__ ids, cons
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) v[j][e] = (T)((float)v[j][e] * scale);
+            for (int e = 0; e < kVec; ++e) v[j][e] = (T)((float)v[j][e] * scale);  // (by 1: the same bits, but a signalling NaN's)
             if (!valid) v[j] = vec{};  // (also where the scale is negative or no number)
             if (c0 + j * step < end) __builtin_nontemporal_store(v[j], reinterpret_cast<vec*>(X + t * hidden + min(c0 + j * step, hidden - kVec)));
         }

@@ -172,7 +172,9 @@ __global__ __launch_bounds__(256) void k_norm(const alch_grad_tensor* __restrict
         int rest = -1;
         float r = 0.f;
         clip_load(a, v, &rest, &r);
-        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);  // (while these are on their way)
+        // (while these are on their way where the table is in registers: they are flat loads, the compiler cannot know where a pointer out of
+        // memory points, and a look into LDS waits for those too)
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);
         if (a.dtype == ALCH_BF16) {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(256) void k_clip(const alch_grad_tensor* __restrict
         float r = 0.f;
         const bool full = a.out && clip_load(a, v, &rest, &r);
         ClipChunk next = {};
-        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);  // (while these are on their way)
+        if (c + (int)gridDim.x < chunks) next = clip_chunk(table, c + gridDim.x);  // (behind the loads, which the compiler waits for here)
         if (c == (int)blockIdx.x) factor = clip_factor(sums, max_norm, norm_out);
         if (a.out && !(a.out == a.grad && factor == 1.f)) {
 #pragma unroll

@@ -22,3 +22,13 @@ def test_smaller_batches_in_the_workspace_of_the_largest(H, V, sizes):
         dW = A.alch_embed_backward(*dev, V, dW_embed=old.cuda(), accumulate=True, workspace=memory[:size])
         check_backward(ids, dX, V, 1.0, dW, old)
         assert bool((memory[size:] == 0x7f).all())
+
+
+@pytest.mark.parametrize("H", [64, 4])
+def test_rows_times_one_are_copies(H):
+    """Every bf16 there is, subnormal ones among them; a signalling NaN comes out quiet, with the rest of its bits."""
+    import paper_2503_01066_amd as A
+    W = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).cuda().view(-1, H)
+    X = A.alch_embed_forward(torch.arange(W.shape[0], dtype=torch.int32, device="cuda"), W)
+    quiet = torch.where(torch.isnan(W), torch.full_like(W, 1.0).view(torch.int16) * 0 + 0x40, torch.zeros_like(W.view(torch.int16)))
+    assert torch.equal(X.view(torch.int16), W.view(torch.int16) | quiet)
