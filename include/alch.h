@@ -490,7 +490,8 @@ typedef struct {
  * alch_grad_clip: the 2-norm over all elements of all tensors, and the gradients scaled so that it does not exceed max_norm:
  *   norm = sqrt(sum g^2);  factor = max_norm / norm where norm > max_norm, else 1;  out = factor * grad
  * A norm that is no finite number (an infinity or NaN among the gradients) gives factor NaN: clipped gradients are NaN
- * then, and alch_adamw_step that is given this factor leaves everything as it was.  The sum is held in 64 bits: finite gradients of any size have
+ * then, and alch_adamw_step that is given this factor leaves everything as it was; without it the NaN of
+ * gradients clipped here reach the weights.  The sum is held in 64 bits: finite gradients of any size have
  * a finite sum (the norm is rounded to fp32 when it is written).
  *   max_norm   >= 0; an infinity only measures
  *   norm_out   device float [2] out: { norm, factor }, 4-byte aligned
