@@ -229,6 +229,9 @@ def _prepare_adamw8(case, seed, g):
         s["master"] = master
     if own:
         import paper_2503_01066_amd as A
+        # codes between the tensors are nobody's, and stay; a pass over the whole buffer leaves a zero there whose sign the gradient's zero has a
+        # part in
+        m[0].copy_(torch.where(held, m[0], m[0] * torch.signbit(grad)))
         parts = lambda flat: [flat[a:a + n] for a, n in layout]
         states = lambda pair: [(pair[0][a:a + n], pair[1][a // GROUP:a // GROUP + _groups(n)]) for a, n in layout]
         s["list"] = A.Adamw8List(parts(s["param"]), parts(grad), states(m), states(v), masters=parts(master) if case["master"] else None,
