@@ -170,6 +170,67 @@ int alch_capture_pack_static(const alch_batch* batch, const uint8_t* keep_mask, 
                              int32_t* cu_kept, int32_t* n_kept_and_status, void* hip_stream);
 size_t alch_capture_pack_static_max_tokens(void);
 
+/*
+ * alch_capture_pack_q8: alch_capture_pack with the kept rows written in 8 bits, for records that are held for long or cross the
+ * host link.  A row's elements share a scale in groups of ALCH_Q8_GROUP, counted from the row's start (the last group of a row may
+ * be shorter).  With a = the largest magnitude of a group, every operation rounded to fp32 (nearest, ties to even):
+ *     scale = a / 127;   code = rint(x * (127 / a))
+ * so that code * scale is off by at most half a step of a / 127, and the largest element of a group comes back to within a
+ * rounding.  A group with a < 2^-100 has scale 0 and codes 0; one with an infinity or NaN has scale NaN and codes 0: it comes back as NaN.
+ * Result and refusals are otherwise alch_capture_pack's: kept_index, cu_kept, n_kept_and_status and the rows behind n_kept, which stay as
+ * they were.  Streams that are to keep all their bits (LSE, for one) go through alch_capture_gather with this call's index; a
+ * record of X, Q, K, V, G, U has its other members recomputed from what was read back, and so consistent with it.
+ *   src       [total_tokens, width] of dtype, rows src_row_stride_bytes apart (a multiple of the element, >= the row)
+ *   codes     int8 [dst_capacity_rows, width] out, dense;  scales  float [dst_capacity_rows, ceil(width / ALCH_Q8_GROUP)] out, dense
+ * src aligned to its element, codes and scales 16-byte aligned.  What the call writes may not overlap other memory of the call.
+ * Rows of bf16 or fp32 whose width is a multiple of 8 and whose address and stride are multiples of 16 bytes take the fast path.
+ */
+#define ALCH_Q8_GROUP 64
+
+typedef struct {
+    const void* src;
+    int8_t* codes;
+    float* scales;
+    int64_t width;
+    size_t src_row_stride_bytes;
+    int32_t dtype; /* alch_dtype of src */
+    int32_t reserved;
+} alch_q8_stream; /* the array of these lives in HOST memory */
+
+int alch_capture_pack_q8(const alch_batch* batch, const uint8_t* keep_mask, int32_t n_streams, const alch_q8_stream* streams,
+                         int64_t dst_capacity_rows, int32_t* kept_index, int32_t* cu_kept, int32_t* n_kept_and_status, void* workspace,
+                         size_t workspace_bytes, void* hip_stream); /* workspace: alch_capture_pack_workspace_bytes */
+
+/*
+ * alch_capture_gather_q8: the rows of alch_capture_pack_q8 alone, with the index of an earlier alch_capture_pack or
+ * alch_capture_pack_q8 on the same batch and mask; see alch_capture_gather.  kept_index == NULL and n_kept_and_status == NULL: every
+ * token is kept (dst_capacity_rows >= total_tokens then).
+ */
+int alch_capture_gather_q8(const alch_batch* batch, int32_t n_streams, const alch_q8_stream* streams, int64_t dst_capacity_rows,
+                           const int32_t* kept_index, const int32_t* n_kept_and_status, void* hip_stream);
+
+/*
+ * alch_record_expand: rows of 8 bits back as tensors, dst[i, c] = codes[r, c] * scales[r, c / ALCH_Q8_GROUP] with r = rows[i] (i without
+ * rows), rounded once.
+ *   rows      device int32 [n_rows] or NULL; an entry outside 0..n_src_rows-1 marks padding: its row of every dst is zero.  The same row
+ *             may be listed several times.  NULL: n_rows <= n_src_rows
+ *   codes     int8 [n_src_rows, width], scales float [n_src_rows, ceil(width / ALCH_Q8_GROUP)], both dense and 16-byte aligned
+ *   dst       [n_rows, width] of dtype, out; rows dst_row_stride_bytes apart (a multiple of the element, >= the row), aligned to its
+ *             element (16 bytes take the fast path, as above); what lies between two rows is left as it was
+ */
+typedef struct {
+    void* dst;
+    const int8_t* codes;
+    const float* scales;
+    int64_t width;
+    size_t dst_row_stride_bytes;
+    int32_t dtype; /* alch_dtype of dst */
+    int32_t reserved;
+} alch_q8_tensor; /* the array of these lives in HOST memory */
+
+int alch_record_expand(int64_t n_rows, const int32_t* rows, int64_t n_src_rows, int32_t n_tensors, const alch_q8_tensor* tensors,
+                       void* hip_stream);
+
 /* ------------------------------------------------------------------------------------
  * Family 2: backward from saved activations (Section 1; Section 4.2; Section 4.3.2).
  */
@@ -360,6 +421,57 @@ int alch_stack_backward_dpo(const alch_layer_shape* shape, int32_t n_layers, int
                             void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Policy optimisation on served responses (the other loss of preference alignment beside Section 6's DPO: the tokens were sampled while
+ * serving, an advantage says how good each was).  An item m is a sampled token: its logits, its label, the log-probability old_logp it
+ * was sampled with, its advantage A, a weight w, and with a KL term its log-probability ref_logp under the frozen reference model.  With
+ *     logp = log softmax(logits)[label],  ratio = exp(logp - old_logp),  u = ratio * A,  b = min(max(ratio, 1 - clip_low), 1 + clip_high) * A
+ *     kl = exp(ref_logp - logp) - (ref_logp - logp) - 1
+ *     loss = sum over items of w * (-min(u, b) + kl_coef * kl)
+ *     d loss / d logits = d * (onehot(label) - softmax),   d = w * (-(b < u ? 0 : u) + kl_coef * (1 - exp(ref_logp - logp)))
+ * The weights hold the mean that is wanted (1 / items, 1 / (sequences * length), ..).  An item whose label is outside 0..vocab-1 or whose
+ * weight is 0 scores nothing: its logits are not read, its gradient is zero, its logp_out 0.  Logits of -inf (forbidden tokens) have
+ * probability 0 and gradient 0; an item all of whose logits are -inf scores nothing either, its logp_out is -inf.  A = 0 has u = b = 0 whatever
+ * the ratio.  NaN and +inf among the logits of an item that scores make its gradient, logp_out and the loss NaN.
+ */
+typedef struct {
+    int32_t n_items;
+    float clip_low, clip_high;  /* >= 0; infinite: no bound on that side */
+    float kl_coef;              /* >= 0, finite; ref_logp must be given where it is not 0 */
+    const int32_t* label;       /* device [n_items] */
+    const float *old_logp, *advantage, *weight; /* device [n_items] */
+    const float* ref_logp;      /* device [n_items] or NULL: kl counts as 0 */
+    const int32_t* item_row;    /* device [n_items], for alch_stack_backward_policy alone: see alch_dpo */
+    const int32_t* item_row_host;
+    float* logp_out;            /* device [n_items] out, or NULL */
+} alch_policy;
+
+/*
+ * alch_policy_loss: the loss of items whose logits are at hand, and its gradient.
+ *   logits    [n_items, vocab], rows ld elements apart
+ *   dlogits   NULL (the loss and logp_out alone), logits itself with the same ld (in place), or other memory [n_items, vocab], rows ld_grad
+ *             apart; what lies between two rows is left as it was
+ *   loss_out  device float [4] out: { loss, sum w * -min(u, b), sum w * kl, sum of w where b < u (the share that is clipped) }
+ *   workspace alch_policy_loss_workspace_bytes(n_items, vocab) bytes, 16-byte aligned; the size never falls with n_items
+ * Sums run in a fixed order: results repeat bit for bit.  Statistics and the loss are held in fp32 or more.  n_items = 0 gives zeros.
+ * Supported: vocab <= 2^28.  Memory that the call writes may not overlap other memory of the call, except dlogits == logits.
+ */
+int alch_policy_loss(alch_dtype dtype, int32_t vocab, const void* logits, int64_t ld, const alch_policy* policy, void* dlogits,
+                     int64_t ld_grad, float* loss_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t alch_policy_loss_workspace_bytes(int32_t n_items, int32_t vocab);
+
+/*
+ * alch_stack_backward_policy: alch_stack_backward[_lora] with the policy loss in place of cross-entropy.  An item's logits are the LM-head
+ * row of stack-output row item_row[m], as for alch_stack_backward_dpo: ascending (equal rows adjacent: the first tokens of several
+ * responses to one shared prompt), n_items <= total_tokens.  loss_out has the four values of alch_policy_loss.  lora / lora_grads may be
+ * NULL; every other argument and the workspace size are those of alch_stack_backward_lora (alch_stack_backward when lora == NULL).
+ */
+int alch_stack_backward_policy(const alch_layer_shape* shape, int32_t n_layers, int32_t vocab, const alch_batch* batch,
+                               const alch_saved* saved, const alch_weights* weights, const alch_lora* lora, const void* X_final,
+                               const void* g_final, const void* W_lm, const alch_policy* policy, const alch_wgrads* wgrads,
+                               const alch_lora_grads* lora_grads, void* dg_final, void* dW_lm, void* dX_embed, float* loss_out,
+                               const alch_hooks* hooks, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * alch_layer_forward: the forward pass of one layer, writing Y and the full record.
  * It is the producer side of the record (what serving prefill computes, Section 4.1) and
  * the "recompute" leg of the comparison in Section 6; record_out members are written,
@@ -530,6 +642,45 @@ typedef struct {
  */
 int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* tensors_host,
                     const alch_adamw* params, void* hip_stream);
+
+/* The moments of alch_adamw8_step: a byte an element, and a byte of scale for every block of ALCH_ADAMW8_BLOCK elements of a tensor, counted
+ * from its start.  A scale byte s stands for 2^(s - 127); 0 stands for 0, and 255 makes every element of the block NaN.
+ *   m  sign, 4 bits of exponent (bias 7), 3 of mantissa (e4m3 without infinities: torch.float8_e4m3fn), times the block's scale
+ *   v  5 bits of exponent (bias 15), 3 of mantissa, no sign, every code finite: code c is (c & 7) * 2^-17 for c < 8, else
+ *      (1 + (c & 7) / 8) * 2^((c >> 3) - 15), times the block's scale
+ * Zeros in all four arrays are the moments of a new run. */
+#define ALCH_ADAMW8_BLOCK 64
+
+typedef struct {
+    void* param;
+    const void* grad; /* of param's type */
+    float* master;    /* as alch_adamw_tensor */
+    uint8_t *m, *v;             /* [n], 16-byte aligned */
+    uint8_t *m_scale, *v_scale; /* [ceil(n / ALCH_ADAMW8_BLOCK)], of any alignment */
+    int64_t n;
+    int64_t first;    /* >= 0, the number of the tensor's first element for its random bits: elements of equal number have equal bits */
+    float weight_decay;
+    int32_t dtype; /* alch_dtype of param and grad */
+} alch_adamw8_tensor;
+
+/*
+ * alch_adamw8_step: alch_adamw_step with both moments held in 8 bits: 16 bytes an element and step with a master copy, where
+ * fp32 moments take 28.  The update of the weights uses the new moments in fp32, before they are rounded:
+ *   x = grad_factor * g;  m = beta1 m + (1 - beta1) x;  v = beta2 v + (1 - beta2) (x x)     each operation rounded to fp32, no fused ones
+ * A block's scale is the power of two that brings its largest new m into [2^7, 2^8), its largest v into [2^15, 2^16) (the byte is
+ * at least 1); then each element is rounded up or down to a neighbouring code, up with a probability that is its distance to the lower one:
+ * rounding to the nearest would never move a v that changes by 1 - beta2 a step, far less than half a code.  A v > 0 is never
+ * rounded to 0 but to the smallest code: m / sqrt(0) would be a step without bound.  A block with a new value that is no finite number
+ * becomes NaN as a whole.
+ * The random bits of element number i (first + index), all numbers mod 2^32:
+ *   mix(x): x ^= x >> 16; x *= 0x6A09E667; x ^= x >> 15; x *= 0xBB67AE85; x ^= x >> 16
+ *   bits = mix((i mod 2^32) + mix(mix(seed ^ mix(step)) ^ (i >> 32)));   m takes the lower 16, v the upper 16: up where the 20 bits
+ * of mantissa that a code has not, plus these 16 bits times 16, carry (values below the smallest normal code, after adding that one).
+ * Results are therefore the same wherever a tensor is cut or in whatever order tensors are listed, given the numbers of its elements.
+ * params as in alch_adamw_step, step (or the schedule's) also chooses the random bits, together with seed.
+ */
+int alch_adamw8_step(int32_t n_tensors, const alch_adamw8_tensor* tensors, const alch_adamw8_tensor* tensors_host,
+                     const alch_adamw* params, uint32_t seed, void* hip_stream);
 
 /*
  * Launch timing for benchmarks.  While enabled, the library brackets its main kernels with two

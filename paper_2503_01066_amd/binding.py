@@ -5,6 +5,7 @@ every step of the computation runs inside the library.  There is no fallback: if
 library has not been built, loading raises.
 """
 import ctypes as C
+import itertools
 import os
 from array import array
 
@@ -103,6 +104,23 @@ class AdamwTensor(C.Structure):
 class CAdamw(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int32),
                 ("schedule", C.c_void_p), ("grad_factor", C.c_void_p)]
+
+
+class CQ8(C.Structure):
+    """alch_q8_stream (tensor: its src) and alch_q8_tensor (its dst)."""
+    _fields_ = [("tensor", C.c_void_p), ("codes", C.c_void_p), ("scales", C.c_void_p), ("width", C.c_int64), ("row_stride_bytes", C.c_size_t),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class CPolicy(C.Structure):
+    _fields_ = [("n_items", C.c_int32), ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("label", C.c_void_p),
+                ("old_logp", C.c_void_p), ("advantage", C.c_void_p), ("weight", C.c_void_p), ("ref_logp", C.c_void_p), ("item_row", C.c_void_p),
+                ("item_row_host", C.c_void_p), ("logp_out", C.c_void_p)]
+
+
+class Adamw8Tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("n", C.c_int64), ("first", C.c_int64), ("weight_decay", C.c_float), ("dtype", C.c_int32)]
 
 
 TRACE_KINDS = ("gemm_mfma", "gemm_generic", "pack_scan", "pack_gather", "attn_bwd", "attn_fwd", "row_ops",
@@ -214,6 +232,21 @@ def lib():
     L.alch_grad_clip_workspace_bytes.argtypes = []
     L.alch_adamw_step.restype = C.c_int
     L.alch_adamw_step.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(CAdamw), C.c_void_p]
+    L.alch_capture_pack_q8.restype = C.c_int
+    L.alch_capture_pack_q8.argtypes = L.alch_capture_pack.argtypes
+    L.alch_capture_gather_q8.restype = C.c_int
+    L.alch_capture_gather_q8.argtypes = L.alch_capture_gather.argtypes
+    L.alch_record_expand.restype = C.c_int
+    L.alch_record_expand.argtypes = [C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+    L.alch_policy_loss.restype = C.c_int
+    L.alch_policy_loss.argtypes = [C.c_int, C.c_int32, C.c_void_p, C.c_int64, C.POINTER(CPolicy), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                   C.c_size_t, C.c_void_p]
+    L.alch_policy_loss_workspace_bytes.restype = C.c_size_t
+    L.alch_policy_loss_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+    L.alch_stack_backward_policy.restype = C.c_int
+    L.alch_stack_backward_policy.argtypes = [C.POINTER(CPolicy) if t is C.POINTER(CDpo) else t for t in L.alch_stack_backward_dpo.argtypes]
+    L.alch_adamw8_step.restype = C.c_int
+    L.alch_adamw8_step.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(CAdamw), C.c_uint32, C.c_void_p]
     L.alch_trace_enable.argtypes = [C.c_int32]
     L.alch_trace_collect.argtypes = [C.POINTER(CTraceRecord), C.c_int32, C.POINTER(C.c_int32)]
     _PACK = C.cast(L.alch_capture_pack, C.c_void_p).value
@@ -336,6 +369,127 @@ def alch_capture_gather(batch, kept_index, status, streams, capacity=None, dsts=
     _check(L.alch_capture_gather(C.byref(batch.c), len(streams), arr.buffer_info()[0], capacity, _ptr(kept_index), _ptr(status),
                                  _stream_handle(stream)))
     return dsts
+
+
+Q8_GROUP = 64  # elements of a row that share a scale
+
+
+def _q8_words(tensors, pairs, index):
+    """The array of a call on records in 8 bits, as the six 64-bit words of each entry, and the most rows that all codes can hold."""
+    words, rows = [], None
+    if len(tensors) != len(pairs):
+        raise ValueError("%d tensors, %d pairs of codes and scales" % (len(tensors), len(pairs)))
+    for k, (t, (codes, scales)) in enumerate(zip(tensors, pairs)):
+        held, width = codes.shape
+        size, stride = t.element_size(), t.stride()
+        if t.dim() != 2 or t.shape[1] != width or t.get_device() != index or (width > 1 and stride[1] != 1 and t.numel() > 0):
+            raise ValueError("tensor %d: rows of %d elements one after another on cuda:%d are needed, got %s with strides %s on %s" % (
+                k, width, index, tuple(t.shape), stride, t.device))
+        if codes.dtype is not torch.int8 or not codes.is_contiguous() or codes.get_device() != index:
+            _check_dense(codes, ("codes", k), torch.int8, index)
+        if scales.dtype is not torch.float32 or scales.shape != (held, -(-width // Q8_GROUP)) or not scales.is_contiguous() or scales.get_device() != index:
+            _check_dense(scales, ("scales", k), torch.float32, index, (held, -(-width // Q8_GROUP)))
+        rows = held if rows is None or held < rows else rows
+        words += (t.data_ptr(), codes.data_ptr(), scales.data_ptr(), width, (stride[0] if t.shape[0] > 1 else width) * size, _code(t.dtype))
+    return array("Q", words), rows
+
+
+def _q8_pairs(rows, streams, stream):
+    return [(_empty((rows, s.shape[1]), torch.int8, s.device, stream), _empty((rows, -(-s.shape[1] // Q8_GROUP)), torch.float32, s.device, stream))
+            for s in streams]
+
+
+def _rows_of_batch(streams, batch):
+    for k, s in enumerate(streams):
+        if s.shape[0] != batch.total_tokens:
+            raise ValueError("streams[%d] has %d rows, the batch %d tokens" % (k, s.shape[0], batch.total_tokens))
+
+
+def alch_capture_pack_q8(batch, keep_mask, streams, capacity=None, dsts=None, stream=None, workspace=None):
+    """alch_capture_pack with the kept rows in 8 bits.  streams: bf16 or fp32 tensors [T, width] (rows may be further apart than the
+    width).  dsts: per stream (codes int8 [rows, width], scales float32 [rows, ceil(width / 64)]), as returned.  Returns
+    (kept_index, cu_kept, n_kept_and_status, dsts)."""
+    L = lib()
+    T, dev = batch.total_tokens, keep_mask.get_device()
+    handle = _place(dev, stream)
+    if keep_mask.element_size() != 1 or keep_mask.numel() != T or not keep_mask.is_contiguous():
+        raise ValueError("keep_mask: a byte for each of the %d tokens is needed, got %s %s" % (T, keep_mask.dtype, tuple(keep_mask.shape)))
+    _rows_of_batch(streams, batch)
+    if dsts is None:
+        capacity = T if capacity is None else int(capacity)
+        dsts = _q8_pairs(capacity, streams, stream)
+    words, held = _q8_words(streams, dsts, dev)
+    if capacity is None:
+        capacity = T if held is None else held
+    elif held is not None and held < capacity:
+        raise ValueError("dsts hold %d rows, capacity is %d" % (held, capacity))
+    if workspace is None:
+        workspace = _empty((max(L.alch_capture_pack_workspace_bytes(T), 256),), torch.uint8, keep_mask.device, stream)
+    else:
+        _check_dense(workspace, "workspace", torch.uint8, dev)
+    # one allocation: the index, the sequences' counts behind it, then the status
+    rows, bounds = max(capacity, 1), batch.n_seqs + 1
+    out = _empty((rows + bounds + 2,), torch.int32, keep_mask.device, stream)
+    at = out.data_ptr()
+    _check(L.alch_capture_pack_q8(C.byref(batch.c), keep_mask.data_ptr(), len(streams), words.buffer_info()[0], capacity, at, at + 4 * rows,
+                                  at + 4 * (rows + bounds), workspace.data_ptr(), workspace.numel(), handle))
+    return out[:rows], out[rows:rows + bounds], out[rows + bounds:], dsts
+
+
+def alch_capture_gather_q8(batch, streams, kept_index=None, status=None, capacity=None, dsts=None, stream=None):
+    """The rows of further streams in 8 bits, with the index and status that an earlier alch_capture_pack or alch_capture_pack_q8 on the same
+    batch and mask returned; without them all tokens are kept.  Returns dsts (see alch_capture_pack_q8)."""
+    L = lib()
+    T = batch.total_tokens
+    dev = streams[0].get_device() if len(streams) else batch.cu_dev.get_device()
+    handle = _place(dev, stream)
+    _rows_of_batch(streams, batch)
+    if (kept_index is None) != (status is None):
+        raise ValueError("kept_index and status are given together")
+    if kept_index is not None:
+        _check_dense(kept_index, "kept_index", torch.int32, dev)
+        _check_dense(status, "status", torch.int32, dev, (2,))
+    most = T if kept_index is None else min(T, kept_index.numel())
+    if dsts is None:
+        capacity = most if capacity is None else int(capacity)
+        dsts = _q8_pairs(capacity, streams, stream)
+    words, held = _q8_words(streams, dsts, dev)
+    if capacity is None:
+        capacity = most if held is None else min(held, most) if kept_index is not None else held
+    elif held is not None and held < capacity:
+        raise ValueError("dsts hold %d rows, capacity is %d" % (held, capacity))
+    if kept_index is not None and capacity > kept_index.numel():
+        raise ValueError("capacity is %d, kept_index has %d rows" % (capacity, kept_index.numel()))
+    _check(L.alch_capture_gather_q8(C.byref(batch.c), len(streams), words.buffer_info()[0], capacity, _ptr(kept_index), _ptr(status), handle))
+    return dsts
+
+
+def alch_record_expand(records, outs=None, rows=None, dtype=torch.bfloat16, n_rows=None, stream=None):
+    """Rows in 8 bits back as tensors.  records: pairs (codes, scales) of equally many rows; rows: device int32 [n], the row of the records
+    that each row of the outputs comes from (one outside of them gives zeros), or None: the first n_rows of them (default: all).  outs: per
+    record a bf16 or fp32 tensor [n, width] (rows may be further apart than the width), or None: new ones of dtype.  Returns outs."""
+    L = lib()
+    records = list(records)
+    if not records:
+        return [] if outs is None else outs
+    first, dev = records[0][0], records[0][0].get_device()
+    handle = _place(dev, stream)
+    held = first.shape[0]
+    if rows is not None:
+        _check_dense(rows, "rows", torch.int32, dev, (rows.numel(),))
+        if n_rows is not None and n_rows != rows.numel():
+            raise ValueError("n_rows is %d, rows has %d" % (n_rows, rows.numel()))
+        n = rows.numel()
+    else:
+        n = held if n_rows is None else int(n_rows)
+    if outs is None:
+        outs = [_empty((n, c.shape[1]), dtype, c.device, stream) for c, s in records]
+    words, least = _q8_words(outs, records, dev)
+    for k, (o, (c, s)) in enumerate(zip(outs, records)):
+        if o.shape[0] != n or c.shape[0] != held:
+            raise ValueError("record %d: %d rows of %d where the call has %d of %d" % (k, o.shape[0], c.shape[0], n, held))
+    _check(L.alch_record_expand(n, _ptr(rows), held, len(records), words.buffer_info()[0], handle))
+    return outs
 
 
 def _saved_struct(saved, version):
@@ -629,6 +783,114 @@ def alch_stack_backward_dpo(shape, batch, saved_layers, weights_layers, X_final,
     return dict(loss=loss, z=z[:n_pairs], dX_embed=dX_embed, dg_final=dg_final, dW_lm=dW_lm, layers=layers)
 
 
+class PolicyItems:
+    """The sampled tokens of a policy loss, on the device: label int32 [n], the log-probability old_logp they were sampled with, their
+    advantage and weight, and their log-probability ref_logp under the reference model (fp32 [n] each, ref_logp may be None).  rows: for
+    alch_stack_backward_policy the stack-output row of each (int32 numpy array, ascending)."""
+
+    def __init__(self, label, old_logp, advantage, weight, ref_logp=None, rows=None):
+        n = self.n_items = label.numel()
+        self.index = label.get_device()
+        _check_dense(label, "label", torch.int32, self.index, (n,))
+        for name, t in (("old_logp", old_logp), ("advantage", advantage), ("weight", weight), ("ref_logp", ref_logp)):
+            if t is not None:
+                _check_dense(t, name, torch.float32, self.index, (n,))
+        self.label, self.old_logp, self.advantage, self.weight, self.ref_logp = label, old_logp, advantage, weight, ref_logp
+        self.rows_host = self.rows = None
+        if rows is not None:
+            self.rows_host = np.ascontiguousarray(rows, dtype=np.int32)
+            if self.rows_host.shape != (n,):
+                raise ValueError("rows: %s for %d items" % (self.rows_host.shape, n))
+            self.rows = torch.from_numpy(self.rows_host.copy()).to(label.device)
+        self.words = (label.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), _ptr(ref_logp), _ptr(self.rows),
+                      None if rows is None else self.rows_host.ctypes.data)
+
+
+def policy_loss_workspace_bytes(n_items, vocab):
+    _check_int32("n_items, vocab", n_items, vocab)
+    return lib().alch_policy_loss_workspace_bytes(n_items, vocab)
+
+
+def alch_policy_loss(logits, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0, want_grad=True, dlogits=None, logp=None, loss=None, workspace=None,
+                     stream=None):
+    """The clipped policy loss of a PolicyItems from its logits [n, vocab] (rows may be further apart), and its gradient.  dlogits: the tensor
+    that the gradient goes to (logits itself: in place); None: a new one, or none at all if not want_grad.  Returns (loss, logp, dlogits): loss
+    a device float tensor [4] {loss, surrogate, kl, clipped share}, logp [n] the items' log-probabilities."""
+    L = lib()
+    (n, vocab), dev, dt = logits.shape, logits.get_device(), logits.dtype
+    handle = _place(dev, stream)
+    _check_int32("n_items, vocab", n, vocab)
+    if items.n_items != n or items.index != dev:
+        raise ValueError("logits %s on %s for %d items" % (tuple(logits.shape), logits.device, items.n_items))
+    if dlogits is None and want_grad:
+        dlogits = _empty((n, vocab), dt, logits.device, stream)
+    for name, t in (("logits", logits), ("dlogits", dlogits)):
+        if t is not None and (t.dtype is not dt or t.shape != logits.shape or t.get_device() != dev or (t.stride(1) != 1 and vocab > 1) or t.stride(0) < 0):
+            raise ValueError("%s: rows of %d elements of %s one after another are needed, got %s %s with strides %s on %s" % (
+                name, vocab, dt, tuple(t.shape), t.dtype, t.stride(), t.device))
+    if logp is None:
+        logp = _empty((n,), torch.float32, logits.device, stream)
+    else:
+        _check_dense(logp, "logp", torch.float32, dev, (n,))
+    if loss is None:
+        loss = _empty((4,), torch.float32, logits.device, stream)
+    else:
+        _check_dense(loss, "loss", torch.float32, dev, (4,))
+    if workspace is None:
+        workspace = _empty((L.alch_policy_loss_workspace_bytes(n, vocab) or 256,), torch.uint8, logits.device, stream)
+    else:
+        _check_dense(workspace, "workspace", torch.uint8, dev)
+    p = CPolicy(n, clip_low, clip_high, kl_coef, *items.words, logp.data_ptr())
+    pitch = lambda t: t.stride(0) if n > 1 else vocab
+    rc = L.alch_policy_loss(_code(dt), vocab, logits.data_ptr(), pitch(logits), C.byref(p), _ptr(dlogits), 0 if dlogits is None else pitch(dlogits),
+                            loss.data_ptr(), workspace.data_ptr(), workspace.numel(), handle)
+    if rc != 0:
+        _check(rc)
+    return loss, logp, dlogits
+
+
+def alch_stack_backward_policy(shape, batch, saved_layers, weights_layers, X_final, g_final, W_lm, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
+                               lora_layers=None, rank=0, scale=1.0, want=WEIGHT_KEYS, want_head=None, lora_grads_layers=None, grads_layers=None,
+                               accumulate=False, hooks=None, workspace=None, stream=None, head_grads=None):
+    """Stack backward under the clipped policy loss.  items: a PolicyItems with rows.  lora_layers: None, or per layer a dict
+    projection -> (A, B).  Returns the dict of alch_stack_backward, its loss the four values of alch_policy_loss, plus logp (device [n_items])."""
+    L = lib()
+    dev, index = X_final.device, X_final.get_device()
+    handle = _place(index, stream)
+    n_layers, vocab, rank = len(saved_layers), W_lm.shape[0], rank if lora_layers is not None else 0
+    if items.rows is None or items.index != index:
+        raise ValueError("items: a PolicyItems with rows on %s is needed" % dev)
+    if grads_layers is None:
+        grads_layers = [{"d" + k: _gradient(w[k], accumulate, stream) for k in want} for w in weights_layers]
+    n = max(n_layers, 1)
+    SA = (CSaved * n)(*[_saved_struct(s_, 0) for s_ in saved_layers])
+    WA = (CWeights * n)(*[_weights_struct(w, 0) for w in weights_layers])
+    GA = (CWgrads * n)(*[_wgrads_struct(g, accumulate) for g in grads_layers])
+    LA = LG = None
+    if lora_layers is not None:
+        if lora_grads_layers is None:
+            lora_grads_layers = [{"d" + m + p_: _gradient(t, accumulate, stream) for p_, ab in lo.items() for m, t in zip("AB", ab)} for lo in lora_layers]
+        pairs = [_lora_structs(lo, lg, rank, scale, accumulate) for lo, lg in zip(lora_layers, lora_grads_layers)]
+        LA, LG = (CLora * n)(*[p_[0] for p_ in pairs]), (CLoraGrads * n)(*[p_[1] for p_ in pairs])
+        need = L.alch_stack_backward_lora_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen, rank)
+    else:
+        need = L.alch_stack_backward_workspace_bytes(C.byref(shape), n_layers, vocab, batch.total_tokens, batch.max_seqlen)
+    dg_final, dW_lm = _head_grads(head_grads, want_head, True, g_final, W_lm, accumulate, stream)
+    dX_embed = _empty(X_final.shape, X_final.dtype, dev, stream)
+    loss, logp = _empty((4,), torch.float32, dev, stream), _empty((items.n_items,), torch.float32, dev, stream)
+    ws = workspace if workspace is not None else _empty((max(int(need), 256),), torch.uint8, dev, stream)
+    p = CPolicy(items.n_items, clip_low, clip_high, kl_coef, *items.words, logp.data_ptr())
+    hk = None
+    if hooks is not None:
+        ready, preempt = hooks
+        hk = CHooks(HOOK_FN(ready) if ready else HOOK_FN(), HOOK_FN(preempt) if preempt else HOOK_FN(), None)
+    _check(L.alch_stack_backward_policy(C.byref(shape), n_layers, vocab, C.byref(batch.c), SA, WA, LA, _ptr(X_final), _ptr(g_final), _ptr(W_lm),
+                                        C.byref(p), GA, LG, _ptr(dg_final), _ptr(dW_lm), _ptr(dX_embed), _ptr(loss),
+                                        C.byref(hk) if hk else None, _ptr(ws), ws.numel(), handle))
+    layers = [dict(g, **(lora_grads_layers[i] if lora_grads_layers is not None else {})) for i, g in enumerate(grads_layers)]
+    return dict(loss=loss, logp=logp, dX_embed=dX_embed, dg_final=dg_final, dW_lm=dW_lm, layers=layers)
+
+
 def alch_gemm(M, N, terms, a_kmajor, b_kmajor, out=None, accumulate=False, stream=None, workspace=None):
     """terms: list of (A, B, K) device tensors (2-D, last dim contiguous).  Returns C [M, N].  workspace: optional
     uint8 device tensor of lib().alch_gemm_workspace_bytes() bytes (lets the last round of tiles be split)."""
@@ -835,6 +1097,45 @@ class AdamwList(_TensorTable):
         self._upload()
 
 
+ADAMW8_BLOCK = 64  # elements of a tensor that share the scale of a moment
+
+
+def adamw8_state(shape, device="cuda"):
+    """The moment of a new run for a parameter of this shape (or of so many elements): (codes, scales), both of zeros."""
+    n = shape if isinstance(shape, int) else torch.Size(shape).numel()
+    return torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(-(-n // ADAMW8_BLOCK), dtype=torch.uint8, device=device)
+
+
+class Adamw8List(_TensorTable):
+    """The tensors of alch_adamw8_step: per parameter its gradient (same type), its moments m and v as pairs (codes, scales) of uint8 tensors
+    (see adamw8_state), in masters its fp32 master copy or None, and its weight decay (one number for all, or one each).  first: the
+    number of each parameter's first element, which its random bits go by; None: counted through the list, every parameter from a multiple of 64
+    on.  device: where a list without tensors belongs."""
+
+    def __init__(self, params, grads, m, v, masters=None, weight_decay=0.0, first=None, device="cuda"):
+        params, grads, m, v = list(params), list(grads), list(m), list(v)
+        n = len(params)
+        masters = [None] * n if masters is None else list(masters)
+        decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        blocks = [-(-p.numel() // ADAMW8_BLOCK) for p in params]
+        first = [ADAMW8_BLOCK * b for b in itertools.accumulate([0] + blocks[:-1])][:n] if first is None else [int(f) for f in first]
+        for name, l in (("grads", grads), ("m", m), ("v", v), ("masters", masters), ("weight_decay", decay), ("first", first)):
+            if len(l) != n:
+                raise ValueError("%d %s for %d parameters" % (len(l), name, n))
+        if any(not 0 <= f <= 1 << 62 for f in first):
+            raise ValueError("first: numbers from 0 to 2^62")
+        super().__init__(Adamw8Tensor, params, device)
+        for i, p in enumerate(params):
+            dt, shape, u8 = p.dtype, p.shape, torch.uint8
+            at = dict(param=self._take(p, "params", i, dt, written=True), grad=self._take(grads[i], "grads", i, dt, shape),
+                      master=None if masters[i] is None else self._take(masters[i], "masters", i, torch.float32, shape, written=True))
+            for name, (codes, scales) in (("m", m[i]), ("v", v[i])):
+                at[name] = self._take(codes, name, i, u8, shape, written=True)
+                at[name + "_scale"] = self._take(scales, name + " scales", i, u8, (blocks[i],), written=True)
+            self.rows.append(Adamw8Tensor(n=p.numel(), first=first[i], weight_decay=decay[i], dtype=_code(dt), **at))
+        self._upload()
+
+
 def grad_clip_workspace_bytes():
     return lib().alch_grad_clip_workspace_bytes()
 
@@ -873,6 +1174,23 @@ def alch_adamw_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, sched
     p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
     tensors._used(stream, handle)
     _check(lib().alch_adamw_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), handle))
+
+
+def alch_adamw8_step(tensors, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, schedule=None, grad_factor=None, stream=None):
+    """One AdamW update of an Adamw8List, in place: alch_adamw_step with both moments in 8 bits, rounded at random.  seed: 32 bits; together with
+    the step (or the schedule's) it chooses the random bits, so that a run with the same seed repeats itself."""
+    dev = tensors.index
+    handle = _place(dev, stream)
+    if schedule is not None:
+        _check_dense(schedule, "schedule", torch.float32, dev, (2,))
+    if grad_factor is not None:
+        _check_dense(grad_factor, "grad_factor", torch.float32, dev, (1,))
+    _check_int32("step", step)
+    if not 0 <= seed < 1 << 32:
+        raise ValueError("seed = %s: a number of 32 bits" % (seed,))
+    p = CAdamw(lr, beta1, beta2, eps, step, _ptr(schedule), _ptr(grad_factor))
+    tensors._used(stream, handle)
+    _check(lib().alch_adamw8_step(tensors.n, tensors.dev_ptr, tensors.host_ptr, C.byref(p), seed, handle))
 
 
 def alch_trace_enable(on):

@@ -103,6 +103,18 @@ static int check_batch(const alch_batch* b) {
         if ((p) && !aligned16(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is not 16-byte aligned", name); \
     } while (0)
 
+#define REQUIRE_WORDS(p, name)                                                                                                \
+    do {                                                                                                                      \
+        if (!(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is NULL", name);                                                      \
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(ALCH_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);         \
+    } while (0)
+
+// Whether two buffers share memory.
+static bool overlap(const void* a, unsigned long long a_bytes, const void* b, unsigned long long b_bytes) {
+    const unsigned long long x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
 // ---- workspace plans -----------------------------------------------------------------------
 
 struct LayerBwdPlan {
@@ -770,6 +782,192 @@ static int check_tensor_ptr(const void* p, int i, const char* name) {
     return ALCH_OK;
 }
 
+// ---- checks of the scored tokens of a head, and of records in 8 bits ------------------------------
+
+// The scored tokens of a DPO or policy head.
+static int check_items(const char* name, const alch_layer_shape* shape, const alch_batch* batch, int n, const int32_t* row, const int32_t* row_host,
+                       bool others) {
+    if (n < 0) return fail(ALCH_ERR_INVALID_ARG, "%s: negative n_items", name);
+    if (n > batch->total_tokens) return fail(ALCH_ERR_SHAPE, "%s: %d items > %d tokens", name, n, batch->total_tokens);
+    if (n > 0 && (!row || !row_host || !others)) return fail(ALCH_ERR_INVALID_ARG, "%s: an array of the items, or item_row_host, is NULL", name);
+    if (((size_t)shape->hidden * dtype_size(shape->dtype)) % 16)
+        return fail(ALCH_ERR_UNSUPPORTED, "%s: a hidden row of %d elements is not a multiple of 16 bytes", name, shape->hidden);
+    for (int m = 0; m < n; ++m) {
+        const int r = row_host[m];
+        if (r < 0 || r >= batch->total_tokens) return fail(ALCH_ERR_SHAPE, "%s: item_row[%d] = %d outside the batch", name, m, r);
+        if (m > 0 && r < row_host[m - 1]) return fail(ALCH_ERR_SHAPE, "%s: item_row is not ascending at item %d", name, m);
+    }
+    return ALCH_OK;
+}
+
+static int check_policy(const alch_policy* p) {
+    if (!p) return fail(ALCH_ERR_INVALID_ARG, "policy is NULL");
+    if (p->n_items < 0) return fail(ALCH_ERR_INVALID_ARG, "policy: negative n_items");
+    if (!(p->clip_low >= 0.f) || !(p->clip_high >= 0.f)) return fail(ALCH_ERR_INVALID_ARG, "policy: clip_low %g, clip_high %g", (double)p->clip_low, (double)p->clip_high);
+    if (!(p->kl_coef >= 0.f) || !(p->kl_coef < INFINITY)) return fail(ALCH_ERR_INVALID_ARG, "policy: kl_coef %g", (double)p->kl_coef);
+    if (p->n_items > 0) {
+        REQUIRE_WORDS(p->label, "policy.label"); REQUIRE_WORDS(p->old_logp, "policy.old_logp");
+        REQUIRE_WORDS(p->advantage, "policy.advantage"); REQUIRE_WORDS(p->weight, "policy.weight");
+        if (p->kl_coef != 0.f && !p->ref_logp) return fail(ALCH_ERR_INVALID_ARG, "policy: kl_coef %g without ref_logp", (double)p->kl_coef);
+    }
+    if (p->ref_logp) REQUIRE_WORDS(p->ref_logp, "policy.ref_logp");
+    if (p->logp_out) REQUIRE_WORDS(p->logp_out, "policy.logp_out");
+    return ALCH_OK;
+}
+
+// Memory of a call: what is written may not share any with the rest.
+struct Memory {
+    const void* p;  // NULL: not given
+    unsigned long long bytes;
+    const char* name;
+    int index;  // >= 0: of the tensor or stream of this number
+    bool written;
+};
+static int check_apart(const Memory* of, size_t n) {
+    const auto said = [](const Memory& m, char (&text)[64]) {
+        if (m.index >= 0) snprintf(text, sizeof(text), "%d: %s", m.index, m.name);
+        else snprintf(text, sizeof(text), "%s", m.name);
+        return text;
+    };
+    for (size_t i = 0; i < n; ++i) {
+        if (!of[i].p || of[i].bytes == 0 || !of[i].written) continue;
+        for (size_t j = 0; j < n; ++j) {
+            if (j == i || !of[j].p || of[j].bytes == 0 || (of[j].written && j < i)) continue;
+            if (overlap(of[i].p, of[i].bytes, of[j].p, of[j].bytes)) {
+                char x[64], y[64];
+                return fail(ALCH_ERR_INVALID_ARG, "%s overlaps %s", said(of[i], x), said(of[j], y));
+            }
+        }
+    }
+    return ALCH_OK;
+}
+// What a policy loss takes and gives beside logits, gradients and workspace.
+static void policy_memory(const alch_policy* p, const float* loss_out, Memory (&of)[7]) {
+    const unsigned long long bytes = 4ull * p->n_items;
+    const Memory all[7] = {{p->label, bytes, "policy.label", -1, false}, {p->old_logp, bytes, "policy.old_logp", -1, false},
+                           {p->advantage, bytes, "policy.advantage", -1, false}, {p->weight, bytes, "policy.weight", -1, false},
+                           {p->ref_logp, bytes, "policy.ref_logp", -1, false}, {p->logp_out, bytes, "policy.logp_out", -1, true},
+                           {loss_out, 4 * sizeof(float), "loss_out", -1, true}};
+    std::copy(all, all + 7, of);
+}
+
+static constexpr int64_t kMaxQ8Width = (int64_t)1 << 31, kMaxQ8Rows = (int64_t)1 << 31;
+
+// A tensor of either direction: `rows` of it and `held` of the codes.
+template <typename Entry>
+static int check_q8(int k, const char* what, const Entry& s, const void* tensor, const char* name, size_t stride, int64_t rows, int64_t held) {
+    if (s.dtype != ALCH_F32 && s.dtype != ALCH_BF16) return fail(ALCH_ERR_INVALID_ARG, "%s %d: bad dtype %d", what, k, s.dtype);
+    if (s.width <= 0 || s.width > kMaxQ8Width) return fail(ALCH_ERR_SHAPE, "%s %d: width %lld", what, k, (long long)s.width);
+    const size_t E = dtype_size((alch_dtype)s.dtype);
+    if (stride < s.width * E || stride % E || stride > (size_t)1 << 40)
+        return fail(ALCH_ERR_SHAPE, "%s %d: rows %zu bytes apart, of %lld elements", what, k, stride, (long long)s.width);
+    if ((rows > 0 && !tensor) || (held > 0 && (!s.codes || !s.scales))) return fail(ALCH_ERR_INVALID_ARG, "%s %d: %s, codes or scales is NULL", what, k, name);
+    if (reinterpret_cast<uintptr_t>(tensor) % E) return fail(ALCH_ERR_INVALID_ARG, "%s %d: %s is not aligned to its elements", what, k, name);
+    if (!aligned16(s.codes) || !aligned16(s.scales)) return fail(ALCH_ERR_INVALID_ARG, "%s %d: codes or scales is not 16-byte aligned", what, k);
+    return ALCH_OK;
+}
+static unsigned long long q8_scale_bytes(int64_t width) { return 4ull * ((width + ALCH_Q8_GROUP - 1) / ALCH_Q8_GROUP); }
+static unsigned long long span(int64_t rows, size_t stride, unsigned long long row) { return rows > 0 ? (unsigned long long)(rows - 1) * stride + row : 0; }
+
+static int check_q8_streams(int32_t n, const alch_q8_stream* streams, int T, int64_t capacity, std::vector<Memory>& of) {
+    if (n < 0) return fail(ALCH_ERR_INVALID_ARG, "n_streams < 0");
+    if (n > 0 && !streams) return fail(ALCH_ERR_INVALID_ARG, "streams is NULL");
+    if (capacity < 0) return fail(ALCH_ERR_INVALID_ARG, "dst_capacity_rows < 0");
+    const int64_t rows = std::min<int64_t>(T, capacity);  // (more are never written)
+    for (int k = 0; k < n; ++k) {
+        const alch_q8_stream& s = streams[k];
+        ALCH_TRY(check_q8(k, "stream", s, s.src, "src", s.src_row_stride_bytes, T, capacity));
+        of.push_back({s.src, span(T, s.src_row_stride_bytes, s.width * dtype_size((alch_dtype)s.dtype)), "src", k, false});
+        of.push_back({s.codes, (unsigned long long)rows * s.width, "codes", k, true});
+        of.push_back({s.scales, (unsigned long long)rows * q8_scale_bytes(s.width), "scales", k, true});
+    }
+    return ALCH_OK;
+}
+
+// (the lists of memory are std::vectors: an exception does not leave the library)
+static int check_pack_q8(const alch_batch* batch, const uint8_t* keep_mask, int32_t n_streams, const alch_q8_stream* streams, int64_t capacity,
+                         const int32_t* kept_index, const int32_t* cu_kept, const int32_t* status, const void* workspace, size_t workspace_bytes) try {
+    ALCH_TRY(check_batch(batch));
+    const int T = batch->total_tokens;
+    if (T > 0 && !keep_mask) return fail(ALCH_ERR_INVALID_ARG, "keep_mask is NULL");
+    OPTIONAL_PTR(keep_mask, "keep_mask");
+    std::vector<Memory> of;
+    ALCH_TRY(check_q8_streams(n_streams, streams, T, capacity, of));
+    if (capacity > 0) REQUIRE_WORDS(kept_index, "kept_index");
+    REQUIRE_WORDS(cu_kept, "cu_kept"); REQUIRE_WORDS(status, "n_kept_and_status");
+    const size_t need = pack_workspace_bytes(T);
+    if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    REQUIRE_WORDS(workspace, "workspace");
+    of.push_back({keep_mask, (unsigned long long)T, "keep_mask", -1, false});
+    of.push_back({batch->cu_seqlens, 4ull * (batch->n_seqs + 1), "cu_seqlens", -1, false});
+    of.push_back({kept_index, 4ull * std::min<int64_t>(T, capacity), "kept_index", -1, true});
+    of.push_back({cu_kept, 4ull * (batch->n_seqs + 1), "cu_kept", -1, true});
+    of.push_back({status, 8, "n_kept_and_status", -1, true});
+    of.push_back({workspace, need, "workspace", -1, true});
+    return check_apart(of.data(), of.size());
+} catch (...) {
+    return fail(ALCH_ERR_UNSUPPORTED, "no host memory for %d streams", n_streams);
+}
+
+static int check_gather_q8(const alch_batch* batch, int32_t n_streams, const alch_q8_stream* streams, int64_t capacity, const int32_t* kept_index,
+                           const int32_t* status) try {
+    ALCH_TRY(check_batch(batch));
+    const int T = batch->total_tokens;
+    std::vector<Memory> of;
+    ALCH_TRY(check_q8_streams(n_streams, streams, T, capacity, of));
+    if (!kept_index != !status) return fail(ALCH_ERR_INVALID_ARG, "kept_index and n_kept_and_status must be given together");
+    if (kept_index) {
+        REQUIRE_WORDS(kept_index, "kept_index"); REQUIRE_WORDS(status, "n_kept_and_status");
+        of.push_back({kept_index, 4ull * std::min<int64_t>(T, capacity), "kept_index", -1, false});
+        of.push_back({status, 8, "n_kept_and_status", -1, false});
+    } else if (capacity < T) {
+        return fail(ALCH_ERR_SHAPE, "dst_capacity_rows %lld < %d tokens, all of which are kept", (long long)capacity, T);
+    }
+    return check_apart(of.data(), of.size());
+} catch (...) {
+    return fail(ALCH_ERR_UNSUPPORTED, "no host memory for %d streams", n_streams);
+}
+
+static int check_expand(int64_t n_rows, const int32_t* rows, int64_t n_src_rows, int32_t n, const alch_q8_tensor* tensors) try {
+    if (n_rows < 0 || n_src_rows < 0 || n < 0) return fail(ALCH_ERR_INVALID_ARG, "negative n_rows / n_src_rows / n_tensors");
+    if (n_rows > kMaxQ8Rows || n_src_rows > kMaxQ8Rows) return fail(ALCH_ERR_UNSUPPORTED, "more than 2^31 rows");
+    if (n > 0 && !tensors) return fail(ALCH_ERR_INVALID_ARG, "tensors is NULL");
+    if (!rows && n_rows > n_src_rows) return fail(ALCH_ERR_SHAPE, "%lld rows of a record of %lld", (long long)n_rows, (long long)n_src_rows);
+    std::vector<Memory> of;
+    if (rows) {
+        REQUIRE_WORDS(rows, "rows");
+        of.push_back({rows, 4ull * n_rows, "rows", -1, false});
+    }
+    for (int k = 0; k < n; ++k) {
+        const alch_q8_tensor& t = tensors[k];
+        ALCH_TRY(check_q8(k, "tensor", t, t.dst, "dst", t.dst_row_stride_bytes, n_rows, n_src_rows));
+        of.push_back({t.codes, (unsigned long long)n_src_rows * t.width, "codes", k, false});
+        of.push_back({t.scales, (unsigned long long)n_src_rows * q8_scale_bytes(t.width), "scales", k, false});
+    }
+    // Column slices of one buffer share its span and no element of it: for those that are as far apart as one another, their columns count.
+    for (int k = 0; k < n; ++k) {
+        const alch_q8_tensor& t = tensors[k];
+        const unsigned long long row = t.width * dtype_size((alch_dtype)t.dtype), all = span(n_rows, t.dst_row_stride_bytes, row);
+        if (all == 0) continue;
+        for (const Memory& m : of)
+            if (m.p && m.bytes && overlap(t.dst, all, m.p, m.bytes))
+                return m.index >= 0 ? fail(ALCH_ERR_INVALID_ARG, "%d: dst overlaps %d: %s", k, m.index, m.name) : fail(ALCH_ERR_INVALID_ARG, "%d: dst overlaps %s", k, m.name);
+        for (int j = 0; j < k; ++j) {
+            const alch_q8_tensor& u = tensors[j];
+            const unsigned long long other = u.width * dtype_size((alch_dtype)u.dtype);
+            if (!overlap(t.dst, all, u.dst, span(n_rows, u.dst_row_stride_bytes, other))) continue;
+            const size_t pitch = t.dst_row_stride_bytes;
+            const uintptr_t x = reinterpret_cast<uintptr_t>(t.dst), y = reinterpret_cast<uintptr_t>(u.dst);
+            const unsigned long long ahead = x < y ? (y - x) % pitch : (x - y) % pitch;  // of the later one's rows before the earlier one's
+            const bool apart = pitch == u.dst_row_stride_bytes && (x < y ? row <= ahead && ahead + other <= pitch : other <= ahead && ahead + row <= pitch);
+            if (!apart) return fail(ALCH_ERR_INVALID_ARG, "%d: dst overlaps %d: dst", j, k);
+        }
+    }
+    return ALCH_OK;
+} catch (...) {
+    return fail(ALCH_ERR_UNSUPPORTED, "no host memory for %d tensors", n);
+}
+
 }  // namespace alch
 
 using namespace alch;
@@ -945,6 +1143,31 @@ int alch_capture_gather(const alch_batch* batch, int32_t n_streams, const alch_s
                               static_cast<hipStream_t>(hip_stream));
 }
 
+// ---- records in 8 bits -------------------------------------------------------------------------
+int alch_capture_pack_q8(const alch_batch* batch, const uint8_t* keep_mask, int32_t n_streams, const alch_q8_stream* streams,
+                         int64_t dst_capacity_rows, int32_t* kept_index, int32_t* cu_kept, int32_t* n_kept_and_status, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_pack_q8(batch, keep_mask, n_streams, streams, dst_capacity_rows, kept_index, cu_kept, n_kept_and_status, workspace, workspace_bytes));
+    return launch_pack_q8(keep_mask, batch->total_tokens, batch->cu_seqlens, batch->n_seqs, n_streams, streams, dst_capacity_rows, kept_index,
+                          cu_kept, n_kept_and_status, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+int alch_capture_gather_q8(const alch_batch* batch, int32_t n_streams, const alch_q8_stream* streams, int64_t dst_capacity_rows,
+                           const int32_t* kept_index, const int32_t* n_kept_and_status, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_gather_q8(batch, n_streams, streams, dst_capacity_rows, kept_index, n_kept_and_status));
+    return launch_gather_q8(batch->total_tokens, n_streams, streams, dst_capacity_rows, kept_index, n_kept_and_status,
+                            static_cast<hipStream_t>(hip_stream));
+}
+
+int alch_record_expand(int64_t n_rows, const int32_t* rows, int64_t n_src_rows, int32_t n_tensors, const alch_q8_tensor* tensors,
+                       void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_expand(n_rows, rows, n_src_rows, n_tensors, tensors));
+    return launch_expand(n_rows, rows, n_src_rows, n_tensors, tensors, static_cast<hipStream_t>(hip_stream));
+}
+
 size_t alch_layer_backward_workspace_bytes(const alch_layer_shape* shape, int32_t total_tokens, int32_t max_seqlen) {
     (void)max_seqlen;
     if (!shape || check_shape(shape) != ALCH_OK || total_tokens < 0) return 0;
@@ -1026,13 +1249,14 @@ size_t alch_stack_backward_workspace_bytes(const alch_layer_shape* shape, int32_
     return plan_stack(*shape, vocab, total_tokens, nullptr, 0).bytes;
 }
 
-// The head is cross-entropy on `labels` (dpo == nullptr) or DPO on the scored items of `dpo`.
+// The head is cross-entropy on `labels` (dpo and policy nullptr), or DPO or the policy loss on their scored items.
 static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, int32_t vocab, const alch_batch* batch,
                                const alch_saved* saved, const alch_weights* weights, const alch_lora* lora,
                                const void* X_final, const void* g_final, const void* W_lm, const int32_t* labels,
                                const uint8_t* loss_mask, const alch_wgrads* wgrads, const alch_lora_grads* lora_grads,
                                void* dg_final, void* dW_lm, void* dX_embed, float* loss_out, const alch_hooks* hooks,
-                               void* workspace, size_t workspace_bytes, void* hip_stream, const alch_dpo* dpo = nullptr) {
+                               void* workspace, size_t workspace_bytes, void* hip_stream, const alch_dpo* dpo = nullptr,
+                               const alch_policy* policy = nullptr) {
     clear_error();
     ALCH_TRY(check_shape(shape));
     ALCH_TRY(check_batch(batch));
@@ -1050,22 +1274,21 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
     const int rank = (lora && n_layers > 0) ? lora[0].rank : 0;
     REQUIRE_ACT(X_final, "X_final", batch->total_tokens); REQUIRE_PTR(g_final, "g_final"); REQUIRE_PTR(W_lm, "W_lm");
     REQUIRE_ACT(dX_embed, "dX_embed", batch->total_tokens);
-    if ((!dpo && batch->total_tokens > 0 && !labels) || !loss_out) return fail(ALCH_ERR_INVALID_ARG, "labels / loss_out is NULL");
+    if ((!dpo && !policy && batch->total_tokens > 0 && !labels) || !loss_out) return fail(ALCH_ERR_INVALID_ARG, "labels / loss_out is NULL");
     OPTIONAL_PTR(dg_final, "dg_final"); OPTIONAL_PTR(dW_lm, "dW_lm");
     if (dpo) {
         if (dpo->n_items < 0 || dpo->n_pairs < 0) return fail(ALCH_ERR_INVALID_ARG, "dpo: negative n_items / n_pairs");
-        if (dpo->n_items > batch->total_tokens) return fail(ALCH_ERR_SHAPE, "dpo: %d items > %d tokens", dpo->n_items, batch->total_tokens);
         if (2 * (long long)dpo->n_pairs > batch->total_tokens) return fail(ALCH_ERR_SHAPE, "dpo: %d pairs need more slots than there are tokens", dpo->n_pairs);
-        if (dpo->n_items > 0 && (!dpo->item_row || !dpo->item_label || !dpo->item_slot || !dpo->item_row_host))
-            return fail(ALCH_ERR_INVALID_ARG, "dpo: item_row / item_label / item_slot / item_row_host is NULL");
         if (dpo->n_pairs > 0 && !dpo->ref_logp) return fail(ALCH_ERR_INVALID_ARG, "dpo: ref_logp is NULL");
-        if (((size_t)shape->hidden * dtype_size(shape->dtype)) % 16)
-            return fail(ALCH_ERR_UNSUPPORTED, "dpo: a hidden row of %d elements is not a multiple of 16 bytes", shape->hidden);
-        for (int m = 0; m < dpo->n_items; ++m) {
-            const int r = dpo->item_row_host[m];
-            if (r < 0 || r >= batch->total_tokens) return fail(ALCH_ERR_SHAPE, "dpo: item_row[%d] = %d outside the batch", m, r);
-            if (m > 0 && r < dpo->item_row_host[m - 1]) return fail(ALCH_ERR_SHAPE, "dpo: item_row is not ascending at item %d", m);
-        }
+        ALCH_TRY(check_items("dpo", shape, batch, dpo->n_items, dpo->item_row, dpo->item_row_host, dpo->item_label && dpo->item_slot));
+    }
+    if (policy) {
+        ALCH_TRY(check_policy(policy));
+        ALCH_TRY(check_items("policy", shape, batch, policy->n_items, policy->item_row, policy->item_row_host, true));
+        REQUIRE_WORDS(loss_out, "loss_out");
+        Memory of[7];
+        policy_memory(policy, loss_out, of);
+        ALCH_TRY(check_apart(of, 7));
     }
     const size_t need = plan_stack(*shape, vocab, batch->total_tokens, nullptr, 0, rank).bytes;
     if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
@@ -1096,14 +1319,15 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
     };
 
     bool compact_head = false;
-    if (dpo) {
-        // DPO head: the stack-output rows of the scored tokens are gathered into [n_items, H]; pass 1 turns each
-        // chunk of their logits into log-probabilities, the slot sums give z, the loss and a weight per slot;
-        // pass 2 forms the logits gradient (recomputing the logits unless one chunk holds them all) and the two
-        // products; the row gradients are summed back into a zero-filled [T, H] (a row may score several tokens).
-        const int M = dpo->n_items, n_slots = 2 * dpo->n_pairs;
+    if (dpo || policy) {
+        // Head on scored tokens: their stack-output rows are gathered into [n_items, H].  DPO: pass 1 turns each chunk of their logits
+        // into log-probabilities, the slot sums give z, the loss and a weight per slot; pass 2 forms the logits gradient (recomputing
+        // the logits unless one chunk holds them all) and the two products.  Policy loss: an item's gradient needs its own row alone, one
+        // pass.  The row gradients are summed back into a zero-filled [T, H] (a row may score several tokens).
+        const int M = dpo ? dpo->n_items : policy->n_items, n_slots = dpo ? 2 * dpo->n_pairs : 0;
+        const int32_t* item_row = dpo ? dpo->item_row : policy->item_row;
         ALCH_TRY(launch_rmsnorm_fwd(dt, X_final, g_final, p.Hf, T, H, s.rms_eps, st));
-        if (M > 0) ALCH_TRY(launch_scatter_rows(p.Hf, dpo->item_row, p.h_Hf, M, (size_t)H * E, st));  // h_Hf[m] = Hf[item_row[m]]
+        if (M > 0) ALCH_TRY(launch_scatter_rows(p.Hf, item_row, p.h_Hf, M, (size_t)H * E, st));  // h_Hf[m] = Hf[item_row[m]]
         const bool one_chunk = M <= kHeadChunkRows;
         auto logits_of = [&](int r0, int rows) {
             GemmDesc d = gemm_ws(dt, rows, vocab, true, true);
@@ -1111,19 +1335,25 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
             add_out(d, p.logits, 0, vocab);
             return launch_gemm(d, st);
         };
-        for (int r0 = 0; r0 < M; r0 += kHeadChunkRows) {
-            const int rows = M - r0 < kHeadChunkRows ? M - r0 : kHeadChunkRows;
-            ALCH_TRY(logits_of(r0, rows));
-            ALCH_TRY(launch_dpo_logp(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, p.dpo_logp + r0, p.dpo_logz + r0, st));
+        if (dpo) {
+            for (int r0 = 0; r0 < M; r0 += kHeadChunkRows) {
+                const int rows = M - r0 < kHeadChunkRows ? M - r0 : kHeadChunkRows;
+                ALCH_TRY(logits_of(r0, rows));
+                ALCH_TRY(launch_dpo_logp(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, p.dpo_logp + r0, p.dpo_logz + r0, st));
+            }
+            ALCH_TRY(launch_dpo_weights(p.dpo_logp, dpo->item_slot, dpo->item_label, M, vocab, dpo->ref_logp, dpo->n_pairs,
+                                        dpo->beta, p.dpo_pi, p.dpo_w, dpo->z_out, loss_out, st));
         }
-        ALCH_TRY(launch_dpo_weights(p.dpo_logp, dpo->item_slot, dpo->item_label, M, vocab, dpo->ref_logp, dpo->n_pairs,
-                                    dpo->beta, p.dpo_pi, p.dpo_w, dpo->z_out, loss_out, st));
+        const long long stride = p.dpo_logz - p.dpo_logp;  // (the four arrays of the plan are equally far apart: the policy loss's terms)
         bool first = true;
         for (int r0 = 0; r0 < M; r0 += kHeadChunkRows) {
             const int rows = M - r0 < kHeadChunkRows ? M - r0 : kHeadChunkRows;
-            if (!one_chunk) ALCH_TRY(logits_of(r0, rows));
-            ALCH_TRY(launch_dpo_grad(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, dpo->item_slot + r0,
-                                     p.dpo_logz + r0, p.dpo_w, n_slots, st));
+            if (policy || !one_chunk) ALCH_TRY(logits_of(r0, rows));
+            if (dpo)
+                ALCH_TRY(launch_dpo_grad(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, dpo->item_slot + r0,
+                                         p.dpo_logz + r0, p.dpo_w, n_slots, st));
+            else
+                ALCH_TRY(launch_policy_rows(dt, p.logits, vocab, rows, vocab, *policy, r0, p.logits, vocab, p.dpo_logp, stride, st));
             {  // gradient of the gathered rows = dlogits W_lm
                 GemmDesc d = gemm_ws(dt, rows, H, true, false);
                 add_seg(d, p.logits, vocab, W_lm, H, vocab);
@@ -1145,7 +1375,8 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
             add_out(d, dW_lm, 0, H);
             ALCH_TRY(launch_gemm_generic(d, st));
         }
-        ALCH_TRY(launch_dpo_scatter(dt, p.h_dHf, dpo->item_row, M, p.dHf, T, H, st));
+        if (policy) ALCH_TRY(launch_policy_sums(p.dpo_logp, stride, M, loss_out, st));
+        ALCH_TRY(launch_dpo_scatter(dt, p.h_dHf, item_row, M, p.dHf, T, H, st));
     } else {
         // LM head + cross-entropy in row chunks: logits -> dlogits in place, never stored whole.
         // With a loss mask (bf16, matrix-core shapes) only the counted tokens -- label >= 0 and mask byte nonzero --
@@ -1278,6 +1509,63 @@ int alch_stack_backward_dpo(const alch_layer_shape* shape, int32_t n_layers, int
     return stack_backward_impl(shape, n_layers, vocab, batch, saved, weights, lora, X_final, g_final, W_lm, nullptr,
                                nullptr, wgrads, lora ? lora_grads : nullptr, dg_final, dW_lm, dX_embed, loss_out, hooks,
                                workspace, workspace_bytes, hip_stream, dpo);
+}
+
+int alch_stack_backward_policy(const alch_layer_shape* shape, int32_t n_layers, int32_t vocab, const alch_batch* batch,
+                               const alch_saved* saved, const alch_weights* weights, const alch_lora* lora, const void* X_final,
+                               const void* g_final, const void* W_lm, const alch_policy* policy, const alch_wgrads* wgrads,
+                               const alch_lora_grads* lora_grads, void* dg_final, void* dW_lm, void* dX_embed, float* loss_out,
+                               const alch_hooks* hooks, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!policy) {
+        clear_error();
+        return fail(ALCH_ERR_INVALID_ARG, "policy is NULL");
+    }
+    return stack_backward_impl(shape, n_layers, vocab, batch, saved, weights, lora, X_final, g_final, W_lm, nullptr,
+                               nullptr, wgrads, lora ? lora_grads : nullptr, dg_final, dW_lm, dX_embed, loss_out, hooks,
+                               workspace, workspace_bytes, hip_stream, nullptr, policy);
+}
+
+static constexpr int kMaxPolicyVocab = 1 << 28;
+
+size_t alch_policy_loss_workspace_bytes(int32_t n_items, int32_t vocab) {
+    if (n_items < 0 || vocab <= 0 || vocab > kMaxPolicyVocab) return 0;
+    return policy_loss_workspace_bytes(n_items, vocab);
+}
+
+int alch_policy_loss(alch_dtype dtype, int32_t vocab, const void* logits, int64_t ld, const alch_policy* policy, void* dlogits,
+                     int64_t ld_grad, float* loss_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    clear_error();
+    if (dtype != ALCH_F32 && dtype != ALCH_BF16) return fail(ALCH_ERR_INVALID_ARG, "bad dtype %d", (int)dtype);
+    if (vocab <= 0) return fail(ALCH_ERR_SHAPE, "vocab <= 0");
+    if (vocab > kMaxPolicyVocab) return fail(ALCH_ERR_UNSUPPORTED, "vocab %d > 2^28", vocab);
+    ALCH_TRY(check_policy(policy));
+    REQUIRE_WORDS(loss_out, "loss_out");
+    const int n = policy->n_items;
+    const size_t need = policy_loss_workspace_bytes(n, vocab);
+    if (!workspace || workspace_bytes < need) return fail(ALCH_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    if (!aligned16(workspace)) return fail(ALCH_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+    unsigned long long read = 0, written = 0;
+    if (n > 0) {
+        REQUIRE_PTR(logits, "logits"); OPTIONAL_PTR(dlogits, "dlogits");
+        if (ld < vocab || (dlogits && ld_grad < vocab)) return fail(ALCH_ERR_SHAPE, "rows %lld and %lld elements apart, vocab %d", (long long)ld, (long long)ld_grad, vocab);
+        const long long most = 1LL << 50;  // (elements of a matrix)
+        if (ld > most / n || (dlogits && ld_grad > most / n)) return fail(ALCH_ERR_UNSUPPORTED, "logits of more than 2^50 elements");
+        read = ((unsigned long long)(n - 1) * ld + vocab) * dtype_size(dtype);
+        written = dlogits ? ((unsigned long long)(n - 1) * ld_grad + vocab) * dtype_size(dtype) : 0;
+        if (dlogits == logits && ld_grad != ld) return fail(ALCH_ERR_SHAPE, "in place, and rows %lld and %lld elements apart", (long long)ld, (long long)ld_grad);
+    }
+    Memory of[10], rest[7];
+    policy_memory(policy, loss_out, rest);
+    std::copy(rest, rest + 7, of);
+    of[7] = {dlogits == logits ? nullptr : logits, read, "logits", -1, false};
+    of[8] = {dlogits, written, "dlogits", -1, true};
+    of[9] = {workspace, need, "workspace", -1, true};
+    ALCH_TRY(check_apart(of, 10));
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    float* terms = static_cast<float*>(workspace);
+    const long long stride = n > 0 ? n : 1;
+    ALCH_TRY(launch_policy_rows(dtype, logits, ld, n, vocab, *policy, 0, dlogits, ld_grad, terms, stride, st));
+    return launch_policy_sums(terms, stride, n, loss_out, st);
 }
 
 int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batch, const void* Q, const void* K,
@@ -1422,12 +1710,6 @@ static int check_embed(alch_dtype dtype, int vocab, int hidden, int n_tokens) {
     return ALCH_OK;
 }
 
-// Whether two buffers share memory.
-static bool overlap(const void* a, unsigned long long a_bytes, const void* b, unsigned long long b_bytes) {
-    const unsigned long long x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y ? y - x < a_bytes : x - y < b_bytes;
-}
-
 // What a call takes beside its tensors (p NULL: not given), none of which may share memory with theirs.
 struct Beside {
     struct Memory {
@@ -1453,12 +1735,6 @@ struct Beside {
         return ALCH_OK;
     }
 };
-
-#define REQUIRE_WORDS(p, name)                                                                                                \
-    do {                                                                                                                      \
-        if (!(p)) return fail(ALCH_ERR_INVALID_ARG, "%s is NULL", name);                                                      \
-        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(ALCH_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);         \
-    } while (0)
 
 int alch_embed_forward(alch_dtype dtype, int32_t vocab, int32_t hidden, int32_t n_tokens, const int32_t* token_ids, const void* W_embed,
                        float scale, void* X, void* hip_stream) {
@@ -1540,16 +1816,21 @@ int alch_grad_clip(int32_t n_tensors, const alch_grad_tensor* tensors, const alc
     return launch_grad_clip(n_tensors, tensors, tensors_host, max_norm, norm_out, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
-int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* tensors_host, const alch_adamw* p,
-                    void* hip_stream) {
-    clear_error();
-    ALCH_TRY(check_tensors(n_tensors, tensors, tensors_host));
+static int check_adamw(const alch_adamw* p) {
     if (!p) return fail(ALCH_ERR_INVALID_ARG, "params is NULL");
     if (!(p->beta1 >= 0 && p->beta1 < 1 && p->beta2 >= 0 && p->beta2 < 1)) return fail(ALCH_ERR_INVALID_ARG, "beta outside 0 <= beta < 1");
     if (!(p->eps >= 0)) return fail(ALCH_ERR_INVALID_ARG, "eps %g", p->eps);
     if (p->schedule) REQUIRE_WORDS(p->schedule, "schedule");
     else if (p->step < 1) return fail(ALCH_ERR_INVALID_ARG, "step %d, the first one is 1", p->step);
     if (p->grad_factor) REQUIRE_WORDS(p->grad_factor, "grad_factor");
+    return ALCH_OK;
+}
+
+int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* tensors_host, const alch_adamw* p,
+                    void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_tensors(n_tensors, tensors, tensors_host));
+    ALCH_TRY(check_adamw(p));
     for (int i = 0; i < n_tensors; ++i) {
         const alch_adamw_tensor& t = tensors_host[i];
         if (t.n == 0) continue;
@@ -1572,6 +1853,34 @@ int alch_adamw_step(int32_t n_tensors, const alch_adamw_tensor* tensors, const a
         ALCH_TRY(read.apart(i, t.v, f32, "v"));
     }
     return launch_adamw(n_tensors, tensors, tensors_host, *p, static_cast<hipStream_t>(hip_stream));
+}
+
+int alch_adamw8_step(int32_t n_tensors, const alch_adamw8_tensor* tensors, const alch_adamw8_tensor* tensors_host, const alch_adamw* p,
+                     uint32_t seed, void* hip_stream) {
+    clear_error();
+    ALCH_TRY(check_tensors(n_tensors, tensors, tensors_host));
+    ALCH_TRY(check_adamw(p));
+    const Beside read({p->schedule, 2 * sizeof(float), "schedule"}, {p->grad_factor, sizeof(float), "grad_factor"},
+                      {tensors, (unsigned long long)n_tensors * sizeof(*tensors), "tensors"});
+    for (int i = 0; i < n_tensors; ++i) {
+        const alch_adamw8_tensor& t = tensors_host[i];
+        if (t.n == 0) continue;
+        ALCH_TRY(check_tensor_ptr(t.param, i, "param"));
+        ALCH_TRY(check_tensor_ptr(t.grad, i, "grad"));
+        ALCH_TRY(check_tensor_ptr(t.m, i, "m"));
+        ALCH_TRY(check_tensor_ptr(t.v, i, "v"));
+        if (t.master) ALCH_TRY(check_tensor_ptr(t.master, i, "master"));
+        if (!t.m_scale || !t.v_scale) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: m_scale or v_scale is NULL", i);
+        if (t.first < 0 || t.first > (int64_t)1 << 62) return fail(ALCH_ERR_INVALID_ARG, "tensor %d: first %lld", i, (long long)t.first);
+        const unsigned long long n = (unsigned long long)t.n, blocks = (n + ALCH_ADAMW8_BLOCK - 1) / ALCH_ADAMW8_BLOCK;
+        ALCH_TRY(read.apart(i, t.param, n * dtype_size((alch_dtype)t.dtype), "param"));
+        ALCH_TRY(read.apart(i, t.master, 4 * n, "master"));
+        ALCH_TRY(read.apart(i, t.m, n, "m"));
+        ALCH_TRY(read.apart(i, t.v, n, "v"));
+        ALCH_TRY(read.apart(i, t.m_scale, blocks, "m_scale"));
+        ALCH_TRY(read.apart(i, t.v_scale, blocks, "v_scale"));
+    }
+    return launch_adamw8(n_tensors, tensors, tensors_host, *p, seed, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

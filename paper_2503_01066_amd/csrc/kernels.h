@@ -342,5 +342,23 @@ size_t grad_clip_workspace_bytes();
 int launch_grad_clip(int n_tensors, const alch_grad_tensor* tensors, const alch_grad_tensor* host, float max_norm, float* norm_out, void* workspace,
                      hipStream_t stream);
 int launch_adamw(int n_tensors, const alch_adamw_tensor* tensors, const alch_adamw_tensor* host, const alch_adamw& p, hipStream_t stream);
+int launch_adamw8(int n_tensors, const alch_adamw8_tensor* tensors, const alch_adamw8_tensor* host, const alch_adamw& p, uint32_t seed,
+                  hipStream_t stream);
+
+// ---- records in 8 bits ---------------------------------------------------------------------
+int launch_pack_q8(const uint8_t* mask, int T, const int* cu_seqlens, int n_seqs, int n_streams, const alch_q8_stream* streams, long long capacity,
+                   int* kept_index, int* cu_kept, int* n_kept_and_status, void* workspace, hipStream_t stream);
+// kept_index NULL: every token.
+int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long long capacity, const int* kept_index, const int* n_kept_and_status,
+                     hipStream_t stream);
+int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n_tensors, const alch_q8_tensor* tensors, hipStream_t stream);
+
+// ---- policy loss ---------------------------------------------------------------------------
+size_t policy_loss_workspace_bytes(int n_items, int vocab);
+// Rows of logits whose items are item0 .. item0 + rows - 1; what every item adds to the loss goes to terms [4, stride], which
+// launch_policy_sums adds up.  dlogits NULL (no gradient), logits itself, or other memory.
+int launch_policy_rows(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits,
+                       long long ld_grad, float* terms, long long stride, hipStream_t stream);
+int launch_policy_sums(const float* terms, long long stride, int n_items, float* loss_out, hipStream_t stream);
 
 }  // namespace alch

@@ -1,0 +1,256 @@
+// Records in 8 bits: the kept rows of activations as int8 codes with an fp32 scale for every 64 elements, and back (Section 4.1 of the
+// paper: what serving leaves behind is kept until it is trained on).
+//
+//   a = max |x| of a group,  scale = a / 127,  code = rint(x * (127 / a));   x' = code * scale
+//
+// Each rounding is made where the definition has it (no fused multiply-add between the product and rint), so that codes and scales
+// are defined bit for bit.  int8 with the group's own scale: an activation of normal distribution comes back to 0.5 % in the 2-norm,
+// 8-bit floats with 3 bits of mantissa leave 2.6 %.
+//
+// Both directions are bound by memory: a kept element is 2 bytes read and 1 1/16 written, and the reverse.
+#include "kernels.h"
+
+namespace alch {
+
+static constexpr int kGroup = ALCH_Q8_GROUP, kThreads = 256;
+static constexpr int kMaxPerLaunch = 16;        // streams of a launch
+static constexpr int kGridMax = 1 << 20;        // work-groups of a launch; rows behind them are gone over in rounds
+static constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: below it 127 / a would leave fp32
+
+typedef float f32x4_q __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_q __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x2_q __attribute__((ext_vector_type(2)));
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, kCtrl, 0xf, 0xf, false);
+    return v > o ? v : o;
+}
+// Over each eight lanes: neighbours, pairs, quads.
+__device__ __forceinline__ uint32_t max_of_8(uint32_t v) {
+    v = dpp_max<0xB1>(v);
+    v = dpp_max<0x4E>(v);
+    return dpp_max<0x141>(v);
+}
+__device__ __forceinline__ uint32_t max_of_64(uint32_t v) {
+    v = dpp_max<0x140>(max_of_8(v));
+    v = dpp_max<0x142>(v);  // (from lane 15 of the row before, then from lane 31: the last lane has seen all)
+    v = dpp_max<0x143>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+struct GroupScale {
+    float scale, r;
+    bool fine;  // no infinity and no NaN
+};
+__device__ __forceinline__ GroupScale group_scale(uint32_t bits) {  // of the largest magnitude
+    const float a = __builtin_bit_cast(float, bits);
+    GroupScale s;
+    s.fine = bits < 0x7f800000u;
+    s.r = s.fine && a >= kTiny ? 127.f / a : 0.f;
+    s.scale = !s.fine ? __builtin_nanf("") : a >= kTiny ? a / 127.f : 0.f;
+    return s;
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+// rint(x r) in the low byte: 1.5 * 2^23 added, the last bit of the sum is 1
+__device__ __forceinline__ uint32_t code_of(float x, float r) {
+#pragma clang fp contract(off)
+    const float y = x * r;
+    return __builtin_bit_cast(uint32_t, y + 12582912.f);
+}
+__device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
+    const bf16x8_q v = __builtin_bit_cast(bf16x8_q, __builtin_nontemporal_load(reinterpret_cast<const f32x4_q*>(p)));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const f32x4_q a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_q*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_q*>(p) + 1);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+}
+__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
+    bf16x8_q v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
+    __builtin_nontemporal_store(__builtin_bit_cast(f32x4_q, v), reinterpret_cast<f32x4_q*>(p));
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    __builtin_nontemporal_store(f32x4_q{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4_q*>(p));
+    __builtin_nontemporal_store(f32x4_q{x[4], x[5], x[6], x[7]}, reinterpret_cast<f32x4_q*>(p) + 1);
+}
+
+// ---- a row, by a work-group --------------------------------------------------------------------
+// Eight elements a lane, so that a group is eight lanes and its maximum three steps of neighbours.
+template <typename T>
+__device__ __forceinline__ void quantise_row_pieces(const T* __restrict__ src, int8_t* __restrict__ codes, float* __restrict__ scales, long long width) {
+    const long long pieces = width >> 3;
+    for (long long base = 0; base < pieces; base += kThreads) {
+        const long long p = base + threadIdx.x;
+        float x[8] = {};
+        if (p < pieces) load8(src + p * 8, x);
+        uint32_t most = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = max(most, magnitude(x[e]));
+        const GroupScale s = group_scale(max_of_8(most));
+        uint32_t c[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = code_of(x[e], s.r);
+        u32x2_q w = {bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7])};
+        if (!s.fine) w = u32x2_q{0, 0};
+        if (p < pieces) {
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x2_q*>(codes + p * 8));
+            if ((threadIdx.x & 7) == 0) scales[p >> 3] = s.scale;
+        }
+    }
+}
+// An element a lane, for rows that are not made of aligned pieces.
+template <typename T>
+__device__ __forceinline__ void quantise_row_elements(const T* __restrict__ src, int8_t* __restrict__ codes, float* __restrict__ scales, long long width) {
+    const int lane = threadIdx.x & 63;
+    const long long groups = (width + kGroup - 1) / kGroup;
+    for (long long g = threadIdx.x >> 6; g < groups; g += kThreads / 64) {
+        const long long at = g * kGroup + lane;
+        const float x = at < width ? (float)src[at] : 0.f;
+        const GroupScale s = group_scale(max_of_64(magnitude(x)));
+        if (at < width) codes[at] = s.fine ? (int8_t)code_of(x, s.r) : 0;
+        if (lane == 0) scales[g] = s.scale;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void expand_row_pieces(const int8_t* __restrict__ codes, const float* __restrict__ scales, T* __restrict__ dst, long long width) {
+    const long long pieces = width >> 3;
+    for (long long p = threadIdx.x; p < pieces; p += kThreads) {
+        float x[8] = {};
+        if (codes) {
+            const u32x2_q c = __builtin_nontemporal_load(reinterpret_cast<const u32x2_q*>(codes + p * 8));
+            const float s = scales[p >> 3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)(c[e >> 2] >> (8 * (e & 3))) * s;
+        }
+        store8(dst + p * 8, x);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void expand_row_elements(const int8_t* __restrict__ codes, const float* __restrict__ scales, T* __restrict__ dst, long long width) {
+    for (long long at = threadIdx.x; at < width; at += kThreads) dst[at] = (T)(codes ? (float)codes[at] * scales[at / kGroup] : 0.f);
+}
+
+// ---- kernels -----------------------------------------------------------------------------------
+struct Q8Stream {  // of either direction: codes and scales dense, the tensor's rows `stride` bytes apart
+    char* tensor;
+    int8_t* codes;
+    float* scales;
+    long long width, stride;
+    int bf16, pieces;
+};
+struct Q8Args {
+    Q8Stream s[kMaxPerLaunch];
+    int n;
+};
+
+__device__ __forceinline__ void quantise_row(const Q8Stream& s, long long from, long long to) {
+    const char* src = s.tensor + from * s.stride;
+    int8_t* codes = s.codes + to * s.width;
+    float* scales = s.scales + to * ((s.width + kGroup - 1) / kGroup);
+    if (s.bf16) {
+        if (s.pieces) quantise_row_pieces(reinterpret_cast<const __bf16*>(src), codes, scales, s.width);
+        else quantise_row_elements(reinterpret_cast<const __bf16*>(src), codes, scales, s.width);
+    } else {
+        if (s.pieces) quantise_row_pieces(reinterpret_cast<const float*>(src), codes, scales, s.width);
+        else quantise_row_elements(reinterpret_cast<const float*>(src), codes, scales, s.width);
+    }
+}
+__device__ __forceinline__ void expand_row(const Q8Stream& s, long long from, long long to) {  // from < 0: zeros
+    char* dst = s.tensor + to * s.stride;
+    const int8_t* codes = from < 0 ? nullptr : s.codes + from * s.width;
+    const float* scales = s.scales + (from < 0 ? 0 : from) * ((s.width + kGroup - 1) / kGroup);
+    if (s.bf16) {
+        if (s.pieces) expand_row_pieces(codes, scales, reinterpret_cast<__bf16*>(dst), s.width);
+        else expand_row_elements(codes, scales, reinterpret_cast<__bf16*>(dst), s.width);
+    } else {
+        if (s.pieces) expand_row_pieces(codes, scales, reinterpret_cast<float*>(dst), s.width);
+        else expand_row_elements(codes, scales, reinterpret_cast<float*>(dst), s.width);
+    }
+}
+
+// A work-group a row (the grid is sized for the most rows that the call can produce).  kept_index NULL: every token, n_rows of them.
+__global__ __launch_bounds__(kThreads) void k_gather_q8(Q8Args a, const int* __restrict__ kept_index, const int* __restrict__ n_kept_and_status,
+                                                        long long n_rows) {
+    if (kept_index) n_rows = min(n_rows, (long long)n_kept_and_status[0]);
+    for (long long r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        const long long t = kept_index ? kept_index[r] : r;
+        for (int k = blockIdx.y; k < a.n; k += gridDim.y) quantise_row(a.s[k], t, r);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_expand(Q8Args a, const int* __restrict__ rows, long long n_rows, long long n_src_rows) {
+    for (long long r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        long long from = rows ? rows[r] : r;
+        if (from < 0 || from >= n_src_rows) from = -1;
+        for (int k = blockIdx.y; k < a.n; k += gridDim.y) expand_row(a.s[k], from, r);
+    }
+}
+
+static bool made_of_pieces(const void* tensor, const void* codes, long long width, size_t stride) {
+    return width % 8 == 0 && stride % 16 == 0 && aligned16(tensor) && aligned16(codes);
+}
+// Streams base .. of a call, at most kMaxPerLaunch of them.
+static Q8Args q8_args(int n, const alch_q8_stream* streams, int base) {
+    Q8Args a;
+    a.n = n - base < kMaxPerLaunch ? n - base : kMaxPerLaunch;
+    for (int k = 0; k < a.n; ++k) {
+        const alch_q8_stream& s = streams[base + k];
+        a.s[k] = {const_cast<char*>(static_cast<const char*>(s.src)), s.codes, s.scales, s.width, (long long)s.src_row_stride_bytes, s.dtype == ALCH_BF16,
+                  made_of_pieces(s.src, s.codes, s.width, s.src_row_stride_bytes)};
+    }
+    return a;
+}
+
+int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long long capacity, const int* kept_index, const int* n_kept_and_status,
+                     hipStream_t stream) {
+    const long long max_rows = T < capacity ? T : capacity;
+    if (max_rows == 0 || n_streams == 0) return ALCH_OK;
+    double bytes = 0;  // of a kept row: their number is on the device
+    for (int k = 0; k < n_streams; ++k) bytes += (double)streams[k].width * (dtype_size((alch_dtype)streams[k].dtype) + 1 + 4.0 / kGroup);
+    TraceScope ts(kTracePackGather, 0.0, bytes, stream);
+    for (int base = 0; base < n_streams; base += kMaxPerLaunch) {
+        const Q8Args a = q8_args(n_streams, streams, base);
+        const dim3 grid((unsigned)(max_rows < kGridMax ? max_rows : kGridMax), max_rows <= 256 ? a.n : 1);
+        k_gather_q8<<<grid, kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows);
+    }
+    ALCH_HIP_TRY(hipGetLastError());
+    return ALCH_OK;
+}
+
+int launch_pack_q8(const uint8_t* mask, int T, const int* cu_seqlens, int n_seqs, int n_streams, const alch_q8_stream* streams, long long capacity,
+                   int* kept_index, int* cu_kept, int* n_kept_and_status, void* workspace, hipStream_t stream) {
+    ALCH_TRY(launch_pack(mask, T, cu_seqlens, n_seqs, 0, nullptr, capacity, kept_index, cu_kept, n_kept_and_status, workspace, stream));
+    return launch_gather_q8(T, n_streams, streams, capacity, kept_index, n_kept_and_status, stream);
+}
+
+int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n_tensors, const alch_q8_tensor* tensors, hipStream_t stream) {
+    if (n_rows == 0 || n_tensors == 0) return ALCH_OK;
+    double bytes = 0;
+    for (int k = 0; k < n_tensors; ++k) bytes += (double)n_rows * tensors[k].width * (dtype_size((alch_dtype)tensors[k].dtype) + 1 + 4.0 / kGroup);
+    TraceScope ts(kTracePackGather, 0.0, bytes, stream);
+    for (int base = 0; base < n_tensors; base += kMaxPerLaunch) {
+        Q8Args a;
+        a.n = n_tensors - base < kMaxPerLaunch ? n_tensors - base : kMaxPerLaunch;
+        for (int k = 0; k < a.n; ++k) {
+            const alch_q8_tensor& t = tensors[base + k];
+            a.s[k] = {static_cast<char*>(t.dst), const_cast<int8_t*>(t.codes), const_cast<float*>(t.scales), t.width, (long long)t.dst_row_stride_bytes,
+                      t.dtype == ALCH_BF16, made_of_pieces(t.dst, t.codes, t.width, t.dst_row_stride_bytes)};
+        }
+        const dim3 grid((unsigned)(n_rows < kGridMax ? n_rows : kGridMax), n_rows <= 256 ? a.n : 1);
+        k_expand<<<grid, kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
+    }
+    ALCH_HIP_TRY(hipGetLastError());
+    return ALCH_OK;
+}
+
+}  // namespace alch
