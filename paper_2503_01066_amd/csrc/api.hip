@@ -1344,7 +1344,6 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
             ALCH_TRY(launch_dpo_weights(p.dpo_logp, dpo->item_slot, dpo->item_label, M, vocab, dpo->ref_logp, dpo->n_pairs,
                                         dpo->beta, p.dpo_pi, p.dpo_w, dpo->z_out, loss_out, st));
         }
-        const long long stride = p.dpo_logz - p.dpo_logp;  // (the four arrays of the plan are equally far apart: the policy loss's terms)
         bool first = true;
         for (int r0 = 0; r0 < M; r0 += kHeadChunkRows) {
             const int rows = M - r0 < kHeadChunkRows ? M - r0 : kHeadChunkRows;
@@ -1353,7 +1352,7 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
                 ALCH_TRY(launch_dpo_grad(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, dpo->item_slot + r0,
                                          p.dpo_logz + r0, p.dpo_w, n_slots, st));
             else
-                ALCH_TRY(launch_policy_rows(dt, p.logits, vocab, rows, vocab, *policy, r0, p.logits, vocab, p.dpo_logp, stride, st));
+                ALCH_TRY(launch_policy_rows(dt, p.logits, vocab, rows, vocab, *policy, r0, p.logits, vocab, p.dpo_logp, p.dpo_logz, st));
             {  // gradient of the gathered rows = dlogits W_lm
                 GemmDesc d = gemm_ws(dt, rows, H, true, false);
                 add_seg(d, p.logits, vocab, W_lm, H, vocab);
@@ -1375,7 +1374,7 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
             add_out(d, dW_lm, 0, H);
             ALCH_TRY(launch_gemm_generic(d, st));
         }
-        if (policy) ALCH_TRY(launch_policy_sums(p.dpo_logp, stride, M, loss_out, st));
+        if (policy) ALCH_TRY(launch_policy_sums(*policy, p.dpo_logp, p.dpo_logz, loss_out, st));
         ALCH_TRY(launch_dpo_scatter(dt, p.h_dHf, item_row, M, p.dHf, T, H, st));
     } else {
         // LM head + cross-entropy in row chunks: logits -> dlogits in place, never stored whole.
@@ -1562,10 +1561,9 @@ int alch_policy_loss(alch_dtype dtype, int32_t vocab, const void* logits, int64_
     of[9] = {workspace, need, "workspace", -1, true};
     ALCH_TRY(check_apart(of, 10));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    float* terms = static_cast<float*>(workspace);
-    const long long stride = n > 0 ? n : 1;
-    ALCH_TRY(launch_policy_rows(dtype, logits, ld, n, vocab, *policy, 0, dlogits, ld_grad, terms, stride, st));
-    return launch_policy_sums(terms, stride, n, loss_out, st);
+    float *own = static_cast<float*>(workspace), *sum = own + n;
+    ALCH_TRY(launch_policy_rows(dtype, logits, ld, n, vocab, *policy, 0, dlogits, ld_grad, own, sum, st));
+    return launch_policy_sums(*policy, own, sum, loss_out, st);
 }
 
 int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batch, const void* Q, const void* K,

@@ -355,10 +355,10 @@ int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n
 
 // ---- policy loss ---------------------------------------------------------------------------
 size_t policy_loss_workspace_bytes(int n_items, int vocab);
-// Rows of logits whose items are item0 .. item0 + rows - 1; what every item adds to the loss goes to terms [4, stride], which
-// launch_policy_sums adds up.  dlogits NULL (no gradient), logits itself, or other memory.
+// Rows of logits whose items are item0 .. item0 + rows - 1.  own and sum [n_items]: what launch_policy_sums makes the loss of.  dlogits NULL (no
+// gradient), logits itself, or other memory.
 int launch_policy_rows(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits,
-                       long long ld_grad, float* terms, long long stride, hipStream_t stream);
-int launch_policy_sums(const float* terms, long long stride, int n_items, float* loss_out, hipStream_t stream);
+                       long long ld_grad, float* own, float* sum, hipStream_t stream);
+int launch_policy_sums(const alch_policy& p, float* own, float* sum, float* loss_out, hipStream_t stream);
 
 }  // namespace alch
