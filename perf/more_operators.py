@@ -289,7 +289,7 @@ def _policy(s):
     if own:
         import paper_2503_01066_amd as A
         loss, logp, grad = A.alch_policy_loss(s["logits"], s["items"], clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl_coef=KL if c["kl"] else 0.0,
-                                              dlogits=s["grad"], logp=s["logp"], loss=s["loss"], workspace=s["ws"])
+                                              want_grad=c["grad"], dlogits=s["grad"], logp=s["logp"], loss=s["loss"], workspace=s["ws"])
         return [loss, logp] + ([grad] if c["grad"] else [])
     x, label = s["logits"].float(), s["label"].long()[:, None]
     most = x.amax(1, keepdim=True)
