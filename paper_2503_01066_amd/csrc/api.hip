@@ -216,6 +216,7 @@ struct StackPlan {
     int *h_labels, *h_index, *h_inv, *h_cu, *h_n, *h_chunk_rows;
     // DPO head: log-probability and log-normaliser per item, sum and weight per slot
     float *dpo_logp, *dpo_logz, *dpo_pi, *dpo_w;
+    void* policy_ws;  // of the policy loss, beside the first two: its items' label logits and sums
     size_t layer_ws_bytes, bytes;
 };
 static StackPlan plan_stack(const alch_layer_shape& s, int vocab, int T, void* ws, size_t ws_bytes, int lora_rank = 0) {
@@ -245,6 +246,7 @@ static StackPlan plan_stack(const alch_layer_shape& s, int vocab, int T, void* w
     p.dpo_logz = static_cast<float*>(a.take(t * sizeof(float)));
     p.dpo_pi = static_cast<float*>(a.take(t * sizeof(float)));
     p.dpo_w = static_cast<float*>(a.take(t * sizeof(float)));
+    p.policy_ws = a.take(policy_scratch_bytes());
     p.layer_ws_bytes = plan_layer_bwd(s, T, nullptr, 0, lora_rank).bytes;
     p.layer_ws = a.take(p.layer_ws_bytes);
     p.bytes = round_up(a.used, 256);
@@ -1352,7 +1354,8 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
                 ALCH_TRY(launch_dpo_grad(dt, p.logits, vocab, rows, vocab, dpo->item_label + r0, dpo->item_slot + r0,
                                          p.dpo_logz + r0, p.dpo_w, n_slots, st));
             else
-                ALCH_TRY(launch_policy_rows(dt, p.logits, vocab, rows, vocab, *policy, r0, p.logits, vocab, p.dpo_logp, p.dpo_logz, st));
+                ALCH_TRY(launch_policy(dt, p.logits, vocab, rows, vocab, *policy, r0, p.logits, vocab, p.dpo_logp, p.dpo_logz, p.policy_ws,
+                                       one_chunk ? loss_out : nullptr, st));
             {  // gradient of the gathered rows = dlogits W_lm
                 GemmDesc d = gemm_ws(dt, rows, H, true, false);
                 add_seg(d, p.logits, vocab, W_lm, H, vocab);
@@ -1374,7 +1377,7 @@ static int stack_backward_impl(const alch_layer_shape* shape, int32_t n_layers, 
             add_out(d, dW_lm, 0, H);
             ALCH_TRY(launch_gemm_generic(d, st));
         }
-        if (policy) ALCH_TRY(launch_policy_sums(*policy, p.dpo_logp, p.dpo_logz, loss_out, st));
+        if (policy && (M == 0 || !one_chunk)) ALCH_TRY(launch_policy_sums(*policy, p.dpo_logp, p.dpo_logz, p.policy_ws, loss_out, st));
         ALCH_TRY(launch_dpo_scatter(dt, p.h_dHf, item_row, M, p.dHf, T, H, st));
     } else {
         // LM head + cross-entropy in row chunks: logits -> dlogits in place, never stored whole.
@@ -1561,9 +1564,9 @@ int alch_policy_loss(alch_dtype dtype, int32_t vocab, const void* logits, int64_
     of[9] = {workspace, need, "workspace", -1, true};
     ALCH_TRY(check_apart(of, 10));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    float *own = static_cast<float*>(workspace), *sum = own + n;
-    ALCH_TRY(launch_policy_rows(dtype, logits, ld, n, vocab, *policy, 0, dlogits, ld_grad, own, sum, st));
-    return launch_policy_sums(*policy, own, sum, loss_out, st);
+    char* scratch = static_cast<char*>(workspace);
+    float *own = reinterpret_cast<float*>(scratch + policy_scratch_bytes()), *sum = own + n;
+    return launch_policy(dtype, logits, ld, n, vocab, *policy, 0, dlogits, ld_grad, own, sum, scratch, loss_out, st);
 }
 
 int alch_attention_forward(const alch_layer_shape* shape, const alch_batch* batch, const void* Q, const void* K,

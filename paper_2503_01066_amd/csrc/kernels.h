@@ -355,10 +355,12 @@ int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n
 
 // ---- policy loss ---------------------------------------------------------------------------
 size_t policy_loss_workspace_bytes(int n_items, int vocab);
-// Rows of logits whose items are item0 .. item0 + rows - 1.  own and sum [n_items]: what launch_policy_sums makes the loss of.  dlogits NULL (no
-// gradient), logits itself, or other memory.
-int launch_policy_rows(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits,
-                       long long ld_grad, float* own, float* sum, hipStream_t stream);
-int launch_policy_sums(const alch_policy& p, float* own, float* sum, float* loss_out, hipStream_t stream);
+size_t policy_scratch_bytes();
+// Rows of logits whose items are item0 .. item0 + rows - 1.  own and sum [n_items]: what the loss is made of, by this call where loss_out is given
+// (all items of the policy, then, are these rows; scratch of policy_scratch_bytes()), else by launch_policy_sums.  dlogits NULL (no gradient),
+// logits itself, or other memory.
+int launch_policy(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits, long long ld_grad,
+                  float* own, float* sum, void* scratch, float* loss_out, hipStream_t stream);
+int launch_policy_sums(const alch_policy& p, float* own, float* sum, void* scratch, float* loss_out, hipStream_t stream);
 
 }  // namespace alch

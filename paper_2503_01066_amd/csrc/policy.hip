@@ -13,6 +13,8 @@
 //   parts  few rows: several work-groups share one, in two launches with the parts' sums between them.
 // The row kernels leave x_label - max and the sum of exponentials of every item; the loss is made of them in 64 bits by one launch, where
 // terms of either sign cancel and a rounding of logp to fp32 would be seen.
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace alch {
@@ -23,12 +25,18 @@ typedef unsigned int u32x4_p __attribute__((ext_vector_type(4)));
 typedef int i32x4_p __attribute__((ext_vector_type(4)));
 
 static constexpr float kLog2e = 1.4426950408889634f;
+static constexpr double kLog2eDouble = 1.4426950408889634;
+static constexpr int kGridMax = 1 << 20;  // work-groups of a launch; rows behind them are gone over in rounds
 
 struct PolicyArgs {
     const int* label;
     const float *old_logp, *advantage, *weight, *ref_logp;
     float low, high, kl_coef;  // 1 - clip_low, 1 + clip_high
     float *own, *sum;          // of every item: its label's logit less the row's largest, and the sum of exponentials (0: it scores nothing)
+
+    PolicyArgs from(int m) const {  // of the items behind the first m
+        return {label + m, old_logp + m, advantage + m, weight + m, ref_logp ? ref_logp + m : nullptr, low, high, kl_coef, own + m, sum + m};
+    }
 };
 
 // d of the gradient, from an item's log-probability.
@@ -45,19 +53,28 @@ __device__ __forceinline__ float slope(const PolicyArgs& a, int m, float logp) {
 }
 __device__ __forceinline__ bool scores(const PolicyArgs& a, int m, int vocab) { return (unsigned)a.label[m] < (unsigned)vocab && a.weight[m] != 0.f; }
 
-template <int kCtrl>
-__device__ __forceinline__ float dpp(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, false));
+// v of the lane that a DPP pattern names; other's value in rows of 16 lanes outside of the mask.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ float from_lane(float other, float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other), __builtin_bit_cast(int, v), kCtrl, kRows, 0xf, false));
 }
+__device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63)); }
+// Over a wavefront: neighbours, pairs, quads, halves of a row of 16 lanes; then row by row into the last one.
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+    v = fmaxf(v, from_lane<0xB1>(v, v));
+    v = fmaxf(v, from_lane<0x4E>(v, v));
+    v = fmaxf(v, from_lane<0x141>(v, v));
+    v = fmaxf(v, from_lane<0x140>(v, v));
+    v = fmaxf(v, from_lane<0x142, 0xa>(v, v));
+    return last_lane(fmaxf(v, from_lane<0x143, 0xc>(v, v)));
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    v += from_lane<0xB1>(0.f, v);
+    v += from_lane<0x4E>(0.f, v);
+    v += from_lane<0x141>(0.f, v);
+    v += from_lane<0x140>(0.f, v);
+    v += from_lane<0x142, 0xa>(0.f, v);
+    return last_lane(v + from_lane<0x143, 0xc>(0.f, v));
 }
 // Over a work-group, the result for everybody.  red: a float a wavefront, of each call its own.
 template <int kThreads>
@@ -127,11 +144,37 @@ __device__ __forceinline__ void piece_sum(const V& x, float base, float (&s)[4])
 #pragma unroll
     for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown((float)x[e], base);
 }
+// scale * exp(x - base).  bf16: the scale goes into the exponent, whose rounding (2^-20 of the result where it has 5 bits before the point) is far
+// below the result's own of 2^-9.
+struct GradOf {
+    float base, scale, log2_scale;
+    uint32_t sign;
+};
+__device__ __forceinline__ GradOf grad_of(float base, float scale) {
+    return {base, scale, __builtin_amdgcn_logf(fabsf(scale)), __builtin_bit_cast(uint32_t, scale) & 0x80000000u};
+}
 template <typename T, typename V>
-__device__ __forceinline__ V piece_grad(const V& x, float base, float scale) {
+__device__ __forceinline__ V piece_grad(const V& x, const GradOf& o) {
     V g;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int e = 0; e < Piece<T>::n; ++e) g[e] = (T)(scale * grown((float)x[e], base));
+        for (int e = 0; e < Piece<T>::n; ++e) g[e] = (T)__builtin_amdgcn_exp2f(fmaf((float)x[e] - o.base, kLog2e, o.log2_scale));
+        return __builtin_bit_cast(V, __builtin_bit_cast(u32x4_p, g) ^ (o.sign | o.sign >> 16));
+    } else {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::n; ++e) g[e] = o.scale * grown((float)x[e], o.base);
+        return g;
+    }
+}
+
+// e: the label's place in the piece, where it is there: in one piece of a row.
+template <typename T, typename V>
+__device__ __forceinline__ V with_label(V g, int e, float at_label) {
+    if ((unsigned)e < (unsigned)Piece<T>::n) {
+#pragma unroll
+        for (int i = 0; i < Piece<T>::n; ++i)
+            if (i == e) g[i] = (T)at_label;
+    }
     return g;
 }
 
@@ -146,36 +189,35 @@ __device__ __forceinline__ void store_piece(void* p, const V& v) {
 }
 
 // ---- held --------------------------------------------------------------------------------------
-template <typename T, int kThreads, int kHeld, bool kGrad>
+template <typename T, int kThreads, int kHeld>
 __global__ __launch_bounds__(kThreads) void k_policy_held(const T* logits, long long ld, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
     typedef typename Piece<T>::type V;
     constexpr int n = Piece<T>::n;
     __shared__ float red[2][kThreads / 64];
     const int m = blockIdx.x, tid = threadIdx.x;
     const T* row = logits + m * ld;
-    T* out = kGrad ? dlogits + m * ld_grad : nullptr;
+    T* out = dlogits + m * ld_grad;
     const RowCut c = cut_row(row, vocab);
     const int extra = extra_of<T>(c, vocab);
     const T* body = row + c.head;
     if (!scores(a, m, vocab)) {
         if (tid == 0) a.own[m] = 0.f, a.sum[m] = 0.f;
-        if constexpr (kGrad) {
-            const V zero = {};
-            for (int p = tid; p < c.pieces; p += kThreads) store_piece(out + c.head + p * n, zero);
-            if (extra >= 0) out[extra] = (T)0.f;
-        }
+        const V zero = {};
+        for (int p = tid; p < c.pieces; p += kThreads) store_piece(out + c.head + p * n, zero);
+        if (extra >= 0) out[extra] = (T)0.f;
         return;
     }
     V x[kHeld];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
         if (tid + k * kThreads < c.pieces) x[k] = load_piece<V>(body + (tid + k * kThreads) * n);
-    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[a.label[m]];
+    const int label = a.label[m];
+    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label];
     float most = xe;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
         if (tid + k * kThreads < c.pieces) most = piece_max<T>(x[k], most);
-    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) most = piece_max<T>(load_piece<V>(body + p * n), most);
+    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) most = piece_max<T>(load_piece<V>(body + (long long)p * n), most);
     most = group_max<kThreads>(most, red[0]);
     const float base = most == -INFINITY ? 0.f : most;  // (without a finite logit the sum is 0, or NaN)
     float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
@@ -185,42 +227,286 @@ __global__ __launch_bounds__(kThreads) void k_policy_held(const T* logits, long 
         asm volatile("" : "+v"(x[k]));
         if (tid + k * kThreads < c.pieces) piece_sum<T>(x[k], base, s);
     }
-    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) piece_sum<T>(load_piece<V>(body + p * n), base, s);
+    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) piece_sum<T>(load_piece<V>(body + (long long)p * n), base, s);
     const float sum = group_sum<kThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
     if (tid == 0) {
         a.own[m] = sum == 0.f ? -INFINITY : xl - base;
         a.sum[m] = sum;
     }
-    if constexpr (kGrad) {
-        const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
-        const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
-        const int label = a.label[m];
-        // (each thread writes what it has read: in place nobody reads what another one has written)
+    const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
+    const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
+    const GradOf grad = grad_of(base, scale);
+    // (each thread writes what it has read: in place nobody reads what another one has written)
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
+    for (int k = 0; k < kHeld; ++k) {
+        asm volatile("" : "+v"(x[k]));
+        const int p = tid + k * kThreads;
+        if (p < c.pieces) store_piece(out + c.head + p * n, with_label<T>(piece_grad<T>(x[k], grad), label - c.head - p * n, at_label));
+    }
+    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads)
+        store_piece(out + c.head + (long long)p * n,
+                    with_label<T>(piece_grad<T>(load_piece<V>(body + (long long)p * n), grad), label - c.head - p * n, at_label));
+    if (extra >= 0) out[extra] = (T)(extra == label ? at_label : scale * grown(xe, base));
+}
+
+// ---- stay --------------------------------------------------------------------------------------
+static constexpr int kStayThreads = 1024, kStayPieces = 16, kStayLds = 9, kStayRegs = kStayPieces - kStayLds;
+
+__device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // reads past the bytes are zero, writes dropped
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    i32x4_p r;
+    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    r[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu));
+    r[2] = __builtin_amdgcn_readfirstlane(bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, long long ld, int rows, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
+    typedef typename Piece<T>::type V;
+    constexpr int n = Piece<T>::n;
+    __shared__ __attribute__((aligned(1024))) V ahead[kStayLds * kStayThreads];
+    __shared__ float red[2][kStayThreads / 64];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), step = (int)gridDim.x;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ahead + (uint32_t)wave * 1024u;
+    struct Item {  // of the row that is on its way
+        int label;
+        float weight, advantage, old_logp, ref_logp;
+        bool counted;
+    };
+    const auto item_of = [&](int r) {
+        const int m = min(r, rows - 1);
+        Item i{a.label[m], a.weight[m], a.advantage[m], a.old_logp[m], a.ref_logp ? a.ref_logp[m] : 0.f, false};
+        i.counted = r < rows && (unsigned)i.label < (unsigned)vocab && i.weight != 0.f;
+        return i;
+    };
+    V next[kStayRegs];
+    float xe_next = -INFINITY, xl_next = 0.f;
+    // The loads of a row: a wavefront fetches what its own lanes will use.  kStayPieces of them are issued whether or not the row reaches
+    // as far, or is wanted at all.
+    const auto fetch = [&](int r, const Item& i) {
+        const T* row = logits + (long long)min(r, rows - 1) * ld;
+        const RowCut c = cut_row(row, vocab);
+        const int bytes = i.counted ? c.pieces * 16 : 0, extra = extra_of<T>(c, vocab);
+        const i32x4_p src = resource(row + c.head, bytes);
+        uint32_t at = (uint32_t)tid * 16u;
+        asm volatile("" : "+v"(at));  // (one register, not one per piece kept across the loop)
+#pragma unroll
+        for (int k = 0; k < kStayLds; ++k)  // (s_nop: a load into LDS takes one wait state after a scalar write of m0)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds0 + k * kStayThreads * 16),
+                         "v"(at + k * kStayThreads * 16), "s"(src)
+                         : "memory", "m0");
+#pragma unroll
+        for (int k = 0; k < kStayRegs; ++k)
+            next[k] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row) + c.head, 0, bytes, 0x00020000),
+                                                                                  at + (kStayLds + k) * kStayThreads * 16, 0, 0));
+        xe_next = i.counted && extra >= 0 ? (float)row[extra] : -INFINITY;
+        xl_next = i.counted ? (float)row[i.label] : 0.f;
+    };
+    Item item = item_of(blockIdx.x), item1 = item_of(blockIdx.x + step);
+    fetch(blockIdx.x, item);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0), known to the compiler: inside the loop it then counts the stores, too
+    for (int r = blockIdx.x; r < rows; r += step) {
+        // the row's loads have landed; the last kStayPieces stores of the row before may still be on their way
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStayPieces) : "memory");
+        const Item item2 = item_of(r + 2 * step);
+        const RowCut c = cut_row(logits + (long long)r * ld, vocab);
+        const int extra = extra_of<T>(c, vocab);
+        T* out = dlogits + (long long)r * ld_grad;
+        const auto dst = __builtin_amdgcn_make_buffer_rsrc(out + c.head, 0, c.pieces * 16, 0x00020000);
+        if (!item.counted) {
+            fetch(r + step, item1);
+            if (tid == 0) a.own[r] = 0.f, a.sum[r] = 0.f;
+            if (extra >= 0) out[extra] = (T)0.f;
+            int at = tid;
+            asm volatile("" : "+v"(at) :: "memory");
+#pragma unroll
+            for (int k = 0; k < kStayPieces; ++k) __builtin_amdgcn_raw_buffer_store_b128(u32x4_p{0, 0, 0, 0}, dst, (at + k * kStayThreads) * 16, 0, 0);
+            item = item1;
+            item1 = item2;
+            continue;
+        }
+        V x[kStayPieces];
+#pragma unroll
+        for (int k = 0; k < kStayLds; ++k) x[k] = ahead[k * kStayThreads + tid];
+#pragma unroll
+        for (int k = 0; k < kStayRegs; ++k) x[kStayLds + k] = next[k];
+        const float xe = xe_next, xl = xl_next;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < kStayPieces; ++k) asm volatile("" : "+v"(x[k]));  // (in registers before the next row overwrites them)
+        fetch(r + step, item1);
+        float most = xe;
+#pragma unroll
+        for (int k = 0; k < kStayPieces; ++k)
+            if (tid + k * kStayThreads < c.pieces) most = piece_max<T>(x[k], most);
+        most = group_max<kStayThreads>(most, red[0]);
+        const float base = most == -INFINITY ? 0.f : most;
+        float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kStayPieces; ++k) {
             asm volatile("" : "+v"(x[k]));
-            const int p = tid + k * kThreads;
-            if (p >= c.pieces) continue;
-            V g = piece_grad<T>(x[k], base, scale);
-            const int e = label - c.head - p * n;
-            if ((unsigned)e < (unsigned)n) g[e] = (T)at_label;
-            store_piece(out + c.head + p * n, g);
+            if (tid + k * kStayThreads < c.pieces) piece_sum<T>(x[k], base, s);
         }
-        for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) {
-            V g = piece_grad<T>(load_piece<V>(body + p * n), base, scale);
-            const int e = label - c.head - p * n;
-            if ((unsigned)e < (unsigned)n) g[e] = (T)at_label;
-            store_piece(out + c.head + p * n, g);
+        const float sum = group_sum<kStayThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+        const float logp = xl - base - logf(sum);
+        const float d = sum == 0.f ? 0.f : slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, logp), scale = sum == 0.f ? 0.f : -d / sum;
+        const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);
+        const GradOf grad = grad_of(base, scale);
+        // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
+        if (tid == 0) {
+            a.own[r] = sum == 0.f ? -INFINITY : xl - base;
+            a.sum[r] = sum;
         }
-        if (extra >= 0) out[extra] = (T)(extra == label ? at_label : scale * grown(xe, base));
+        if (extra >= 0) out[extra] = (T)(extra == item.label ? at_label : scale * grown(xe, base));
+        int at = tid;
+        asm volatile("" : "+v"(at) :: "memory");
+#pragma unroll
+        for (int k = 0; k < kStayPieces; ++k) {
+            asm volatile("" : "+v"(x[k]));
+            const V g = with_label<T>(piece_grad<T>(x[k], grad), item.label - c.head - (at + k * kStayThreads) * n, at_label);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_p, g), dst, (at + k * kStayThreads) * 16, 0, 0);
+        }
+        item = item1;
+        item1 = item2;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// ---- parts -------------------------------------------------------------------------------------
+// The sum of a row, or of a part of it, in one pass: with the largest logit so far and the power of two above its exponential, by which the terms are
+// scaled; where a larger one comes the sum is moved by the difference of the powers, exactly.  Nothing is held, so that work-groups are small
+// and many rows are on their way at once.
+static constexpr int kPartThreads = 256, kPartBatch = 8;
+static constexpr int kMaxParts = 64, kMaxPartials = 2048;  // of a row; of a call
+
+struct Partial {  // of a part: its largest logit, and its sum of exponentials relative to that one (0: it has no finite logit)
+    float most, sum;
+};
+// Beyond it a power is no longer exact (masks of the type's lowest value, for one).
+static constexpr float kPowerMost = 1048576.f;
+__device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowerMost ? ceilf(most * kLog2e) : 0.f; }
+// 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
+__device__ __forceinline__ float grown2(float x, float power) {
+    return __builtin_amdgcn_exp2f(fmaf(x, 1.9259629e-8f, fmaf(x, kLog2e, -power)));
+}
+__device__ __forceinline__ float moved(float sum, float from, float to) { return ldexpf(sum, (int)(from - to)); }
+
+// The pieces of part j of n.
+__device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, int* end) {
+    const int each = (pieces + n - 1) / n;
+    *begin = min(j * each, pieces);
+    *end = min(*begin + each, pieces);
+}
+// A row of its parts, by all lanes of a wavefront: kMaxParts at most.  base is the largest logit (0: there is none), sum relative to it.
+struct Whole {
+    float base, sum;
+};
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+__device__ __forceinline__ double part_in(const Partial& p, float base) {  // (a part of NaN alone has no largest one either)
+    return p.most == -INFINITY ? (double)p.sum : (double)p.sum * exp2(((double)p.most - (double)base) * kLog2eDouble);
+}
+__device__ __forceinline__ Whole whole_row(const Partial* __restrict__ partial, int parts) {
+    const int lane = threadIdx.x & 63;
+    const Partial p = lane < parts ? partial[lane] : Partial{-INFINITY, 0.f};
+    const float most = wave_max(p.most), base = most == -INFINITY ? 0.f : most;
+    return {base, (float)wave_sum(part_in(p, base))};
+}
+
+// Part j of row m is work-group m * parts + j's; parts == 1: the row is whole, and its sum goes to where k_policy_sums finds it.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, long long ld, int rows, int vocab, PolicyArgs a, int parts,
+                                                               Partial* __restrict__ partial) {
+    typedef typename Piece<T>::type V;
+    constexpr int n = Piece<T>::n;
+    __shared__ float red[3][kPartThreads / 64];
+    const int tid = threadIdx.x;
+    V least;
+#pragma unroll
+    for (int e = 0; e < n; ++e) least[e] = (T)-INFINITY;
+    for (long long b = blockIdx.x; b < (long long)rows * parts; b += gridDim.x) {
+        const int m = (int)(b / parts), j = (int)(b % parts);
+        const T* row = logits + m * ld;
+        if (!scores(a, m, vocab)) {
+            if (tid == 0 && parts == 1) a.own[m] = 0.f, a.sum[m] = 0.f;
+            continue;
+        }
+        const RowCut c = cut_row(row, vocab);
+        int p, end;
+        part_of(c.pieces, j, parts, &p, &end);
+        p += tid;
+        const T* body = row + c.head;
+        const int extra = j == 0 ? extra_of<T>(c, vocab) : -1;
+        const float xe = extra >= 0 ? (float)row[extra] : -INFINITY;
+        const auto load = [&](V (&x)[kPartBatch], int at) {
+#pragma unroll
+            for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
+        };
+        V next[kPartBatch];
+        load(next, p);
+        const float xl = j == 0 && tid == 0 ? (float)row[a.label[m]] : 0.f;
+        float most = xe, at = power(xe), s[4] = {extra >= 0 ? grown2(xe, at) : 0.f, 0.f, 0.f, 0.f};
+        for (; p < end; p += kPartBatch * kPartThreads) {
+            V x[kPartBatch];
+#pragma unroll
+            for (int k = 0; k < kPartBatch; ++k) x[k] = next[k];
+            load(next, p + kPartBatch * kPartThreads);
+            float higher = most;
+#pragma unroll
+            for (int k = 0; k < kPartBatch; ++k) higher = piece_max<T>(x[k], higher);
+            const float to = power(higher);
+            if (to != at && most != -INFINITY) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = moved(s[i], at, to);
+            }
+            most = higher;
+            at = to;
+#pragma unroll
+            for (int k = 0; k < kPartBatch; ++k) {
+                asm volatile("" : "+v"(x[k]));
+#pragma unroll
+                for (int e = 0; e < n; ++e) s[e & 3] += grown2((float)x[k][e], at);
+            }
+        }
+        const float group = group_max<kPartThreads>(most, red[0]), base = group == -INFINITY ? 0.f : group, sum = (s[0] + s[1]) + (s[2] + s[3]);
+        float total = group_sum<kPartThreads>(most == -INFINITY ? sum : moved(sum, at, power(group)), red[1]);
+        if (fabsf(base) <= kPowerMost) {
+            total = (float)((double)total * exp2((double)power(base) - (double)base * kLog2eDouble));
+        } else {  // (the powers say nothing: once more, from the largest one)
+            float once[4] = {extra >= 0 ? grown(xe, base) : 0.f, 0.f, 0.f, 0.f};
+            int q, to;
+            part_of(c.pieces, j, parts, &q, &to);
+            for (q += tid; q < to; q += kPartThreads) piece_sum<T>(load_piece<V>(body + (long long)q * n), base, once);
+            total = group_sum<kPartThreads>((once[0] + once[1]) + (once[2] + once[3]), red[2]);
+        }
+        if (tid == 0) {
+            if (parts > 1) {
+                partial[b] = {group, total};
+                if (j == 0) a.own[m] = xl;
+            } else {
+                a.own[m] = total == 0.f ? -INFINITY : xl - base;
+                a.sum[m] = total;
+            }
+        }
     }
 }
 
 // ---- the loss ----------------------------------------------------------------------------------
 // Its four sums, in a fixed order and in 64 bits, by one work-group.
-static constexpr int kSumThreads = 1024;
+static constexpr int kSumThreads = 1024, kSumGroups = 256;
 struct PolicySums {
     double loss, surrogate, kl, clipped;
+    __device__ __forceinline__ void add(const PolicySums& o) {
+        loss += o.loss;
+        surrogate += o.surrogate;
+        kl += o.kl;
+        clipped += o.clipped;
+    }
 };
 __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, double own, double sum, float* __restrict__ logp_out) {
     PolicySums s = {};
@@ -248,75 +534,209 @@ __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, doub
     return s;
 }
 template <int kThreads>
-__device__ __forceinline__ void put_sums(PolicySums s, double (*red)[4], float* __restrict__ loss_out) {
+__device__ __forceinline__ void group_sums(const PolicySums& s, double (*red)[4], double* out) {  // to [4]
     double of[4] = {s.loss, s.surrogate, s.kl, s.clipped};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) of[i] += __shfl_xor(of[i], d, 64);
+        of[i] = wave_sum(of[i]);
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6][i] = of[i];
     }
     __syncthreads();
     if (threadIdx.x >= 4) return;
     double t = 0.0;
     for (int w = 0; w < kThreads / 64; ++w) t += red[w][threadIdx.x];
-    loss_out[threadIdx.x] = (float)t;
+    out[threadIdx.x] = t;
 }
-__global__ __launch_bounds__(kSumThreads) void k_policy_sums(PolicyArgs a, int n, float* __restrict__ logp_out, float* __restrict__ loss_out) {
-    __shared__ double red[kSumThreads / 64][4];
+template <int kThreads>
+__device__ __forceinline__ void put_sums(const PolicySums& s, double (*red)[4], float* __restrict__ loss_out) {
+    __shared__ double total[4];
+    group_sums<kThreads>(s, red, total);
+    if (threadIdx.x < 4) loss_out[threadIdx.x] = (float)total[threadIdx.x];
+}
+// Thread `first` of `stride`: its items' share.
+__device__ __forceinline__ PolicySums items_sums(const PolicyArgs& a, int n, int first, int stride, float* __restrict__ logp_out) {
     PolicySums s = {};
-    for (int m = threadIdx.x; m < n; m += kSumThreads) {
-        const PolicySums t = item_sums(a, m, a.own[m], a.sum[m], logp_out);
-        s.loss += t.loss;
-        s.surrogate += t.surrogate;
-        s.kl += t.kl;
-        s.clipped += t.clipped;
+    for (int m = first; m < n; m += stride) s.add(item_sums(a, m, a.own[m], a.sum[m], logp_out));
+    return s;
+}
+// The same of rows that were summed in parts (own is the label's logit as it stands), by a work-group.  Parts are joined by as many lanes as there
+// are, several rows at once: a 64-bit exponential each is what this takes.
+template <int kThreads>
+__device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int vocab, int parts, const Partial* __restrict__ partial,
+                                                 float* __restrict__ logp_out) {
+    __shared__ double joined[kMaxPartials / 2];
+    __shared__ float largest[kMaxPartials / 2];
+    const int lanes = parts <= 1 ? 1 : 1 << (32 - __builtin_clz(parts - 1)), tid = threadIdx.x, j = tid & (lanes - 1);
+    for (int first = 0; first < n; first += kThreads / lanes) {
+        const int m = first + tid / lanes;
+        const bool counted = m < n && scores(a, m, vocab);
+        const Partial p = counted && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.f};
+        float most = p.most;
+        for (int d = lanes >> 1; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        const float base = most == -INFINITY ? 0.f : most;
+        double sum = part_in(p, base);
+        for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        if (m < n && j == 0) {
+            joined[m] = counted ? sum : -1.0;
+            largest[m] = base;
+        }
     }
-    put_sums<kSumThreads>(s, red, loss_out);
+    __syncthreads();
+    PolicySums s = {};
+    for (int m = tid; m < n; m += kThreads) {
+        const bool counted = joined[m] != -1.0;
+        const double sum = counted ? joined[m] : 0.0;
+        s.add(item_sums(a, m, !counted ? 0.0 : sum == 0.0 ? -INFINITY : (double)a.own[m] - (double)largest[m], sum, logp_out));
+    }
+    return s;
+}
+__global__ __launch_bounds__(kSumThreads) void k_policy_sums(PolicyArgs a, int n, int vocab, int parts, const Partial* __restrict__ partial,
+                                                             float* __restrict__ logp_out, float* __restrict__ loss_out) {
+    __shared__ double red[kSumThreads / 64][4];
+    if (parts > 1) put_sums<kSumThreads>(parts_sums<kSumThreads>(a, n, vocab, parts, partial, logp_out), red, loss_out);
+    else put_sums<kSumThreads>(items_sums(a, n, threadIdx.x, kSumThreads, logp_out), red, loss_out);
 }
 
+// Many items: a work-group to each kSumThreads of them (64-bit logarithms and exponentials take 18 us for 6001 items by one), and one that adds theirs.
+__global__ __launch_bounds__(kSumThreads) void k_policy_sums_of(PolicyArgs a, int n, float* __restrict__ logp_out, double (*__restrict__ sums)[4]) {
+    __shared__ double red[kSumThreads / 64][4];
+    group_sums<kSumThreads>(items_sums(a, n, blockIdx.x * kSumThreads + threadIdx.x, gridDim.x * kSumThreads, logp_out), red, sums[blockIdx.x]);
+}
+__global__ __launch_bounds__(64) void k_policy_sums_join(const double (*__restrict__ sums)[4], int n, float* __restrict__ loss_out) {
+    const int i = threadIdx.x & 3;
+    double t = 0.0;
+    for (int k = threadIdx.x >> 2; k < n; k += 16) t += sums[k][i];
+#pragma unroll
+    for (int d = 4; d < 64; d <<= 1) t += __shfl_xor(t, d, 64);
+    if (threadIdx.x < 4) loss_out[i] = (float)t;
+}
+static void launch_sums(const PolicyArgs& a, int n, void* scratch, float* logp_out, float* loss_out, hipStream_t stream) {
+    if (n <= 2 * kSumThreads) {  // (1501 items: 5.5 us, 10 by two launches)
+        k_policy_sums<<<1, kSumThreads, 0, stream>>>(a, n, 0, 0, nullptr, logp_out, loss_out);
+        return;
+    }
+    const int groups = std::min((n + kSumThreads - 1) / kSumThreads, kSumGroups);
+    const auto sums = static_cast<double(*)[4]>(scratch);
+    k_policy_sums_of<<<groups, kSumThreads, 0, stream>>>(a, n, logp_out, sums);
+    k_policy_sums_join<<<1, 64, 0, stream>>>(sums, groups, loss_out);
+}
+
+// The gradient of rows that were summed in parts, a work-group a part, and by the first work-group the loss.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* logits, long long ld, int vocab, PolicyArgs a, int rows, int parts,
+                                                                    const Partial* __restrict__ partial, T* dlogits, long long ld_grad,
+                                                                    float* __restrict__ logp_out, float* __restrict__ loss_out) {
+    typedef typename Piece<T>::type V;
+    constexpr int n = Piece<T>::n;
+    __shared__ double red[kPartThreads / 64][4];
+    const int tid = threadIdx.x, b = (int)blockIdx.x - 1;
+    if (b < 0) {
+        put_sums<kPartThreads>(parts_sums<kPartThreads>(a, rows, vocab, parts, partial, logp_out), red, loss_out);
+        return;
+    }
+    const int m = b / parts, j = b % parts;
+    const T* row = logits + m * ld;
+    T* out = dlogits + m * ld_grad;
+    const RowCut c = cut_row(row, vocab);
+    int begin, end;
+    part_of(c.pieces, j, parts, &begin, &end);
+    const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m];
+    float base = 0.f, scale = 0.f, at_label = 0.f;
+    bool some = false;  // logits that the gradient depends on
+    if (scores(a, m, vocab)) {
+        const Whole w = whole_row(partial + (long long)m * parts, parts);
+        some = w.sum != 0.f;
+        if (some) {
+            const float logp = a.own[m] - w.base - logf(w.sum), d = slope(a, m, logp);
+            base = w.base;
+            scale = -d / w.sum;
+            at_label = d * -expm1f(logp);
+        }
+    }
+    const GradOf grad = grad_of(base, scale);
+#pragma unroll 4
+    for (int p = begin + tid; p < end; p += kPartThreads) {
+        V g = {};
+        if (some) g = with_label<T>(piece_grad<T>(load_piece<V>(row + c.head + (long long)p * n), grad), label - c.head - p * n, at_label);
+        store_piece(out + c.head + (long long)p * n, g);
+    }
+    if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? at_label : scale * grown((float)row[extra], base));
+}
+
+// Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole.
+static int parts_of(int rows, int vocab, size_t element) {
+    const long long wanted = ((long long)vocab * (long long)element + 8191) / 8192;
+    return (int)std::max<long long>(std::min<long long>(std::min<long long>(wanted, kMaxParts), kMaxPartials / rows), 1);
+}
+
+size_t policy_scratch_bytes() { return std::max(kMaxPartials * sizeof(Partial), kSumGroups * 4 * sizeof(double)); }
 size_t policy_loss_workspace_bytes(int n_items, int vocab) {
     (void)vocab;
-    return round_up((size_t)(n_items > 0 ? n_items : 1) * 2 * sizeof(float), 256);
+    return round_up((size_t)(n_items > 0 ? n_items : 1) * 2 * sizeof(float), 256) + policy_scratch_bytes();
 }
 
 static PolicyArgs policy_args(const alch_policy& p, int item0, float* own, float* sum) {
-    return {p.label + item0, p.old_logp + item0, p.advantage + item0, p.weight + item0, p.ref_logp ? p.ref_logp + item0 : nullptr,
-            1.f - p.clip_low, 1.f + p.clip_high, p.kl_coef, own + item0, sum + item0};
-}
-
-template <typename T, bool kGrad>
-static void launch_held(const T* logits, long long ld, int rows, int vocab, const PolicyArgs& a, T* dlogits, long long ld_grad, hipStream_t stream) {
-    const int pieces = vocab / Piece<T>::n + 1;
-    const auto go = [&](auto kernel, int threads) { kernel<<<rows, threads, 0, stream>>>(logits, ld, vocab, a, dlogits, ld_grad); };
-    if (pieces <= 256) go(k_policy_held<T, 256, 1, kGrad>, 256);
-    else if (pieces <= 256 * 4) go(k_policy_held<T, 256, 4, kGrad>, 256);
-    else if (pieces <= 256 * 8) go(k_policy_held<T, 256, 8, kGrad>, 256);
-    else if (pieces <= 256 * 16) go(k_policy_held<T, 256, 16, kGrad>, 256);
-    else if (pieces <= 512 * 16) go(k_policy_held<T, 512, 16, kGrad>, 512);
-    else go(k_policy_held<T, 1024, 16, kGrad>, 1024);
+    return PolicyArgs{p.label, p.old_logp, p.advantage, p.weight, p.ref_logp, 1.f - p.clip_low, 1.f + p.clip_high, p.kl_coef, own, sum}.from(item0);
 }
 
 template <typename T>
-static void launch_rows(const T* logits, long long ld, int rows, int vocab, const PolicyArgs& a, T* dlogits, long long ld_grad, hipStream_t stream) {
-    if (dlogits) launch_held<T, true>(logits, ld, rows, vocab, a, dlogits, ld_grad, stream);
-    else launch_held<T, false>(logits, ld, rows, vocab, a, dlogits, ld_grad, stream);
+static void launch_held(const T* logits, long long ld, int rows, int vocab, const PolicyArgs& a, T* dlogits, long long ld_grad, hipStream_t stream) {
+    const int pieces = vocab / Piece<T>::n + 1;
+    const auto go = [&](auto kernel, int threads) {
+        for (int r = 0; r < rows; r += kGridMax)
+            kernel<<<std::min(rows - r, kGridMax), threads, 0, stream>>>(logits + r * ld, ld, vocab, a.from(r), dlogits + r * ld_grad, ld_grad);
+    };
+    if (pieces <= 256) go(k_policy_held<T, 256, 1>, 256);
+    else if (pieces <= 256 * 4) go(k_policy_held<T, 256, 4>, 256);
+    else if (pieces <= 256 * 8) go(k_policy_held<T, 256, 8>, 256);
+    else if (pieces <= 256 * 16) go(k_policy_held<T, 256, 16>, 256);
+    else if (pieces <= 512 * 16) go(k_policy_held<T, 512, 16>, 512);
+    else go(k_policy_held<T, 1024, 16>, 1024);
 }
 
-int launch_policy_rows(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits,
-                       long long ld_grad, float* own, float* sum, hipStream_t stream) {
-    if (rows <= 0) return ALCH_OK;
+template <typename T>
+static int launch_rows(const T* logits, long long ld, int rows, int vocab, const PolicyArgs& a, T* dlogits, long long ld_grad, Partial* partial,
+                       float* logp_out, float* loss_out, hipStream_t stream) {
+    int n_cu = 0;
+    ALCH_TRY(compute_units(&n_cu));
+    const int pieces = vocab / Piece<T>::n + 1, parts = loss_out ? parts_of(rows, vocab, sizeof(T)) : 1;
+    if (parts > 1 || !dlogits) {
+        k_policy_parts<<<(int)std::min<long long>((long long)rows * parts, kGridMax), kPartThreads, 0, stream>>>(logits, ld, rows, vocab, a, parts, partial);
+        if (dlogits)
+            k_policy_part_grads<<<rows * parts + 1, kPartThreads, 0, stream>>>(logits, ld, vocab, a, rows, parts, partial, dlogits, ld_grad, logp_out, loss_out);
+        else if (parts > 1)
+            k_policy_sums<<<1, kSumThreads, 0, stream>>>(a, rows, vocab, parts, partial, logp_out, loss_out);
+        else if (loss_out)
+            launch_sums(a, rows, partial, logp_out, loss_out, stream);
+        return ALCH_OK;
+    }
+    // pieces of both matrices' rows begin together, and the row fits
+    const bool alike = (ld - ld_grad) * (long long)sizeof(T) % 16 == 0;
+    if (alike && pieces > 512 * 16 && pieces <= kStayThreads * kStayPieces)
+        k_policy_stay<<<std::min(rows, n_cu), kStayThreads, 0, stream>>>(logits, ld, rows, vocab, a, dlogits, ld_grad);
+    else
+        launch_held<T>(logits, ld, rows, vocab, a, dlogits, ld_grad, stream);
+    if (loss_out) launch_sums(a, rows, partial, logp_out, loss_out, stream);
+    return ALCH_OK;
+}
+
+int launch_policy(alch_dtype dt, const void* logits, long long ld, int rows, int vocab, const alch_policy& p, int item0, void* dlogits, long long ld_grad,
+                  float* own, float* sum, void* scratch, float* loss_out, hipStream_t stream) {
+    if (rows <= 0) return loss_out ? launch_policy_sums(p, own, sum, scratch, loss_out, stream) : ALCH_OK;
     const double E = (double)dtype_size(dt);
     TraceScope ts(kTraceCrossEntropy, 0.0, (double)rows * vocab * E * (dlogits ? 2 : 1), stream);
     const PolicyArgs a = policy_args(p, item0, own, sum);
-    if (dt == ALCH_BF16) launch_rows(static_cast<const __bf16*>(logits), ld, rows, vocab, a, static_cast<__bf16*>(dlogits), ld_grad, stream);
-    else launch_rows(static_cast<const float*>(logits), ld, rows, vocab, a, static_cast<float*>(dlogits), ld_grad, stream);
+    Partial* partial = static_cast<Partial*>(scratch);
+    if (dt == ALCH_BF16)
+        ALCH_TRY(launch_rows(static_cast<const __bf16*>(logits), ld, rows, vocab, a, static_cast<__bf16*>(dlogits), ld_grad, partial, p.logp_out, loss_out, stream));
+    else
+        ALCH_TRY(launch_rows(static_cast<const float*>(logits), ld, rows, vocab, a, static_cast<float*>(dlogits), ld_grad, partial, p.logp_out, loss_out, stream));
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }
 
-int launch_policy_sums(const alch_policy& p, float* own, float* sum, float* loss_out, hipStream_t stream) {
-    k_policy_sums<<<1, kSumThreads, 0, stream>>>(policy_args(p, 0, own, sum), p.n_items, p.logp_out, loss_out);
+int launch_policy_sums(const alch_policy& p, float* own, float* sum, void* scratch, float* loss_out, hipStream_t stream) {
+    launch_sums(policy_args(p, 0, own, sum), p.n_items, scratch, p.logp_out, loss_out, stream);
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
 }

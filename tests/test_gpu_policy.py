@@ -33,6 +33,7 @@ def make(n, V, dtype, seed, std=3.0, pad=0, kl=True):
 def formula(x, label, old, adv, weight, ref, kl_coef=KL, low=LOW, high=HIGH):
     """(loss [4], logp, dlogits) in 64 bits, and what the tolerances are made of."""
     x, V = x.double(), x.shape[1]
+    x = x - x.max(1, keepdim=True).values  # (64 bits lose the logarithm of a sum beside a logit of 1e38)
     counted = (label >= 0) & (label < V) & (weight != 0)
     safe = label.long().clamp(0, V - 1)
     logz = torch.logsumexp(x, 1)
@@ -163,6 +164,29 @@ def test_items_that_score_nothing_and_forbidden_tokens(dtype, V):
     fine = [0, 3, 5, 6, 7]
     loss, logp, _ = run({k: v[fine].contiguous() if v is not None else None for k, v in e.items()})
     assert bool(torch.isfinite(loss).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(3, 5000), (3, 128256), (300, 2000), (600, 40000), (300, 100000)])
+def test_rows_of_the_lowest_value_and_of_huge_ones(dtype, n, V):
+    """Finite logits of any size have a distribution: a row all of whose tokens were masked with the type's lowest value is uniform, one among
+    masked ones has all of it, and the difference of large logits counts, not their size."""
+    import paper_2503_01066_amd as A
+    c = make(n, V, dtype, 2)
+    low, at = torch.finfo(DT[dtype]).min, c["label"].long()[:, None]
+    c["x"][0] = low
+    c["x"][1] = low
+    c["x"][1].scatter_(0, at[1], 3.0)
+    c["x"][2, : V // 2] = low
+    for r, by in ((n // 2, 3e5), (n // 2 + 1, -3e5), (n - 2, 1e30), (n - 1, -1e30)):
+        if r > 2:
+            c["x"][r] = by
+    logp = torch.log_softmax(c["x"].double(), 1).gather(1, at)[:, 0]
+    c["old"], c["ref"] = (logp + 0.05).float(), (logp - 0.1).float()
+    _, got, dx = check(A, c)
+    assert abs(got[0].item() + math.log(V)) <= 1e-5 and got[1].item() == 0.0 and bool((dx[1] == 0).all())
+    f = A.alch_policy_loss(c["x"], A.PolicyItems(c["label"], c["old"], c["adv"], c["weight"], ref_logp=c["ref"]), clip_low=LOW, clip_high=HIGH, kl_coef=KL, want_grad=False)
+    assert bool(((f[1].double() - logp).abs() <= 1e-5 * (1 + logp.abs())).all())
 
 
 def test_clipping_and_its_bounds():
