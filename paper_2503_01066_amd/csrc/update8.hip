@@ -19,10 +19,19 @@
 namespace alch {
 
 static constexpr int kBlock = ALCH_ADAMW8_BLOCK;
-static constexpr int kChunk = 1024;  // elements, four a thread: 16 blocks, a block a row of 16 lanes
+// Elements of a chunk: four a thread and round, so that a block is a row of 16 lanes.  A work-group's look for its chunk is 150 instructions of each
+// wavefront, which more rounds share.
+static constexpr int kRound = 1024, kRounds = 4, kChunk = kRound * kRounds;
 
 typedef float f32x4_a __attribute__((ext_vector_type(4)));
+typedef float f32x2_a __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4_a __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_a __attribute__((ext_vector_type(4)));
+
+// Pointers out of the table: without the address space they would be flat ones, whose loads also wait for LDS.
+template <typename T> using Global = __attribute__((address_space(1))) T*;
+template <typename T>
+__device__ __forceinline__ Global<T> global(T* p) { return (Global<T>)p; }
 
 struct Adamw8Args {
     const alch_adamw8_tensor* tensors;
@@ -48,40 +57,58 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ f32x4_a load4(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_a*>(p)); }
-__device__ __forceinline__ f32x4_a load4(const __bf16* p) {
-    return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const bf16x4_a*>(p)), f32x4_a);
-}
-__device__ __forceinline__ void store4(float* p, f32x4_a v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4_a*>(p)); }
-__device__ __forceinline__ void store4(__bf16* p, f32x4_a v) {
-    __builtin_nontemporal_store(__builtin_convertvector(v, bf16x4_a), reinterpret_cast<bf16x4_a*>(p));
-}
-// Four consecutive elements, of which n are there.
-template <typename V, typename T>
-__device__ __forceinline__ V load_some(const T* p, int n) {
-    V v = {};
+// Four consecutive elements, of which n are there; kFull: all of them.
+template <bool kFull>
+__device__ __forceinline__ f32x4_a load4(Global<const float> p, int n) {
+    if constexpr (kFull) return __builtin_nontemporal_load((Global<const f32x4_a>)p);
+    f32x4_a v = {};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (e < n) v[e] = p[e];
     return v;
 }
-template <typename T>
-__device__ __forceinline__ void store_some(T* p, f32x4_a v, int n) {
+template <bool kFull>
+__device__ __forceinline__ f32x4_a load4(Global<const __bf16> p, int n) {
+    if constexpr (kFull) return __builtin_convertvector(__builtin_nontemporal_load((Global<const bf16x4_a>)p), f32x4_a);
+    f32x4_a v = {};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (e < n) p[e] = (T)v[e];
+        if (e < n) v[e] = (float)p[e];
+    return v;
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n) {
-    if (n == 4) return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+template <bool kFull>
+__device__ __forceinline__ void store4(Global<float> p, f32x4_a v, int n) {
+    if constexpr (kFull) {
+        __builtin_nontemporal_store(v, (Global<f32x4_a>)p);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < n) p[e] = v[e];
+}
+template <bool kFull>
+__device__ __forceinline__ void store4(Global<__bf16> p, f32x4_a v, int n) {
+    if constexpr (kFull) {
+        __builtin_nontemporal_store(__builtin_convertvector(v, bf16x4_a), (Global<bf16x4_a>)p);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < n) p[e] = (__bf16)v[e];
+}
+template <bool kFull>
+__device__ __forceinline__ uint32_t load_codes(Global<const uint8_t> p, int n) {
+    if constexpr (kFull) return __builtin_nontemporal_load((Global<const uint32_t>)p);
     uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (e < n) w |= (uint32_t)p[e] << (8 * e);
     return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t w, int n) {
-    if (n == 4) {
-        __builtin_nontemporal_store(w, reinterpret_cast<uint32_t*>(p));
+template <bool kFull>
+__device__ __forceinline__ void store_codes(Global<uint8_t> p, uint32_t w, int n) {
+    if constexpr (kFull) {
+        __builtin_nontemporal_store(w, (Global<uint32_t>)p);
         return;
     }
 #pragma unroll
@@ -92,23 +119,30 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t w, int n) {
 __device__ __forceinline__ float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t as_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return byte == 255u ? __builtin_nanf("") : as_float(byte << 23); }
-// (codes below 8 are denormal numbers here, which the product makes normal)
-__device__ __forceinline__ float from_m(uint32_t code) {
-    return (code & 0x7fu) == 0x7fu ? __builtin_nanf("") : as_float((code & 0x80u) << 24 | (code & 0x7fu) << 20) * 0x1p120f;
+__device__ __forceinline__ f32x4_a from_m(uint32_t codes) {
+    const f32x2_a a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    return f32x4_a{a[0], a[1], b[0], b[1]};
 }
-__device__ __forceinline__ float from_v(uint32_t code) { return as_float(code << 20) * 0x1p112f; }
+// (codes below 8 are denormal numbers here, which the product makes normal)
+__device__ __forceinline__ f32x4_a from_v(uint32_t codes) {
+    constexpr uint32_t kMask = 0x0ff00000u;
+    return f32x4_a{as_float(codes << 20 & kMask), as_float(codes << 12 & kMask), as_float(codes << 4 & kMask), as_float(codes >> 4 & kMask)} * 0x1p112f;
+}
 
-// y >= 0 as a code whose smallest normal value is 2^kLowest: 3 bits of mantissa, rounded up where the 20 bits behind them and the random
-// ones carry.  Below 2^kLowest the codes are evenly spaced, as they are in the next binade: there the value is moved.
+// y >= 0 (its bits, and itself) as a code in the byte above bit 20 whose smallest normal value is 2^kLowest: 3 bits of mantissa, rounded up where the
+// 20 bits behind them and the random ones carry.  Below 2^kLowest the codes are as far apart as in the next binade, and y is moved there
+// by adding 2^kLowest; of the two readings the right one is the larger (they meet at 2^kLowest, where the slopes of bits over value cross).
 template <int kLowest>
 __device__ __forceinline__ uint32_t to_code(float y, uint32_t random16) {
-#pragma clang fp contract(off)
     constexpr float kSmall = kLowest == -6 ? 0x1p-6f : 0x1p-14f;
-    constexpr uint32_t kBias = (126 + kLowest) * 8;
+    constexpr uint32_t kBias = (uint32_t)(126 + kLowest) << 23;
     static_assert(kLowest == -6 || kLowest == -14, "");
-    const bool small = y < kSmall;
-    const uint32_t bits = as_bits(small ? y + kSmall : y);
-    return ((bits + (random16 << 4)) >> 20) - (small ? kBias + 8 : kBias);
+    const uint32_t bits = max(as_bits(y), as_bits(y + kSmall) - (8u << 20));
+    return (bits + ((random16 << 4) - kBias)) >> 20;
+}
+__device__ __forceinline__ uint32_t bytes4(const u32x4_a& c, uint32_t select) {  // the byte that select names of each
+    const uint32_t low = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u + select * 0x0101u), high = __builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400u + select * 0x0101u);
+    return __builtin_amdgcn_perm(high, low, 0x05040100u);
 }
 
 template <int kCtrl>
@@ -126,76 +160,111 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
 }
 __device__ __forceinline__ float inverse(uint32_t byte) { return as_float((254u - min(byte, 253u)) << 23); }
 
-template <typename T, bool kMaster>
+// sqrt(v), one unit in the last place; the instruction takes denormal numbers for 0, so that where a wavefront has numbers near them all are moved.
+__device__ __forceinline__ f32x4_a root(f32x4_a v) {
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) least = min(least, as_bits(v[e]) - 1u);  // (0 is no such number)
+    float up = 1.f, down = 1.f;
+    if (__builtin_expect(__any(least < 0x10000000u), 0)) {  // 2^-95
+        const bool move = least < 0x10000000u;
+        f32x4_a r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool tiny = move && v[e] < 0x1p-95f;
+            up = tiny ? 0x1p64f : 1.f;
+            down = tiny ? 0x1p-32f : 1.f;
+            r[e] = __builtin_amdgcn_sqrtf(v[e] * up) * down;
+        }
+        return r;
+    }
+    f32x4_a r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_sqrtf(v[e]);
+    return r;
+}
+
+template <typename T, bool kMaster, bool kFull>
 __device__ __forceinline__ void adamw8(const alch_adamw8_tensor& t, long long begin, int elements, const Adamw8Args& a, const Rates& r) {
 #pragma clang fp contract(off)
-    const int own = threadIdx.x * 4, n = min(max(elements - own, 0), 4);
+    const int own = threadIdx.x * 4, n = kFull ? 4 : min(max(elements - own, 0), 4);
     const long long at = begin + own, block = at / kBlock;
-    const bool there = (own & ~(kBlock - 1)) < elements;  // some of its block is
-    f32x4_a g = {}, w = {};
-    uint32_t mc = 0, vc = 0, ms = 0, vs = 0;
-    const T* grad = static_cast<const T*>(t.grad) + at;
-    T* param = static_cast<T*>(t.param) + at;
-    if (n == 4) {
-        g = load4(grad);
-        if constexpr (kMaster) w = load4(t.master + at);
-        else w = load4(param);
-    } else if (n > 0) {
-        g = load_some<f32x4_a>(grad, n);
-        if constexpr (kMaster) w = load_some<f32x4_a>(t.master + at, n);
-        else w = load_some<f32x4_a>(param, n);
-    }
-    if (n > 0) {
-        mc = load_codes(t.m + at, n);
-        vc = load_codes(t.v + at, n);
-    }
+    const bool there = kFull || (own & ~(kBlock - 1)) < elements;  // some of its block is
+    const auto grad = global(static_cast<const T*>(t.grad)) + at;
+    const auto param = global(static_cast<T*>(t.param)) + at;
+    const auto master = global(t.master) + at;
+    const auto mp = global(t.m) + at, vp = global(t.v) + at;
+    const auto msp = global(t.m_scale) + block, vsp = global(t.v_scale) + block;
+    const f32x4_a g = load4<kFull>((Global<const T>)grad, n);
+    f32x4_a w;
+    if constexpr (kMaster) w = load4<kFull>((Global<const float>)master, n);
+    else w = load4<kFull>((Global<const T>)param, n);
+    const uint32_t mc = load_codes<kFull>((Global<const uint8_t>)mp, n), vc = load_codes<kFull>((Global<const uint8_t>)vp, n);
+    uint32_t ms = 0, vs = 0;
     if (there) {
-        ms = t.m_scale[block];
-        vs = t.v_scale[block];
+        ms = *msp;
+        vs = *vsp;
     }
     const float sm = scale_of(ms), sv = scale_of(vs);
-    f32x4_a m, v;
+    f32x4_a m = from_m(mc), v = from_v(vc);
     uint32_t most_m = 0, most_v = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float x = g[e] * r.factor;
-        m[e] = from_m(mc >> (8 * e) & 0xffu) * sm * a.b1 + x * a.d1;
-        v[e] = from_v(vc >> (8 * e) & 0xffu) * sv * a.b2 + x * x * a.d2;
-        if (e >= n) m[e] = v[e] = 0.f;  // (behind the tensor: a block that is NaN makes these NaN too, which would not matter)
+        m[e] = m[e] * sm * a.b1 + x * a.d1;
+        v[e] = v[e] * sv * a.b2 + x * x * a.d2;
+        if (!kFull && e >= n) m[e] = v[e] = 0.f;  // (behind the tensor; a block that is NaN would make these NaN too)
         most_m = max(most_m, as_bits(m[e]) & 0x7fffffffu);
-        most_v = max(most_v, as_bits(v[e]) & 0x7fffffffu);
-        w[e] -= r.lr * (m[e] * r.c1 / (sqrtf(v[e]) * r.c2 + a.eps) + t.weight_decay * w[e]);
+        most_v = max(most_v, as_bits(v[e]));
     }
-    const uint32_t nms = scale_byte<7>(max_of_16(most_m)), nvs = scale_byte<15>(max_of_16(most_v));
+    // (a v that is NaN may have its sign bit set)
+    const uint32_t nms = scale_byte<7>(max_of_16(most_m)), nvs = scale_byte<15>(max_of_16(most_v) & 0x7fffffffu);
     const float im = inverse(nms), iv = inverse(nvs);
-    uint32_t nm = 0, nv = 0;
+    const unsigned long long first = (unsigned long long)(t.first + at);
+    const uint32_t upper = (uint32_t)((unsigned long long)(t.first + begin) >> 32);
+    u32x4_a random, cm, cv, ym;
+    if (__builtin_expect((uint32_t)((unsigned long long)(t.first + begin + kRound - 1) >> 32) == upper, 1)) {
+        const uint32_t key = (uint32_t)__builtin_amdgcn_readfirstlane((int)mix(r.key ^ upper));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) random[e] = mix((uint32_t)first + e + key);
+    } else {  // the numbers' upper half changes among these
+#pragma unroll
+        for (int e = 0; e < 4; ++e) random[e] = mix((uint32_t)(first + e) + mix(r.key ^ (uint32_t)((first + e) >> 32)));
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const unsigned long long number = (unsigned long long)(t.first + at + e);
-        const uint32_t random = mix((uint32_t)number + ((number >> 32) ? mix(r.key ^ (uint32_t)(number >> 32)) : mix(r.key)));
         const float y = m[e] * im;
-        uint32_t c = to_code<-6>(fabsf(y), random & 0xffffu) | (as_bits(y) >> 31 << 7);
-        if (nms == 255u) c = 127u;
-        nm |= c << (8 * e);
-        c = to_code<-14>(v[e] * iv, random >> 16);
-        if (v[e] > 0.f && c == 0u) c = 1u;
-        if (nvs == 255u) c = 255u;
-        nv |= c << (8 * e);
+        ym[e] = as_bits(y);
+        cm[e] = to_code<-6>(fabsf(y), random[e] & 0xffffu);
+        cv[e] = max(to_code<-14>(v[e] * iv, random[e] >> 16), min(as_bits(v[e]), 1u));  // (0 for 0 alone)
     }
-    if (n > 0) {
-        store_codes(t.m + at, nm, n);
-        store_codes(t.v + at, nv, n);
-    }
+    uint32_t nm = bytes4(cm, 0) | (bytes4(ym, 3) & 0x80808080u), nv = bytes4(cv, 0);
+    if (nms == 255u) nm = 0x7f7f7f7fu;
+    if (nvs == 255u) nv = 0xffffffffu;
+    store_codes<kFull>(mp, nm, n);
+    store_codes<kFull>(vp, nv, n);
     if (there && (own & (kBlock - 1)) == 0) {
-        t.m_scale[block] = (uint8_t)nms;
-        t.v_scale[block] = (uint8_t)nvs;
+        *msp = (uint8_t)nms;
+        *vsp = (uint8_t)nvs;
     }
-    if (n == 4) {
-        if constexpr (kMaster) store4(t.master + at, w);
-        store4(param, w);
-    } else if (n > 0) {
-        if constexpr (kMaster) store_some(t.master + at, w, n);
-        store_some(param, w, n);
+    const f32x4_a q = root(v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float change = m[e] * r.c1 * __builtin_amdgcn_rcpf(fmaf(q[e], r.c2, a.eps));
+        w[e] = fmaf(-r.lr, fmaf(t.weight_decay, w[e], change), w[e]);
+    }
+    if constexpr (kMaster) store4<kFull>(master, w, n);
+    store4<kFull>(param, w, n);
+}
+template <typename T, bool kMaster>
+__device__ __forceinline__ void adamw8_chunk(const alch_adamw8_tensor& t, long long begin, const Adamw8Args& a, const Rates& r) {
+    const long long left = (long long)t.n - begin;
+    if (left >= kChunk) {
+#pragma unroll 1
+        for (int k = 0; k < kRounds; ++k) adamw8<T, kMaster, true>(t, begin + k * kRound, kRound, a, r);
+    } else {
+#pragma unroll 1
+        for (long long at = 0; at < left; at += kRound) adamw8<T, kMaster, false>(t, begin + at, (int)min((long long)kRound, left - at), a, r);
     }
 }
 
@@ -219,13 +288,12 @@ __global__ __launch_bounds__(256) void k_adamw8(Adamw8Args a) {
     for (int c = blockIdx.x; c < table.chunks; c += gridDim.x) {
         const auto k = table.find(c);
         const long long begin = (long long)k.index * kChunk;
-        const int elements = (int)min((long long)kChunk, (long long)k.t.n - begin);
         if (k.t.dtype == ALCH_BF16) {
-            if (k.t.master) adamw8<__bf16, true>(k.t, begin, elements, a, r);
-            else adamw8<__bf16, false>(k.t, begin, elements, a, r);
+            if (k.t.master) adamw8_chunk<__bf16, true>(k.t, begin, a, r);
+            else adamw8_chunk<__bf16, false>(k.t, begin, a, r);
         } else {
-            if (k.t.master) adamw8<float, true>(k.t, begin, elements, a, r);
-            else adamw8<float, false>(k.t, begin, elements, a, r);
+            if (k.t.master) adamw8_chunk<float, true>(k.t, begin, a, r);
+            else adamw8_chunk<float, false>(k.t, begin, a, r);
         }
     }
 }

@@ -228,6 +228,30 @@ def test_values_that_are_no_numbers_and_extremes():
     assert bool(torch.isfinite(again[0][0].view(-1, 64)[8:]).all())
 
 
+def test_second_moments_near_the_smallest_numbers():
+    """Their roots are divided by as they are, without eps too."""
+    import paper_2503_01066_amd as A
+    n = 64 * 9 + 5
+    r = np.random.default_rng(3)
+    grad = torch.from_numpy((10.0 ** r.uniform(-22, -13, n) * r.choice([-1, 1], n)).astype(np.float32)).cuda()
+    grad[:64] = torch.from_numpy((10.0 ** r.uniform(-19.5, -18.5, 64)).astype(np.float32)).cuda()
+    grad[64] = 1.0  # (a block of usual size with tiny ones in it)
+    grad = torch.where(grad.abs() < 3e-21, torch.zeros_like(grad), grad)  # (whose squares, times 1 - beta2, would be no numbers but 0)
+    grad[(grad.double().square() * 0.001).float() == 0] = 0
+    before = [[torch.ones(n, device="cuda"), grad, None]]
+    zeros = (np.zeros(n, np.uint8), np.zeros(10, np.uint8))
+    after = [[x.clone() if x is not None else None for x in before[0]]]
+    hyper = dict(HYPER, eps=0.0)
+    ms, vs, firsts = run(A, after, [(zeros, zeros)], [0.0], step=1, **hyper)
+    zero = (grad == 0)
+    assert bool(torch.isnan(after[0][0][zero]).all()) and int((~zero).sum()) > 400  # (0 / 0, as without eps it is)
+    codes, nw, ew = reference(*before[0][:2], zeros, zeros, None, 0.0, 1.0, seed=7, first=0, step=1, **hyper)
+    keep = ~zero.cpu().numpy()
+    assert (np.abs(after[0][0].double().cpu().numpy() - nw)[keep] <= ew[keep]).all()
+    for x, y in zip(ms[0] + vs[0], codes):
+        assert np.array_equal(x.cpu().numpy(), y)
+
+
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_factor_or_step_that_changes_nothing(bad):
     import paper_2503_01066_amd as A
