@@ -374,35 +374,30 @@ def alch_capture_gather(batch, kept_index, status, streams, capacity=None, dsts=
 Q8_GROUP = 64  # elements of a row that share a scale
 
 
-def _q8_words(tensors, pairs, index):
-    """The array of a call on records in 8 bits, as the six 64-bit words of each entry, and the most rows that all codes can hold."""
-    words, rows = [], None
+def _q8_entries(tensors, pairs, rows, index, what):
+    """The array of a call on records in 8 bits for tensors of so many rows: what the call takes (and keeps), and the rows that all codes have.
+    (18 tensors for six streams: 9 us here, 1.5 by the extension)"""
+    out = None if _marshal is None else _marshal.q8_entries(tensors, pairs, rows, index)
+    if out is not None:
+        return out
     if len(tensors) != len(pairs):
         raise ValueError("%d tensors, %d pairs of codes and scales" % (len(tensors), len(pairs)))
+    words, least = array("Q"), None
     for k, (t, (codes, scales)) in enumerate(zip(tensors, pairs)):
         held, width = codes.shape
-        size, stride = t.element_size(), t.stride()
-        if t.dim() != 2 or t.shape[1] != width or t.get_device() != index or (width > 1 and stride[1] != 1 and t.numel() > 0):
-            raise ValueError("tensor %d: rows of %d elements one after another on cuda:%d are needed, got %s with strides %s on %s" % (
-                k, width, index, tuple(t.shape), stride, t.device))
-        if codes.dtype is not torch.int8 or not codes.is_contiguous() or codes.get_device() != index:
-            _check_dense(codes, ("codes", k), torch.int8, index)
-        if scales.dtype is not torch.float32 or scales.shape != (held, -(-width // Q8_GROUP)) or not scales.is_contiguous() or scales.get_device() != index:
-            _check_dense(scales, ("scales", k), torch.float32, index, (held, -(-width // Q8_GROUP)))
-        rows = held if rows is None or held < rows else rows
-        words += (t.data_ptr(), codes.data_ptr(), scales.data_ptr(), width, (stride[0] if t.shape[0] > 1 else width) * size, _code(t.dtype))
-    return array("Q", words), rows
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.get_device() != index or (width > 1 and t.stride(1) != 1):
+            raise ValueError("%s[%d]: %d rows of %d elements, one after another, on cuda:%d are needed, got %s with strides %s on %s" % (
+                what, k, rows, width, index, tuple(t.shape), t.stride(), t.device))
+        _check_dense(codes, ("codes", k), torch.int8, index)
+        _check_dense(scales, ("scales", k), torch.float32, index, (held, -(-width // Q8_GROUP)))
+        least = held if least is None else min(least, held)
+        words.extend((t.data_ptr(), codes.data_ptr(), scales.data_ptr(), width, (t.stride(0) if rows > 1 else width) * t.element_size(), _code(t.dtype)))
+    return words.tobytes(), least
 
 
 def _q8_pairs(rows, streams, stream):
     return [(_empty((rows, s.shape[1]), torch.int8, s.device, stream), _empty((rows, -(-s.shape[1] // Q8_GROUP)), torch.float32, s.device, stream))
             for s in streams]
-
-
-def _rows_of_batch(streams, batch):
-    for k, s in enumerate(streams):
-        if s.shape[0] != batch.total_tokens:
-            raise ValueError("streams[%d] has %d rows, the batch %d tokens" % (k, s.shape[0], batch.total_tokens))
 
 
 def alch_capture_pack_q8(batch, keep_mask, streams, capacity=None, dsts=None, stream=None, workspace=None):
@@ -414,11 +409,10 @@ def alch_capture_pack_q8(batch, keep_mask, streams, capacity=None, dsts=None, st
     handle = _place(dev, stream)
     if keep_mask.element_size() != 1 or keep_mask.numel() != T or not keep_mask.is_contiguous():
         raise ValueError("keep_mask: a byte for each of the %d tokens is needed, got %s %s" % (T, keep_mask.dtype, tuple(keep_mask.shape)))
-    _rows_of_batch(streams, batch)
     if dsts is None:
         capacity = T if capacity is None else int(capacity)
         dsts = _q8_pairs(capacity, streams, stream)
-    words, held = _q8_words(streams, dsts, dev)
+    entries, held = _q8_entries(streams, dsts, T, dev, "streams")
     if capacity is None:
         capacity = T if held is None else held
     elif held is not None and held < capacity:
@@ -431,9 +425,10 @@ def alch_capture_pack_q8(batch, keep_mask, streams, capacity=None, dsts=None, st
     rows, bounds = max(capacity, 1), batch.n_seqs + 1
     out = _empty((rows + bounds + 2,), torch.int32, keep_mask.device, stream)
     at = out.data_ptr()
-    _check(L.alch_capture_pack_q8(C.byref(batch.c), keep_mask.data_ptr(), len(streams), words.buffer_info()[0], capacity, at, at + 4 * rows,
+    _check(L.alch_capture_pack_q8(C.byref(batch.c), keep_mask.data_ptr(), len(streams), entries, capacity, at, at + 4 * rows,
                                   at + 4 * (rows + bounds), workspace.data_ptr(), workspace.numel(), handle))
-    return out[:rows], out[rows:rows + bounds], out[rows + bounds:], dsts
+    index, cu_kept, status = out.split((rows, bounds, 2))
+    return index, cu_kept, status, dsts
 
 
 def alch_capture_gather_q8(batch, streams, kept_index=None, status=None, capacity=None, dsts=None, stream=None):
@@ -443,7 +438,6 @@ def alch_capture_gather_q8(batch, streams, kept_index=None, status=None, capacit
     T = batch.total_tokens
     dev = streams[0].get_device() if len(streams) else batch.cu_dev.get_device()
     handle = _place(dev, stream)
-    _rows_of_batch(streams, batch)
     if (kept_index is None) != (status is None):
         raise ValueError("kept_index and status are given together")
     if kept_index is not None:
@@ -453,14 +447,14 @@ def alch_capture_gather_q8(batch, streams, kept_index=None, status=None, capacit
     if dsts is None:
         capacity = most if capacity is None else int(capacity)
         dsts = _q8_pairs(capacity, streams, stream)
-    words, held = _q8_words(streams, dsts, dev)
+    entries, held = _q8_entries(streams, dsts, T, dev, "streams")
     if capacity is None:
         capacity = most if held is None else min(held, most) if kept_index is not None else held
     elif held is not None and held < capacity:
         raise ValueError("dsts hold %d rows, capacity is %d" % (held, capacity))
     if kept_index is not None and capacity > kept_index.numel():
         raise ValueError("capacity is %d, kept_index has %d rows" % (capacity, kept_index.numel()))
-    _check(L.alch_capture_gather_q8(C.byref(batch.c), len(streams), words.buffer_info()[0], capacity, _ptr(kept_index), _ptr(status), handle))
+    _check(L.alch_capture_gather_q8(C.byref(batch.c), len(streams), entries, capacity, _ptr(kept_index), _ptr(status), handle))
     return dsts
 
 
@@ -484,11 +478,10 @@ def alch_record_expand(records, outs=None, rows=None, dtype=torch.bfloat16, n_ro
         n = held if n_rows is None else int(n_rows)
     if outs is None:
         outs = [_empty((n, c.shape[1]), dtype, c.device, stream) for c, s in records]
-    words, least = _q8_words(outs, records, dev)
-    for k, (o, (c, s)) in enumerate(zip(outs, records)):
-        if o.shape[0] != n or c.shape[0] != held:
-            raise ValueError("record %d: %d rows of %d where the call has %d of %d" % (k, o.shape[0], c.shape[0], n, held))
-    _check(L.alch_record_expand(n, _ptr(rows), held, len(records), words.buffer_info()[0], handle))
+    entries, least = _q8_entries(outs, records, n, dev, "outs")
+    if least != held or any(c.shape[0] != held for c, s in records):
+        raise ValueError("records of different numbers of rows")
+    _check(L.alch_record_expand(n, _ptr(rows), held, len(records), entries, handle))
     return outs
 
 

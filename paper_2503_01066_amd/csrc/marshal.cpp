@@ -6,6 +6,9 @@
 //
 // alch_embed_forward: the rows of one token are 1.7 us on the GPU and a launch of 3 to 4 from the host; marshalled in Python the call took
 // 6.0 with X given and 7.1 without, with this 4.2 and 5.0.
+//
+// Records in 8 bits: the entries of their calls, from 18 tensors for six streams.
+#define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -102,7 +105,41 @@ PyObject* embed_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"embed_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(embed_forward)), METH_FASTCALL, nullptr},
+// (tensors, pairs of codes and scales, rows of each tensor, device) -> (the entries of alch_capture_pack_q8 or alch_record_expand, rows of the codes), or
+// None as above, where the pairs have different numbers of rows, too.
+PyObject* q8_entries(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 4, "q8_entries takes four arguments");
+    const auto list = [](PyObject* o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); };
+    if (!list(a[0]) || !list(a[1])) Py_RETURN_NONE;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
+    const long long rows = PyLong_AsLongLong(a[2]), device = PyLong_AsLongLong(a[3]);
+    if (PyErr_Occurred()) return nullptr;
+    if (count == 0 || count > kMost || PySequence_Fast_GET_SIZE(a[1]) != count) Py_RETURN_NONE;
+    static_assert(sizeof(alch_q8_stream) == sizeof(alch_q8_tensor), "one layout");
+    alch_q8_tensor of[kMost];
+    int64_t held = -1;
+    for (Py_ssize_t k = 0; k < count; ++k) {
+        PyObject* pair = PySequence_Fast_GET_ITEM(a[1], k);
+        if (!list(pair) || PySequence_Fast_GET_SIZE(pair) != 2) Py_RETURN_NONE;
+        const at::Tensor *t = plain(PySequence_Fast_GET_ITEM(a[0], k)), *c = plain(PySequence_Fast_GET_ITEM(pair, 0)), *s = plain(PySequence_Fast_GET_ITEM(pair, 1));
+        if (!t || !c || !s || t->dim() != 2 || c->dim() != 2 || s->dim() != 2) Py_RETURN_NONE;
+        const int64_t width = c->size(1), groups = (width + ALCH_Q8_GROUP - 1) / ALCH_Q8_GROUP;
+        const auto type = t->scalar_type();
+        if (held < 0) held = c->size(0);
+        if (t->size(0) != rows || t->size(1) != width || (width > 1 && t->stride(1) != 1) || (type != at::kBFloat16 && type != at::kFloat) ||
+            t->get_device() != device || c->get_device() != device || s->get_device() != device || c->size(0) != held || c->scalar_type() != at::kChar ||
+            !c->is_contiguous() || s->size(0) != held || s->size(1) != groups || s->scalar_type() != at::kFloat || !s->is_contiguous())
+            Py_RETURN_NONE;
+        of[k] = alch_q8_tensor{t->data_ptr(), static_cast<const int8_t*>(c->data_ptr()), static_cast<const float*>(s->data_ptr()), width,
+                               (size_t)(rows > 1 ? t->stride(0) : width) * t->element_size(), type == at::kFloat ? ALCH_F32 : ALCH_BF16, 0};
+    }
+    return Py_BuildValue("(y#L)", reinterpret_cast<const char*>(of), (Py_ssize_t)(count * sizeof(of[0])), (long long)held);
+    END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"q8_entries", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(q8_entries)), METH_FASTCALL, nullptr},
+                         {"embed_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(embed_forward)), METH_FASTCALL, nullptr},
                          {"capture_pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(capture_pack)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -9,11 +9,13 @@
 //
 // Both directions are bound by memory: a kept element is 2 bytes read and 1 1/16 written, and the reverse.
 #include "kernels.h"
+#include "mask_scan.h"
 
 namespace alch {
 
 static constexpr int kGroup = ALCH_Q8_GROUP, kThreads = 256;
 static constexpr int kMaxPerLaunch = 16;        // streams of a launch
+static constexpr int kSmallRows = 256;          // up to so many rows the streams of a row have a work-group each
 static constexpr int kGridMax = 1 << 20;        // work-groups of a launch; rows behind them are gone over in rounds
 static constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: below it 127 / a would leave fp32
 
@@ -84,26 +86,39 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 }
 
 // ---- a row, by a work-group --------------------------------------------------------------------
-// Eight elements a lane, so that a group is eight lanes and its maximum three steps of neighbours.
+// Eight elements a lane, so that a group is eight lanes and its maximum three steps of neighbours; kBatch pieces a thread are on their way at
+// once (a row of 14336 elements: two rounds).
+static constexpr int kBatch = 4;
 template <typename T>
 __device__ __forceinline__ void quantise_row_pieces(const T* __restrict__ src, int8_t* __restrict__ codes, float* __restrict__ scales, long long width) {
     const long long pieces = width >> 3;
-    for (long long base = 0; base < pieces; base += kThreads) {
-        const long long p = base + threadIdx.x;
-        float x[8] = {};
-        if (p < pieces) load8(src + p * 8, x);
-        uint32_t most = 0;
+    for (long long base = 0; base < pieces; base += kThreads * kBatch) {
+        float x[kBatch][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = max(most, magnitude(x[e]));
-        const GroupScale s = group_scale(max_of_8(most));
-        uint32_t c[8];
+        for (int b = 0; b < kBatch; ++b) {
+            const long long p = base + b * kThreads + threadIdx.x;
+            if (p < pieces) load8(src + p * 8, x[b]);
+            else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = code_of(x[e], s.r);
-        u32x2_q w = {bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7])};
-        if (!s.fine) w = u32x2_q{0, 0};
-        if (p < pieces) {
-            __builtin_nontemporal_store(w, reinterpret_cast<u32x2_q*>(codes + p * 8));
-            if ((threadIdx.x & 7) == 0) scales[p >> 3] = s.scale;
+                for (int e = 0; e < 8; ++e) x[b][e] = 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (base + b * kThreads >= pieces) break;
+            const long long p = base + b * kThreads + threadIdx.x;
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, magnitude(x[b][e]));
+            const GroupScale s = group_scale(max_of_8(most));
+            uint32_t c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = code_of(x[b][e], s.r);
+            u32x2_q w = {bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7])};
+            if (!s.fine) w = u32x2_q{0, 0};
+            if (p < pieces) {
+                __builtin_nontemporal_store(w, reinterpret_cast<u32x2_q*>(codes + p * 8));
+                if ((threadIdx.x & 7) == 0) scales[p >> 3] = s.scale;
+            }
         }
     }
 }
@@ -124,15 +139,27 @@ __device__ __forceinline__ void quantise_row_elements(const T* __restrict__ src,
 template <typename T>
 __device__ __forceinline__ void expand_row_pieces(const int8_t* __restrict__ codes, const float* __restrict__ scales, T* __restrict__ dst, long long width) {
     const long long pieces = width >> 3;
-    for (long long p = threadIdx.x; p < pieces; p += kThreads) {
-        float x[8] = {};
-        if (codes) {
-            const u32x2_q c = __builtin_nontemporal_load(reinterpret_cast<const u32x2_q*>(codes + p * 8));
-            const float s = scales[p >> 3];
+    for (long long base = 0; base < pieces; base += kThreads * kBatch) {
+        u32x2_q c[kBatch];
+        float s[kBatch];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)(c[e >> 2] >> (8 * (e & 3))) * s;
+        for (int b = 0; b < kBatch; ++b) {
+            const long long p = base + b * kThreads + threadIdx.x;
+            c[b] = u32x2_q{0, 0};
+            s[b] = 0.f;
+            if (codes && p < pieces) {
+                c[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x2_q*>(codes + p * 8));
+                s[b] = scales[p >> 3];
+            }
         }
-        store8(dst + p * 8, x);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const long long p = base + b * kThreads + threadIdx.x;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)(c[b][e >> 2] >> (8 * (e & 3))) * s[b];
+            if (p < pieces) store8(dst + p * 8, x);
+        }
     }
 }
 template <typename T>
@@ -188,6 +215,54 @@ __global__ __launch_bounds__(kThreads) void k_gather_q8(Q8Args a, const int* __r
     }
 }
 
+// Scan and rows of a batch of at most 4096 * kLoads tokens in one launch: every work-group finds its row's token in the mask by itself, the first
+// one writes the counts; blockIdx.y deals out the streams of a row.
+template <int kLoads>
+__global__ __launch_bounds__(kScanThreads) void k_pack_small_q8(Q8Args a, const uint8_t* __restrict__ mask, int T, const int* __restrict__ cu_seqlens,
+                                                                int n_bounds, int* __restrict__ kept_index, int* __restrict__ cu_kept,
+                                                                int* __restrict__ n_kept_and_status, long long capacity) {
+    __shared__ int token;
+    __shared__ int prefix[kLoads * kScanThreads];
+    __shared__ unsigned short kept_bits[kLoads * kScanThreads];
+    const int tid = threadIdx.x, r = blockIdx.x;
+    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    uint32_t bits[kLoads];
+    int count[kLoads], carry = 0;
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) count[l] = nonzero_bytes16(mask, (l * kScanThreads + tid) * kTokPerThread, T, bits[l]);
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+        int total;
+        const int ex = carry + block_exclusive_scan(count[l], total);
+        if (first) {
+            prefix[l * kScanThreads + tid] = ex;
+            kept_bits[l * kScanThreads + tid] = (unsigned short)bits[l];
+        }
+        if (r >= ex && r < ex + count[l]) {
+            uint32_t left = bits[l];
+            for (int i = ex; i < r; ++i) left &= left - 1;
+            token = (l * kScanThreads + tid) * kTokPerThread + __ffs(left) - 1;
+            if (blockIdx.y == 0 && r < capacity) kept_index[r] = token;
+        }
+        carry += total;
+    }
+    __syncthreads();
+    if (first) {
+        if (tid == 0) {
+            n_kept_and_status[0] = carry;
+            n_kept_and_status[1] = (long long)carry > capacity ? 1 : 0;
+        }
+        for (int s = tid; s < n_bounds; s += kScanThreads) {
+            const int end = cu_seqlens[s], owner = end / kTokPerThread;
+            int n = carry;
+            if (owner < kLoads * kScanThreads) n = prefix[owner] + __popc(kept_bits[owner] & ((1u << (end % kTokPerThread)) - 1u));
+            cu_kept[s] = n;
+        }
+    }
+    if (r >= carry || r >= capacity) return;
+    for (int k = blockIdx.y; k < a.n; k += gridDim.y) quantise_row(a.s[k], token, r);
+}
+
 __global__ __launch_bounds__(kThreads) void k_expand(Q8Args a, const int* __restrict__ rows, long long n_rows, long long n_src_rows) {
     for (long long r = blockIdx.x; r < n_rows; r += gridDim.x) {
         long long from = rows ? rows[r] : r;
@@ -211,16 +286,20 @@ static Q8Args q8_args(int n, const alch_q8_stream* streams, int base) {
     return a;
 }
 
+static double row_bytes(int n_streams, const alch_q8_stream* streams) {  // of a kept row: their number is on the device
+    double bytes = 0;
+    for (int k = 0; k < n_streams; ++k) bytes += (double)streams[k].width * (dtype_size((alch_dtype)streams[k].dtype) + 1 + 4.0 / kGroup);
+    return bytes;
+}
+
 int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long long capacity, const int* kept_index, const int* n_kept_and_status,
                      hipStream_t stream) {
     const long long max_rows = T < capacity ? T : capacity;
     if (max_rows == 0 || n_streams == 0) return ALCH_OK;
-    double bytes = 0;  // of a kept row: their number is on the device
-    for (int k = 0; k < n_streams; ++k) bytes += (double)streams[k].width * (dtype_size((alch_dtype)streams[k].dtype) + 1 + 4.0 / kGroup);
-    TraceScope ts(kTracePackGather, 0.0, bytes, stream);
+    TraceScope ts(kTracePackGather, 0.0, row_bytes(n_streams, streams), stream);
     for (int base = 0; base < n_streams; base += kMaxPerLaunch) {
         const Q8Args a = q8_args(n_streams, streams, base);
-        const dim3 grid((unsigned)(max_rows < kGridMax ? max_rows : kGridMax), max_rows <= 256 ? a.n : 1);
+        const dim3 grid((unsigned)(max_rows < kGridMax ? max_rows : kGridMax), max_rows <= kSmallRows ? a.n : 1);
         k_gather_q8<<<grid, kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows);
     }
     ALCH_HIP_TRY(hipGetLastError());
@@ -229,6 +308,16 @@ int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long l
 
 int launch_pack_q8(const uint8_t* mask, int T, const int* cu_seqlens, int n_seqs, int n_streams, const alch_q8_stream* streams, long long capacity,
                    int* kept_index, int* cu_kept, int* n_kept_and_status, void* workspace, hipStream_t stream) {
+    const long long max_rows = T < capacity ? T : capacity;
+    if (T <= 2 * kTokPerBlock && max_rows > 0 && n_streams > 0 && n_streams <= kMaxPerLaunch) {
+        TraceScope ts(kTracePackGather, 0.0, row_bytes(n_streams, streams), stream);
+        const Q8Args a = q8_args(n_streams, streams, 0);
+        const dim3 grid((unsigned)max_rows, max_rows <= kSmallRows ? n_streams : 1);
+        const auto kernel = T <= kTokPerBlock ? k_pack_small_q8<1> : k_pack_small_q8<2>;
+        kernel<<<grid, kScanThreads, 0, stream>>>(a, mask, T, cu_seqlens, n_seqs + 1, kept_index, cu_kept, n_kept_and_status, capacity);
+        ALCH_HIP_TRY(hipGetLastError());
+        return ALCH_OK;
+    }
     ALCH_TRY(launch_pack(mask, T, cu_seqlens, n_seqs, 0, nullptr, capacity, kept_index, cu_kept, n_kept_and_status, workspace, stream));
     return launch_gather_q8(T, n_streams, streams, capacity, kept_index, n_kept_and_status, stream);
 }
@@ -246,7 +335,7 @@ int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n
             a.s[k] = {static_cast<char*>(t.dst), const_cast<int8_t*>(t.codes), const_cast<float*>(t.scales), t.width, (long long)t.dst_row_stride_bytes,
                       t.dtype == ALCH_BF16, made_of_pieces(t.dst, t.codes, t.width, t.dst_row_stride_bytes)};
         }
-        const dim3 grid((unsigned)(n_rows < kGridMax ? n_rows : kGridMax), n_rows <= 256 ? a.n : 1);
+        const dim3 grid((unsigned)(n_rows < kGridMax ? n_rows : kGridMax), n_rows <= kSmallRows ? a.n : 1);
         k_expand<<<grid, kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
     }
     ALCH_HIP_TRY(hipGetLastError());

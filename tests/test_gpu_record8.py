@@ -79,7 +79,7 @@ def test_pack_widths(dtype, width):
     check(A, mask, streams)
 
 
-@pytest.mark.parametrize("T,keep", [(1, 1.0), (1, 0.0), (16, 0.0), (300, 1.0), (4095, 0.5), (4096, 0.02), (4097, 0.3), (9000, 0.9), (270001, 0.01)])
+@pytest.mark.parametrize("T,keep", [(1, 1.0), (1, 0.0), (16, 0.0), (300, 1.0), (4095, 0.5), (4096, 0.02), (4097, 0.3), (8192, 0.02), (8192, 1.0), (8193, 0.1), (9000, 0.9), (270001, 0.01)])
 def test_pack_lengths_and_masks(T, keep):
     import paper_2503_01066_amd as A
     r = np.random.default_rng(T)
@@ -200,6 +200,44 @@ def test_first_rows_and_refusals():
             call()
     with pytest.raises(TypeError):
         A.alch_capture_gather_q8(b, [x.half()])
+
+
+@pytest.mark.parametrize("form", ["lists", "tuples", "slices", "many", "columns apart", "host", "half", "rows", "codes", "scales", "no pair", "unequal", "none"])
+def test_entries_by_the_extension_and_in_python(monkeypatch, form):
+    """The same results, and the same errors for what either refuses."""
+    import paper_2503_01066_amd as A
+    from paper_2503_01066_amd import binding
+    assert binding._marshal is not None
+    T = 40
+    wide = values(T, 400, "bf16", 5)
+    streams = [wide[:, :64], wide[:, 64:163], wide[:, 168:].float()]
+    dsts = [[torch.zeros((T, s.shape[1]), dtype=torch.int8, device="cuda"), torch.zeros((T, -(-s.shape[1] // 64)), device="cuda")] for s in streams]
+    if form == "tuples": streams, dsts = tuple(streams), tuple(tuple(d) for d in dsts)
+    if form == "many": streams, dsts = streams * 30, [[c.clone(), s.clone()] for c, s in dsts * 30]
+    if form == "columns apart": streams[1] = wide[:, 1:199:2]
+    if form == "host": streams[2] = streams[2].cpu()
+    if form == "half": streams[0] = streams[0].half()
+    if form == "rows": streams[1] = streams[1][:39]
+    if form == "codes": dsts[1][0] = dsts[1][0].int()
+    if form == "scales": dsts[1][1] = dsts[1][1][:, :1]
+    if form == "no pair": dsts = dsts[:2]
+    if form == "unequal": dsts[0] = [t[:30] for t in dsts[0]]
+    if form == "none": streams, dsts = [], []
+    mask = (torch.arange(T, device="cuda") % 3 == 0).to(torch.uint8)
+    out = []
+    for ext in (binding._marshal, None):
+        monkeypatch.setattr(binding, "_marshal", ext)
+        for pair in dsts:
+            for t in pair:
+                t.zero_()
+        try:
+            index, cu, status, d = A.alch_capture_pack_q8(A.Batch(np.array([0, 13, T], np.int32)), mask, streams, dsts=dsts)
+            back = A.alch_record_expand(d) if form != "unequal" else []
+            out.append([t.tolist() for t in (index[:14], cu, status)] + [t.nan_to_num().tolist() for p in d for t in p] + [t.float().nan_to_num().tolist() for t in back])
+        except Exception as e:  # noqa: BLE001 (compared below)
+            out.append((type(e), str(e)))
+    assert out[0] == out[1]
+    assert isinstance(out[0], tuple) == (form in ("columns apart", "host", "half", "rows", "codes", "scales", "no pair"))
 
 
 def test_calls_on_another_stream_and_captured():
