@@ -7,6 +7,7 @@ library has not been built, loading raises.
 import ctypes as C
 import itertools
 import os
+import struct
 from array import array
 
 import numpy as np
@@ -239,12 +240,12 @@ def lib():
     L.alch_record_expand.restype = C.c_int
     L.alch_record_expand.argtypes = [C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
     L.alch_policy_loss.restype = C.c_int
-    L.alch_policy_loss.argtypes = [C.c_int, C.c_int32, C.c_void_p, C.c_int64, C.POINTER(CPolicy), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+    L.alch_policy_loss.argtypes = [C.c_int, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                    C.c_size_t, C.c_void_p]
     L.alch_policy_loss_workspace_bytes.restype = C.c_size_t
     L.alch_policy_loss_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
     L.alch_stack_backward_policy.restype = C.c_int
-    L.alch_stack_backward_policy.argtypes = [C.POINTER(CPolicy) if t is C.POINTER(CDpo) else t for t in L.alch_stack_backward_dpo.argtypes]
+    L.alch_stack_backward_policy.argtypes = [C.c_void_p if t is C.POINTER(CDpo) else t for t in L.alch_stack_backward_dpo.argtypes]
     L.alch_adamw8_step.restype = C.c_int
     L.alch_adamw8_step.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(CAdamw), C.c_uint32, C.c_void_p]
     L.alch_trace_enable.argtypes = [C.c_int32]
@@ -795,8 +796,12 @@ class PolicyItems:
             if self.rows_host.shape != (n,):
                 raise ValueError("rows: %s for %d items" % (self.rows_host.shape, n))
             self.rows = torch.from_numpy(self.rows_host.copy()).to(label.device)
-        self.words = (label.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), _ptr(ref_logp), _ptr(self.rows),
-                      None if rows is None else self.rows_host.ctypes.data)
+        self.words = struct.pack("=7Q", label.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), _ptr(ref_logp) or 0,
+                                 _ptr(self.rows) or 0, 0 if rows is None else self.rows_host.ctypes.data)
+
+    def policy(self, clip_low, clip_high, kl_coef, logp):
+        """The alch_policy of a call (2 us less than the structure filled member by member)."""
+        return struct.pack("=i3f", self.n_items, clip_low, clip_high, kl_coef) + self.words + struct.pack("=Q", logp.data_ptr())
 
 
 def policy_loss_workspace_bytes(n_items, vocab):
@@ -818,7 +823,7 @@ def alch_policy_loss(logits, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0, wa
     if dlogits is None and want_grad:
         dlogits = _empty((n, vocab), dt, logits.device, stream)
     for name, t in (("logits", logits), ("dlogits", dlogits)):
-        if t is not None and (t.dtype is not dt or t.shape != logits.shape or t.get_device() != dev or (t.stride(1) != 1 and vocab > 1) or t.stride(0) < 0):
+        if t is not None and (t.dtype is not dt or t.shape != logits.shape or t.get_device() != dev or (t.stride(1) != 1 and vocab > 1)):
             raise ValueError("%s: rows of %d elements of %s one after another are needed, got %s %s with strides %s on %s" % (
                 name, vocab, dt, tuple(t.shape), t.dtype, t.stride(), t.device))
     if logp is None:
@@ -833,10 +838,12 @@ def alch_policy_loss(logits, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0, wa
         workspace = _empty((L.alch_policy_loss_workspace_bytes(n, vocab) or 256,), torch.uint8, logits.device, stream)
     else:
         _check_dense(workspace, "workspace", torch.uint8, dev)
-    p = CPolicy(n, clip_low, clip_high, kl_coef, *items.words, logp.data_ptr())
-    pitch = lambda t: t.stride(0) if n > 1 else vocab
-    rc = L.alch_policy_loss(_code(dt), vocab, logits.data_ptr(), pitch(logits), C.byref(p), _ptr(dlogits), 0 if dlogits is None else pitch(dlogits),
-                            loss.data_ptr(), workspace.data_ptr(), workspace.numel(), handle)
+    if dlogits is None:
+        grad, pitch = None, 0
+    else:
+        grad, pitch = dlogits.data_ptr(), dlogits.stride(0) if n > 1 else vocab
+    rc = L.alch_policy_loss(_code(dt), vocab, logits.data_ptr(), logits.stride(0) if n > 1 else vocab, items.policy(clip_low, clip_high, kl_coef, logp), grad,
+                            pitch, loss.data_ptr(), workspace.data_ptr(), workspace.numel(), handle)
     if rc != 0:
         _check(rc)
     return loss, logp, dlogits
@@ -872,13 +879,12 @@ def alch_stack_backward_policy(shape, batch, saved_layers, weights_layers, X_fin
     dX_embed = _empty(X_final.shape, X_final.dtype, dev, stream)
     loss, logp = _empty((4,), torch.float32, dev, stream), _empty((items.n_items,), torch.float32, dev, stream)
     ws = workspace if workspace is not None else _empty((max(int(need), 256),), torch.uint8, dev, stream)
-    p = CPolicy(items.n_items, clip_low, clip_high, kl_coef, *items.words, logp.data_ptr())
     hk = None
     if hooks is not None:
         ready, preempt = hooks
         hk = CHooks(HOOK_FN(ready) if ready else HOOK_FN(), HOOK_FN(preempt) if preempt else HOOK_FN(), None)
     _check(L.alch_stack_backward_policy(C.byref(shape), n_layers, vocab, C.byref(batch.c), SA, WA, LA, _ptr(X_final), _ptr(g_final), _ptr(W_lm),
-                                        C.byref(p), GA, LG, _ptr(dg_final), _ptr(dW_lm), _ptr(dX_embed), _ptr(loss),
+                                        items.policy(clip_low, clip_high, kl_coef, logp), GA, LG, _ptr(dg_final), _ptr(dW_lm), _ptr(dX_embed), _ptr(loss),
                                         C.byref(hk) if hk else None, _ptr(ws), ws.numel(), handle))
     layers = [dict(g, **(lora_grads_layers[i] if lora_grads_layers is not None else {})) for i, g in enumerate(grads_layers)]
     return dict(loss=loss, logp=logp, dX_embed=dX_embed, dg_final=dg_final, dW_lm=dW_lm, layers=layers)

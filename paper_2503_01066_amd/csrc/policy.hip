@@ -400,7 +400,7 @@ __device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, in
     *begin = min(j * each, pieces);
     *end = min(*begin + each, pieces);
 }
-// A row of its parts, by all lanes of a wavefront: kMaxParts at most.  base is the largest logit (0: there is none), sum relative to it.
+// A row of its parts, one to a lane of a wavefront (kMaxParts at most).  base is the largest logit (0: there is none), sum relative to it.
 struct Whole {
     float base, sum;
 };
@@ -412,9 +412,7 @@ __device__ __forceinline__ double wave_sum(double v) {
 __device__ __forceinline__ double part_in(const Partial& p, float base) {  // (a part of NaN alone has no largest one either)
     return p.most == -INFINITY ? (double)p.sum : (double)p.sum * exp2(((double)p.most - (double)base) * kLog2eDouble);
 }
-__device__ __forceinline__ Whole whole_row(const Partial* __restrict__ partial, int parts) {
-    const int lane = threadIdx.x & 63;
-    const Partial p = lane < parts ? partial[lane] : Partial{-INFINITY, 0.f};
+__device__ __forceinline__ Whole whole_row(const Partial& p) {
     const float most = wave_max(p.most), base = most == -INFINITY ? 0.f : most;
     return {base, (float)wave_sum(part_in(p, base))};
 }
@@ -497,6 +495,44 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
     }
 }
 
+// The parts of few rows: kHeld pieces a thread, which are on their way before the item has been looked at.  (Latency is all there is here: 17 rows in
+// 544 parts of 8 KB, both launches 14.1 us with the kernel above and the item first.)
+template <typename T, int kHeld>
+__global__ __launch_bounds__(kPartThreads) void k_policy_few(const T* logits, long long ld, int vocab, PolicyArgs a, int parts, Partial* __restrict__ partial) {
+    typedef typename Piece<T>::type V;
+    constexpr int n = Piece<T>::n;
+    __shared__ float red[2][kPartThreads / 64];
+    const int tid = threadIdx.x, m = (int)blockIdx.x / parts, j = (int)blockIdx.x % parts;
+    const T* row = logits + m * ld;
+    const RowCut c = cut_row(row, vocab);
+    int begin, end;
+    part_of(c.pieces, j, parts, &begin, &end);
+    const T* body = row + c.head;
+    V x[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (begin + tid + k * kPartThreads < end) x[k] = load_piece<V>(body + (long long)(begin + tid + k * kPartThreads) * n);
+    const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m];
+    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, weight = a.weight[m];
+    if ((unsigned)label >= (unsigned)vocab || weight == 0.f) return;
+    const float xl = j == 0 && tid == 0 ? (float)row[label] : 0.f;
+    float most = xe;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (begin + tid + k * kPartThreads < end) most = piece_max<T>(x[k], most);
+    most = group_max<kPartThreads>(most, red[0]);
+    const float base = most == -INFINITY ? 0.f : most;
+    float s[4] = {extra >= 0 ? grown(xe, base) : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (begin + tid + k * kPartThreads < end) piece_sum<T>(x[k], base, s);
+    const float sum = group_sum<kPartThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+    if (tid == 0) {
+        partial[blockIdx.x] = {most, sum};
+        if (j == 0) a.own[m] = xl;
+    }
+}
+
 // ---- the loss ----------------------------------------------------------------------------------
 // Its four sums, in a fixed order and in 64 bits, by one work-group.
 static constexpr int kSumThreads = 1024, kSumGroups = 256;
@@ -567,19 +603,30 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
                                                  float* __restrict__ logp_out) {
     __shared__ double joined[kMaxPartials / 2];
     __shared__ float largest[kMaxPartials / 2];
-    const int lanes = parts <= 1 ? 1 : 1 << (32 - __builtin_clz(parts - 1)), tid = threadIdx.x, j = tid & (lanes - 1);
-    for (int first = 0; first < n; first += kThreads / lanes) {
-        const int m = first + tid / lanes;
-        const bool counted = m < n && scores(a, m, vocab);
-        const Partial p = counted && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.f};
-        float most = p.most;
-        for (int d = lanes >> 1; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-        const float base = most == -INFINITY ? 0.f : most;
-        double sum = part_in(p, base);
-        for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        if (m < n && j == 0) {
-            joined[m] = counted ? sum : -1.0;
-            largest[m] = base;
+    const int lanes = parts <= 1 ? 1 : 1 << (32 - __builtin_clz(parts - 1)), tid = threadIdx.x, j = tid & (lanes - 1), rows = kThreads / lanes;
+    constexpr int kAhead = 4;
+    for (int first = 0; first < n; first += rows * kAhead) {
+        Partial p[kAhead];
+        bool counted[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int m = first + k * rows + tid / lanes;
+            p[k] = m < n && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.f};  // (of rows that do not score: whatever was there)
+            counted[k] = m < n && scores(a, m, vocab);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int m = first + k * rows + tid / lanes;
+            if (first + k * rows >= n) break;
+            float most = p[k].most;
+            for (int d = lanes >> 1; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+            const float base = most == -INFINITY ? 0.f : most;
+            double sum = part_in(p[k], base);
+            for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+            if (m < n && j == 0) {
+                joined[m] = counted[k] ? sum : -1.0;
+                largest[m] = base;
+            }
         }
     }
     __syncthreads();
@@ -612,7 +659,7 @@ __global__ __launch_bounds__(64) void k_policy_sums_join(const double (*__restri
     if (threadIdx.x < 4) loss_out[i] = (float)t;
 }
 static void launch_sums(const PolicyArgs& a, int n, void* scratch, float* logp_out, float* loss_out, hipStream_t stream) {
-    if (n <= 2 * kSumThreads) {  // (1501 items: 5.5 us, 10 by two launches)
+    if (n <= 3 * kSumThreads) {  // (1501 items: 5.5 us, 10 by two launches)
         k_policy_sums<<<1, kSumThreads, 0, stream>>>(a, n, 0, 0, nullptr, logp_out, loss_out);
         return;
     }
@@ -622,13 +669,14 @@ static void launch_sums(const PolicyArgs& a, int n, void* scratch, float* logp_o
     k_policy_sums_join<<<1, 64, 0, stream>>>(sums, groups, loss_out);
 }
 
-// The gradient of rows that were summed in parts, a work-group a part, and by the first work-group the loss.
+// The gradient of rows that were summed in parts, a work-group a part, and by the first work-group the loss.  What a part begins with is on its way
+// before the row's sum is known.
 template <typename T>
 __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* logits, long long ld, int vocab, PolicyArgs a, int rows, int parts,
                                                                     const Partial* __restrict__ partial, T* dlogits, long long ld_grad,
                                                                     float* __restrict__ logp_out, float* __restrict__ loss_out) {
     typedef typename Piece<T>::type V;
-    constexpr int n = Piece<T>::n;
+    constexpr int n = Piece<T>::n, kHeld = 2;
     __shared__ double red[kPartThreads / 64][4];
     const int tid = threadIdx.x, b = (int)blockIdx.x - 1;
     if (b < 0) {
@@ -641,27 +689,39 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     const RowCut c = cut_row(row, vocab);
     int begin, end;
     part_of(c.pieces, j, parts, &begin, &end);
-    const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m];
+    const T* body = row + c.head;
+    V x[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (begin + tid + k * kPartThreads < end) x[k] = load_piece<V>(body + (long long)(begin + tid + k * kPartThreads) * n);
+    const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m], lane = tid & 63;
+    const float xe = extra >= 0 ? (float)row[extra] : 0.f, weight = a.weight[m], advantage = a.advantage[m], old_logp = a.old_logp[m];
+    const float ref_logp = a.ref_logp ? a.ref_logp[m] : 0.f, own = a.own[m];  // (own, and the parts below: of a row that does not score anything)
+    const Partial part = lane < parts ? partial[(long long)m * parts + lane] : Partial{-INFINITY, 0.f};
     float base = 0.f, scale = 0.f, at_label = 0.f;
     bool some = false;  // logits that the gradient depends on
-    if (scores(a, m, vocab)) {
-        const Whole w = whole_row(partial + (long long)m * parts, parts);
+    if ((unsigned)label < (unsigned)vocab && weight != 0.f) {
+        const Whole w = whole_row(part);
         some = w.sum != 0.f;
         if (some) {
-            const float logp = a.own[m] - w.base - logf(w.sum), d = slope(a, m, logp);
+            const float logp = own - w.base - logf(w.sum), d = slope(a, weight, advantage, old_logp, ref_logp, logp);
             base = w.base;
             scale = -d / w.sum;
             at_label = d * -expm1f(logp);
         }
     }
     const GradOf grad = grad_of(base, scale);
-#pragma unroll 4
-    for (int p = begin + tid; p < end; p += kPartThreads) {
+    const auto put = [&](int p, const V& v) {
         V g = {};
-        if (some) g = with_label<T>(piece_grad<T>(load_piece<V>(row + c.head + (long long)p * n), grad), label - c.head - p * n, at_label);
+        if (some) g = with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, at_label);
         store_piece(out + c.head + (long long)p * n, g);
-    }
-    if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? at_label : scale * grown((float)row[extra], base));
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (begin + tid + k * kPartThreads < end) put(begin + tid + k * kPartThreads, x[k]);
+#pragma unroll 4
+    for (int p = begin + tid + kHeld * kPartThreads; p < end; p += kPartThreads) put(p, load_piece<V>(body + (long long)p * n));
+    if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? at_label : scale * grown(xe, base));
 }
 
 // Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole, of which 256 and more (128 short ones) fill the card, unless
@@ -705,7 +765,10 @@ static int launch_rows(const T* logits, long long ld, int rows, int vocab, const
     ALCH_TRY(compute_units(&n_cu));
     const int pieces = vocab / Piece<T>::n + 1, parts = loss_out ? parts_of(rows, vocab, sizeof(T)) : 1;
     if (parts > 1 || !dlogits) {
-        k_policy_parts<<<(int)std::min<long long>((long long)rows * parts, kGridMax), kPartThreads, 0, stream>>>(logits, ld, rows, vocab, a, parts, partial);
+        const int held = (pieces + parts * kPartThreads - 1) / (parts * kPartThreads);  // of a part, a thread
+        if (parts > 1 && held <= 2) k_policy_few<T, 2><<<rows * parts, kPartThreads, 0, stream>>>(logits, ld, vocab, a, parts, partial);
+        else if (parts > 1 && held <= 8) k_policy_few<T, 8><<<rows * parts, kPartThreads, 0, stream>>>(logits, ld, vocab, a, parts, partial);
+        else k_policy_parts<<<(int)std::min<long long>((long long)rows * parts, kGridMax), kPartThreads, 0, stream>>>(logits, ld, rows, vocab, a, parts, partial);
         if (dlogits)
             k_policy_part_grads<<<rows * parts + 1, kPartThreads, 0, stream>>>(logits, ld, vocab, a, rows, parts, partial, dlogits, ld_grad, logp_out, loss_out);
         else if (parts > 1)

@@ -210,7 +210,9 @@ def test_items_of_a_policy_loss():
     f = lambda n=4: torch.zeros(n)
     label = torch.zeros(4, dtype=torch.int32)
     it = A.PolicyItems(label, f(), f(), f(), rows=[0, 1, 1, 2])
-    assert it.rows.tolist() == [0, 1, 1, 2] and it.words[4] is None
+    assert it.rows.tolist() == [0, 1, 1, 2] and it.words[32:40] == bytes(8) and len(it.policy(0.2, 0.3, 0.1, f())) == C.sizeof(B.CPolicy)
+    p = B.CPolicy.from_buffer_copy(it.policy(0.25, 0.5, 0.125, label))
+    assert (p.n_items, p.clip_low, p.clip_high, p.kl_coef, p.label, p.ref_logp, p.item_row, p.logp_out) == (4, 0.25, 0.5, 0.125, label.data_ptr(), None, it.rows.data_ptr(), label.data_ptr())
     for bad in (dict(label=label.long()), dict(old=f(3)), dict(weight=f().double()), dict(ref_logp=f(8)[::2]), dict(rows=[0, 1])):
         a = dict(dict(label=label, old=f(), advantage=f(), weight=f(), ref_logp=None, rows=None), **bad)
         with pytest.raises(ValueError):
