@@ -14,6 +14,7 @@
 // The row kernels leave x_label - max and the sum of exponentials of every item; the loss is made of them in 64 bits by one launch, where
 // terms of either sign cancel and a rounding of logp to fp32 would be seen.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -266,6 +267,7 @@ __device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // read
 template <typename T>
 __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, long long ld, int rows, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
     typedef typename Piece<T>::type V;
+    typedef std::conditional_t<sizeof(T) == 2, unsigned short, unsigned int> Bits;
     constexpr int n = Piece<T>::n;
     __shared__ __attribute__((aligned(1024))) V ahead[kStayLds * kStayThreads];
     __shared__ float red[2][kStayThreads / 64];
@@ -276,20 +278,23 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         float weight, advantage, old_logp, ref_logp;
         bool counted;
     };
-    const auto item_of = [&](int r) {
+    const auto item_of = [&](int r) {  // (by scalar loads: a vector load here would be waited for with the stores before it)
         const int m = min(r, rows - 1);
-        Item i{a.label[m], a.weight[m], a.advantage[m], a.old_logp[m], a.ref_logp ? a.ref_logp[m] : 0.f, false};
+        const auto at = [m](const auto* p) { return ((const __attribute__((address_space(4))) std::remove_cv_t<std::remove_pointer_t<decltype(p)>>*)(uintptr_t)p)[m]; };
+        Item i{at(a.label), at(a.weight), at(a.advantage), at(a.old_logp), a.ref_logp ? at(a.ref_logp) : 0.f, false};
         i.counted = r < rows && (unsigned)i.label < (unsigned)vocab && i.weight != 0.f;
         return i;
     };
     V next[kStayRegs];
-    float xe_next = -INFINITY, xl_next = 0.f;
+    Bits xe_next, xl_next;  // what this thread has beside its pieces, and the label's logit: as loaded, for the row's own turn to look at
     // The loads of a row: a wavefront fetches what its own lanes will use.  kStayPieces of them are issued whether or not the row reaches
     // as far, or is wanted at all.
     const auto fetch = [&](int r, const Item& i) {
         const T* row = logits + (long long)min(r, rows - 1) * ld;
         const RowCut c = cut_row(row, vocab);
-        const int bytes = i.counted ? c.pieces * 16 : 0, extra = extra_of<T>(c, vocab);
+        const int bytes = i.counted ? c.pieces * 16 : 0;
+        xe_next = reinterpret_cast<const Bits*>(row)[max(extra_of<T>(c, vocab), 0)];
+        xl_next = reinterpret_cast<const Bits*>(row)[i.counted ? i.label : 0];
         const i32x4_p src = resource(row + c.head, bytes);
         uint32_t at = (uint32_t)tid * 16u;
         asm volatile("" : "+v"(at));  // (one register, not one per piece kept across the loop)
@@ -302,8 +307,6 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         for (int k = 0; k < kStayRegs; ++k)
             next[k] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row) + c.head, 0, bytes, 0x00020000),
                                                                                   at + (kStayLds + k) * kStayThreads * 16, 0, 0));
-        xe_next = i.counted && extra >= 0 ? (float)row[extra] : -INFINITY;
-        xl_next = i.counted ? (float)row[i.label] : 0.f;
     };
     Item item = item_of(blockIdx.x), item1 = item_of(blockIdx.x + step);
     fetch(blockIdx.x, item);
@@ -333,7 +336,8 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         for (int k = 0; k < kStayLds; ++k) x[k] = ahead[k * kStayThreads + tid];
 #pragma unroll
         for (int k = 0; k < kStayRegs; ++k) x[kStayLds + k] = next[k];
-        const float xe = xe_next, xl = xl_next;
+        asm volatile("" : "+v"(xe_next), "+v"(xl_next));
+        const float xe = extra >= 0 ? (float)__builtin_bit_cast(T, xe_next) : -INFINITY, xl = (float)__builtin_bit_cast(T, xl_next);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) asm volatile("" : "+v"(x[k]));  // (in registers before the next row overwrites them)
