@@ -7,7 +7,8 @@
 // are defined bit for bit.  int8 with the group's own scale: an activation of normal distribution comes back to 0.5 % in the 2-norm,
 // 8-bit floats with 3 bits of mantissa leave 2.6 %.
 //
-// Both directions are bound by memory: a kept element is 2 bytes read and 1 1/16 written, and the reverse.
+// Both directions are bound by memory: a kept element is 2 bytes read and 1 1/16 written, and the reverse.  A quarter of 70001 tokens of 38912 bf16
+// elements: 358 us, 5.8 TB/s; 8192 rows of them back: 175 us, 5.6 TB/s.
 #include <algorithm>
 
 #include "kernels.h"
@@ -360,7 +361,7 @@ static double row_bytes(int n_streams, const alch_q8_stream* streams) {  // of a
     return bytes;
 }
 
-// Whether a wavefront is enough for a row: up to so many elements.  487 + 163 fp32 elements, 2501 rows of 5003 tokens: 12.0 us with a work-group a row.
+// Whether a wavefront is enough for a row: up to so many elements.  487 + 163 fp32 elements, 2501 rows of 5003 tokens: 8.5 us, 12.0 with a work-group a row.
 static constexpr int kShortRow = 1024;
 static bool short_rows(const Q8Args& a) {
     bool all = true;
