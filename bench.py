@@ -42,6 +42,8 @@ def parse():
                     help="config2/config5: no base weight gradients (the frozen base of parameter-efficient fine-tuning)")
     ap.add_argument("--offload", action="store_true",
                     help="config4: records live in pinned host memory and are prefetched layer by layer during the walk")
+    ap.add_argument("--record-bits", type=int, default=16, choices=[16, 8],
+                    help="with --offload: 8 keeps the records as int8 codes with a scale for every 64 elements (O and LSE are recomputed)")
     ap.add_argument("--six-stream", action="store_true",
                     help="pack / keep only X, Q, K, V, G, U; the backward recomputes O, LSE and X2")
     ap.add_argument("--four-stream", action="store_true",
@@ -58,7 +60,10 @@ def parse():
                     help="config2: leave out the `also` object (configs 3, 4 and 5 measured in the same run)")
     ap.add_argument("--traffic-json", default=os.path.join(ROOT, "profiles", "traffic.json"),
                     help="measured HBM bytes per launch (from the rocprofv3 --pmc summaries)")
-    return ap.parse_args()
+    args = ap.parse_args()
+    if args.record_bits == 8 and not args.offload:
+        ap.error("--record-bits goes with --offload")
+    return args
 
 
 def cpu_baseline_layer(workload, seed=0, full=False):
@@ -472,7 +477,7 @@ def run_config4(args, torch, A):
         mode += ", loss on a Bernoulli(0.25) subset of the tokens (head and top layer run on the counted rows)"
     if args.offload:
         # Section 4.3: the records wait in pinned host memory; the walk prefetches them one layer ahead
-        store = A.RecordStore(L, recs[0])
+        store = A.RecordStore(L, recs[0], bits=args.record_bits)
         for l in range(L):
             store.offload(l, recs[l])
         torch.cuda.synchronize()
@@ -482,7 +487,7 @@ def run_config4(args, torch, A):
                              args.steps, args.warmup)
         offload = {"record_bytes_per_layer": store.bytes_per_layer,
                    "host_to_device_gbps": store.bytes_per_layer * L / t_reuse / 1e9}
-        mode += ", records prefetched from pinned host memory"
+        mode += ", records prefetched from pinned host memory" + (" in 8 bits" if args.record_bits == 8 else "")
     A.alch_trace_enable(True)
     if not args.offload:
         t_reuse, out = timed(lambda: backward(X_final, recs), args.steps, args.warmup)
