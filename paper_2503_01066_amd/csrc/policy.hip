@@ -254,10 +254,10 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
 }
 
 // ---- stay --------------------------------------------------------------------------------------
-// 6001 x 128256 bf16 with gradient: 590 us, 652 by the kernel above.  5.1 TB/s where every row scores; rows that do not, which are written only, fall to
-// the work-groups unevenly (4.9 with a tenth of them).  What the loop must not do is wait for everything between a row's fetch and its stores: a single
-// element converted where it is loaded, or an item by a vector load, costs 3 to 13 % (100352 columns 466 us, 496).
+// 6001 x 128256 bf16 with gradient: 580 us, 652 by the kernel above.  What the loop must not do is wait for everything between a row's fetch and its
+// stores: a single element converted where it is loaded, or an item by a vector load, costs 3 to 13 % (100352 columns 466 us, 496).
 static constexpr int kStayThreads = 1024, kStayPieces = 16, kStayLds = 9, kStayRegs = kStayPieces - kStayLds;
+static constexpr int kStayRows = 1024;  // of a work-group in a launch
 static constexpr int kHeldBytes = kStayThreads * kStayPieces * 16;  // the longest row that a work-group holds
 
 __device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // reads past the bytes are zero, writes dropped
@@ -270,6 +270,58 @@ __device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // read
     return r;
 }
 
+// The rows of work-group b of n: list[0 .. counted) score, list[kStayRows - 1] downwards the others do not.  Either kind is dealt out in turn, from the
+// first work-group and from the last one: a row that scores costs twice as much as one that is only written.  With the rows in turn whatever they are
+// 6001 of them take 601, 572 and 512 us where 0.1, 0.3 and 0.6 do not score, so dealt 592, 521 and 442; where all do, 2 us more.
+struct Dealt {
+    int counted, others;
+};
+__device__ __forceinline__ Dealt deal_rows(const PolicyArgs& a, int rows, int vocab, unsigned b, unsigned n, int* list, int (*counts)[64]) {
+    constexpr int kLoads = 4;  // (a count of each wavefront and load is a lane of the scan)
+    static_assert(kLoads * (kStayThreads / 64) == 64, "");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int before = 0, turn = 0;
+    for (int base = 0; base < rows; base += kLoads * kStayThreads, turn ^= 1) {
+        int label[kLoads];
+        float weight[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int m = min(base + k * kStayThreads + tid, rows - 1);
+            label[k] = a.label[m];
+            weight[k] = a.weight[m];
+        }
+        unsigned long long which[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) which[k] = __ballot(base + k * kStayThreads + tid < rows && (unsigned)label[k] < (unsigned)vocab && weight[k] != 0.f);
+        if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) counts[turn][k * (kStayThreads / 64) + wave] = __popcll(which[k]);
+        }
+        __syncthreads();
+        const int own = counts[turn][lane];
+        int sum = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += o;
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int m = base + k * kStayThreads + tid;
+            const int at = before + __builtin_amdgcn_readlane(sum - own, k * (kStayThreads / 64) + wave) + __popcll(which[k] & ((1ull << lane) - 1));
+            if (which[k] >> lane & 1) {
+                if ((unsigned)at % n == b) list[(unsigned)at / n] = m;
+            } else if (m < rows && (unsigned)(m - at) % n == n - 1 - b) {
+                list[kStayRows - 1 - (unsigned)(m - at) / n] = m;
+            }
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    __syncthreads();
+    const auto share = [n](unsigned all, unsigned first) { return (int)((all + n - 1 - first) / n); };
+    return {share(before, b), share(rows - before, n - 1 - b)};
+}
+
 template <typename T>
 __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, long long ld, int rows, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
     typedef typename Piece<T>::type V;
@@ -277,26 +329,32 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
     constexpr int n = Piece<T>::n;
     __shared__ __attribute__((aligned(1024))) V ahead[kStayLds * kStayThreads];
     __shared__ float red[2][kStayThreads / 64];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), step = (int)gridDim.x;
+    __shared__ int list[kStayRows], counts[2][64];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Dealt mine = deal_rows(a, rows, vocab, blockIdx.x, gridDim.x, list, counts);
+    const int total = mine.counted + mine.others;
+    if (total == 0) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ahead + (uint32_t)wave * 1024u;
     struct Item {  // of the row that is on its way
-        int label;
+        int row, label;
         float weight, advantage, old_logp, ref_logp;
         bool counted;
     };
-    const auto item_of = [&](int r) {  // (by scalar loads: a vector load here would be waited for with the stores before it)
-        const int m = min(r, rows - 1);
+    // A few rows that do not score go first, or the last rows that do would wait for their stores (1000 rows, a tenth: 126 us, last 132); many go last,
+    // where all work-groups only write (6001 rows, six tenths: 442 us, first 475).
+    const int from = 4 * mine.others > total ? mine.counted : 0;
+    const auto item_of = [&](int i) {  // (by scalar loads: a vector load here would be waited for with the stores before it)
+        const bool other = i >= from && i < from + mine.others;
+        const int m = i >= total ? 0 : __builtin_amdgcn_readfirstlane(list[other ? kStayRows - 1 - (i - from) : i < from ? i : i - mine.others]);
         const auto at = [m](const auto* p) { return ((const __attribute__((address_space(4))) std::remove_cv_t<std::remove_pointer_t<decltype(p)>>*)(uintptr_t)p)[m]; };
-        Item i{at(a.label), at(a.weight), at(a.advantage), at(a.old_logp), a.ref_logp ? at(a.ref_logp) : 0.f, false};
-        i.counted = r < rows && (unsigned)i.label < (unsigned)vocab && i.weight != 0.f;
-        return i;
+        return Item{m, at(a.label), at(a.weight), at(a.advantage), at(a.old_logp), a.ref_logp ? at(a.ref_logp) : 0.f, i < total && !other};
     };
     V next[kStayRegs];
     Bits xe_next, xl_next;  // what this thread has beside its pieces, and the label's logit: as loaded, for the row's own turn to look at
     // The loads of a row: a wavefront fetches what its own lanes will use.  kStayPieces of them are issued whether or not the row reaches
     // as far, or is wanted at all.
-    const auto fetch = [&](int r, const Item& i) {
-        const T* row = logits + (long long)min(r, rows - 1) * ld;
+    const auto fetch = [&](const Item& i) {
+        const T* row = logits + (long long)i.row * ld;
         const RowCut c = cut_row(row, vocab);
         const int bytes = i.counted ? c.pieces * 16 : 0;
         xe_next = reinterpret_cast<const Bits*>(row)[max(extra_of<T>(c, vocab), 0)];
@@ -314,19 +372,20 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
             next[k] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row) + c.head, 0, bytes, 0x00020000),
                                                                                   at + (kStayLds + k) * kStayThreads * 16, 0, 0));
     };
-    Item item = item_of(blockIdx.x), item1 = item_of(blockIdx.x + step);
-    fetch(blockIdx.x, item);
+    Item item = item_of(0), item1 = item_of(1);
+    fetch(item);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0), known to the compiler: inside the loop it then counts the stores, too
-    for (int r = blockIdx.x; r < rows; r += step) {
+    for (int i = 0; i < total; ++i) {
         // the row's loads have landed; the last kStayPieces stores of the row before may still be on their way
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStayPieces) : "memory");
-        const Item item2 = item_of(r + 2 * step);
+        const Item item2 = item_of(i + 2);
+        const int r = item.row;
         const RowCut c = cut_row(logits + (long long)r * ld, vocab);
         const int extra = extra_of<T>(c, vocab);
         T* out = dlogits + (long long)r * ld_grad;
         const auto dst = __builtin_amdgcn_make_buffer_rsrc(out + c.head, 0, c.pieces * 16, 0x00020000);
         if (!item.counted) {
-            fetch(r + step, item1);
+            fetch(item1);
             if (tid == 0) a.own[r] = 0.f, a.sum[r] = 0.f;
             if (extra >= 0) out[extra] = (T)0.f;
             int at = tid;
@@ -347,7 +406,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) asm volatile("" : "+v"(x[k]));  // (in registers before the next row overwrites them)
-        fetch(r + step, item1);
+        fetch(item1);
         float most = xe;
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k)
@@ -789,10 +848,14 @@ static int launch_rows(const T* logits, long long ld, int rows, int vocab, const
     }
     // pieces of both matrices' rows begin together, and the row fits
     const bool alike = (ld - ld_grad) * (long long)sizeof(T) % 16 == 0;
-    if (alike && pieces > 512 * 16 && pieces <= kStayThreads * kStayPieces)
-        k_policy_stay<<<std::min(rows, n_cu), kStayThreads, 0, stream>>>(logits, ld, rows, vocab, a, dlogits, ld_grad);
-    else
+    if (alike && pieces > 512 * 16 && pieces <= kStayThreads * kStayPieces) {
+        const int most = (kStayRows - 1) * n_cu;  // (of both kinds together a work-group may have one more than its share)
+        for (long long r = 0; r < rows; r += most)
+            k_policy_stay<<<(int)std::min<long long>(rows - r, n_cu), kStayThreads, 0, stream>>>(logits + r * ld, ld, (int)std::min<long long>(rows - r, most), vocab,
+                                                                                                 a.from((int)r), dlogits + r * ld_grad, ld_grad);
+    } else {
         launch_held<T>(logits, ld, rows, vocab, a, dlogits, ld_grad, stream);
+    }
     if (loss_out) launch_sums(a, rows, partial, logp_out, loss_out, stream);
     return ALCH_OK;
 }

@@ -302,3 +302,45 @@ def test_offsets_beyond_32_bits():
     assert abs(logp[-1].item() - math.log(p)) <= 1e-5 and abs(logp[3].item() + math.log(V)) <= 1e-5
     assert bool((dx[4:-1] == 0).all()) and bool((dx[:3] == 0).all()) and bool((dx[-1] == 0).all())  # (the last item's ratio is clipped)
     assert abs(dx[3, 0].item() * V - 1) <= 2 ** -8 and abs(dx[3, V - 1].item() + 1) <= 2 ** -8
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 65600), ("bf16", 131001), ("f32", 32808)])
+@pytest.mark.parametrize("n", [257, 700, 4500])
+@pytest.mark.parametrize("pattern", ["none", "all", "last", "first half", "every other", "a tenth not"])
+def test_which_rows_of_a_long_vocabulary_score(dtype, V, n, pattern):
+    """Rows are dealt to the work-groups by whether they score, 4096 of them at a time."""
+    import paper_2503_01066_amd as A
+    c = make(n, V, dtype, n)
+    at = torch.arange(n, device="cuda")
+    scores = {"none": at < 0, "all": at >= 0, "last": at == n - 1, "first half": at < n // 2, "every other": at % 2 == 1,
+              "a tenth not": torch.rand(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)) > 0.1}[pattern]
+    c["weight"][~scores & (at % 3 != 0)] = 0
+    c["label"][~scores & (at % 3 == 0)] = -1
+    check(A, c)
+
+
+def test_more_rows_than_the_work_groups_of_a_launch_have_lists_for():
+    """34 GB of logits, in place: 1023 rows a compute unit are a launch.  All logits are 0, so that p = 1 / V, a power of two's neighbour: -d / V."""
+    import paper_2503_01066_amd as A
+    V, n = 65544, 1023 * torch.cuda.get_device_properties(0).multi_processor_count + 300
+    if torch.cuda.mem_get_info()[0] < n * V * 2 + (4 << 30):
+        pytest.skip("needs %d GB of device memory" % (n * V * 2 >> 30))
+    x = torch.zeros(n, V, dtype=torch.bfloat16, device="cuda")
+    at = torch.arange(n, device="cuda")
+    label, weight = (at * 7919 % V).int(), torch.ones(n, device="cuda")
+    weight[at % 5 == 2] = 0
+    old, adv = torch.full((n,), -math.log(V), device="cuda"), 1.0 + at.float() / n
+    loss, logp, dx = A.alch_policy_loss(x, A.PolicyItems(label, old, adv, weight), dlogits=x)
+    counted = weight != 0
+    # ln V = 11.1: its rounding, that of the sum (V / 1024 + 32 additions) and of the logarithm; old's own
+    e = U * (V / 1024 + 36 + 6 * 11.1)
+    assert bool((logp[counted].double() + math.log(V)).abs().max() <= e) and bool((logp[~counted] == 0).all())
+    for b in range(0, n, 8192):
+        got, lab, c = dx[b:b + 8192], label[b:b + 8192].long(), counted[b:b + 8192]
+        d = torch.where(c, -adv[b:b + 8192], torch.zeros(1, device="cuda")).double()
+        assert bool(((got.gather(1, lab[:, None])[:, 0].double() - d * (1 - 1 / V)).abs() <= (2.0 ** -8 + 2 * e) * d.abs()).all())
+        got.scatter_(1, lab[:, None], 0)
+        most, least = got.amax(1).double(), got.masked_fill(torch.zeros_like(got, dtype=torch.bool).scatter_(1, lab[:, None], True), 1.0).amin(1).double()
+        for side in (most, least):
+            assert bool(((side[c] + d[c] / V).abs() <= (2.0 ** -8 + 3 * e) * d[c].abs() / V).all())
+        assert bool((most[~c] == 0).all()) and bool((got[~c].amin(1) == 0).all())
