@@ -6,8 +6,8 @@
 //
 // A row of logits is one softmax, and its gradient needs the row's sum alone: bound by memory, a row read once and written once.
 // Three kernels:
-//   held   a work-group a row, which stays in its registers between the sum and the gradient (up to 256 KB; what a row has beyond them is
-//          read twice);
+//   held   a work-group a row, which stays in its registers between the sum and the gradient (up to 256 KB; rows longer than that also in LDS, up to
+//          400 KB; what they have beyond is read twice);
 //   stay   rows of 128 to 256 KB: a row is half of a compute unit's registers, so that no second work-group fits that could load while
 //          this one computes.  One work-group a unit stays and has the next row on its way, 9 of 16 pieces to LDS, the others to registers;
 //   parts  few rows: several work-groups share one, in two launches with the parts' sums between them.
@@ -183,82 +183,15 @@ template <typename V>
 __device__ __forceinline__ V load_piece(const void* p) {
     return __builtin_bit_cast(V, __builtin_nontemporal_load(static_cast<const u32x4_p*>(p)));
 }
+template <typename V>
+__device__ __forceinline__ V load_again(const void* p) {  // (of what will be read once more: it may stay in the caches)
+    return __builtin_bit_cast(V, *static_cast<const u32x4_p*>(p));
+}
 typedef u32x4_p u32x4_any __attribute__((aligned(2)));  // (rows of the gradient may begin elsewhere than those of the logits)
 template <typename V>
 __device__ __forceinline__ void store_piece(void* p, const V& v) {
     __builtin_nontemporal_store(__builtin_bit_cast(u32x4_p, v), static_cast<u32x4_any*>(p));
 }
-
-// ---- held --------------------------------------------------------------------------------------
-// 6000 x 50257 bf16 with gradient 220 us (5.2 TB/s of logits and gradient: a copy's rate), 9000 x 16000 105 us (5.2).  A row beyond the registers
-// reads its rest twice: 1500 x 150001 bf16 233 us (3.7).  The second bound keeps 32 KB rows at six wavefronts a SIMD: left to itself the compiler
-// takes 182 registers for 2500 x 7001 fp32, two wavefronts, and 53 us in place of 34.
-template <typename T, int kThreads, int kHeld>
-__global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(const T* logits, long long ld, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
-    typedef typename Piece<T>::type V;
-    constexpr int n = Piece<T>::n;
-    __shared__ float red[2][kThreads / 64];
-    const int m = blockIdx.x, tid = threadIdx.x;
-    const T* row = logits + m * ld;
-    T* out = dlogits + m * ld_grad;
-    const RowCut c = cut_row(row, vocab);
-    const int extra = extra_of<T>(c, vocab);
-    const T* body = row + c.head;
-    if (!scores(a, m, vocab)) {
-        if (tid == 0) a.own[m] = 0.f, a.sum[m] = 0.f;
-        const V zero = {};
-        for (int p = tid; p < c.pieces; p += kThreads) store_piece(out + c.head + p * n, zero);
-        if (extra >= 0) out[extra] = (T)0.f;
-        return;
-    }
-    V x[kHeld];
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < c.pieces) x[k] = load_piece<V>(body + (tid + k * kThreads) * n);
-    const int label = a.label[m];
-    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label];
-    float most = xe;
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < c.pieces) most = piece_max<T>(x[k], most);
-    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) most = piece_max<T>(load_piece<V>(body + (long long)p * n), most);
-    most = group_max<kThreads>(most, red[0]);
-    const float base = most == -INFINITY ? 0.f : most;  // (without a finite logit the sum is 0, or NaN)
-    float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
-    // (the empty asm keeps the row packed in registers: without it the compiler carries converted copies across)
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-        asm volatile("" : "+v"(x[k]));
-        if (tid + k * kThreads < c.pieces) piece_sum<T>(x[k], base, s);
-    }
-    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads) piece_sum<T>(load_piece<V>(body + (long long)p * n), base, s);
-    const float sum = group_sum<kThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
-    if (tid == 0) {
-        a.own[m] = sum == 0.f ? -INFINITY : xl - base;
-        a.sum[m] = sum;
-    }
-    const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
-    const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
-    const GradOf grad = grad_of(base, scale);
-    // (each thread writes what it has read: in place nobody reads what another one has written)
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-        asm volatile("" : "+v"(x[k]));
-        const int p = tid + k * kThreads;
-        if (p < c.pieces) store_piece(out + c.head + p * n, with_label<T>(piece_grad<T>(x[k], grad), label - c.head - p * n, at_label));
-    }
-    for (int p = tid + kHeld * kThreads; p < c.pieces; p += kThreads)
-        store_piece(out + c.head + (long long)p * n,
-                    with_label<T>(piece_grad<T>(load_piece<V>(body + (long long)p * n), grad), label - c.head - p * n, at_label));
-    if (extra >= 0) out[extra] = (T)(extra == label ? at_label : scale * grown(xe, base));
-}
-
-// ---- stay --------------------------------------------------------------------------------------
-// 6001 x 128256 bf16 with gradient: 580 us, 652 by the kernel above.  What the loop must not do is wait for everything between a row's fetch and its
-// stores: a single element converted where it is loaded, or an item by a vector load, costs 3 to 13 % (100352 columns 466 us, 496).
-static constexpr int kStayThreads = 1024, kStayPieces = 16, kStayLds = 9, kStayRegs = kStayPieces - kStayLds;
-static constexpr int kStayRows = 1024;  // of a work-group in a launch
-static constexpr int kHeldBytes = kStayThreads * kStayPieces * 16;  // the longest row that a work-group holds
 
 __device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // reads past the bytes are zero, writes dropped
     const uint64_t a = reinterpret_cast<uint64_t>(p);
@@ -269,6 +202,168 @@ __device__ __forceinline__ i32x4_p resource(const void* p, int bytes) {  // read
     r[3] = 0x00020000;
     return r;
 }
+
+// 16 bytes a lane, from `offset` of the resource on, to `lds` and the wavefront's lanes one after another.  (s_nop: such a load takes one wait state after a
+// scalar write of m0)
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const i32x4_p& src) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(src) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+
+// ---- a sum in one pass -------------------------------------------------------------------------
+// With the largest logit so far and the power of two above its exponential, by which the terms are scaled; where a larger one comes the sum is moved by
+// the difference of the powers, exactly.
+// Beyond it a power is no longer exact (masks of the type's lowest value, for one).
+static constexpr float kPowerMost = 1048576.f;
+__device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowerMost ? ceilf(most * kLog2e) : 0.f; }
+// 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
+__device__ __forceinline__ float grown2(float x, float power) {
+    return __builtin_amdgcn_exp2f(fmaf(x, 1.9259629e-8f, fmaf(x, kLog2e, -power)));
+}
+__device__ __forceinline__ float moved(float sum, float from, float to) { return ldexpf(sum, (int)(from - to)); }
+// Adds pieces to the sums s of a thread whose largest logit so far is most, scaled by at.
+template <typename T, typename V, int kBatch>
+__device__ __forceinline__ void add_pieces(V (&x)[kBatch], float& most, float& at, float (&s)[4]) {
+    float higher = most;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) higher = piece_max<T>(x[k], higher);
+    const float to = power(higher);
+    if (to != at && most != -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = moved(s[i], at, to);
+    }
+    most = higher;
+    at = to;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+        asm volatile("" : "+v"(x[k]));
+#pragma unroll
+        for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown2((float)x[k][e], at);
+    }
+}
+// The factor of a sum scaled by the power of two above exp(base), relative to exp(base): where |base| <= kPowerMost.
+__device__ __forceinline__ double from_power(float base) { return exp2((double)power(base) - (double)base * kLog2eDouble); }
+
+// ---- held --------------------------------------------------------------------------------------
+// 6000 x 50257 bf16 with gradient 220 us (5.2 TB/s of logits and gradient: a copy's rate), 9000 x 16000 105 us (5.2).  The second bound keeps 32 KB
+// rows at six wavefronts a SIMD: left to itself the compiler takes 182 registers for 2500 x 7001 fp32, two wavefronts, and 53 us in place of 34.
+// kLds: so many pieces a thread more are in LDS, and what a row has beyond those is read twice, for its sum in one pass; the second time most of it comes
+// from the L2 (3000 x 128256 fp32, a fifth of each row read again: 571 us, 5.1 TB/s; without LDS, and with a pass more for the largest
+// logit, 821).
+template <typename T, int kThreads, int kHeld, int kLds = 0>
+__global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(const T* logits, long long ld, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
+    typedef typename Piece<T>::type V;
+    constexpr int n = Piece<T>::n, kBatch = 2;
+    __shared__ float red[3][kThreads / 64];
+    __shared__ __attribute__((aligned(1024))) V lower[kLds > 0 ? kLds * kThreads : 1];
+    const int m = blockIdx.x, tid = threadIdx.x;
+    const T* row = logits + m * ld;
+    T* out = dlogits + m * ld_grad;
+    const RowCut c = cut_row(row, vocab);
+    const int extra = extra_of<T>(c, vocab);
+    const T* body = row + c.head;
+    if (!scores(a, m, vocab)) {
+        if (tid == 0) a.own[m] = 0.f, a.sum[m] = 0.f;
+        const V zero = {};
+        for (int p = tid; p < c.pieces; p += kThreads) store_piece(out + c.head + (long long)p * n, zero);
+        if (extra >= 0) out[extra] = (T)0.f;
+        return;
+    }
+    V x[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < c.pieces) x[k] = load_piece<V>(body + (tid + k * kThreads) * n);
+    if constexpr (kLds > 0) {  // (each wavefront what its own lanes will use)
+        const i32x4_p src = resource(body, c.pieces * 16);
+        const uint32_t lds = lds_offset(lower) + (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6) * 1024u;
+#pragma unroll
+        for (int k = 0; k < kLds; ++k) load_to_lds(lds + k * kThreads * 16, (uint32_t)(tid + (kHeld + k) * kThreads) * 16u, src);
+    }
+    const int label = a.label[m];
+    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label];
+    float most = xe;
+    float rest_most = -INFINITY, at = 0.f, rest[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (kLds > 0) {
+        V least;
+#pragma unroll
+        for (int e = 0; e < n; ++e) least[e] = (T)-INFINITY;
+        for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kBatch * kThreads) {
+            V y[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) y[k] = p + k * kThreads < c.pieces ? load_again<V>(body + (long long)(p + k * kThreads) * n) : least;
+            add_pieces<T>(y, rest_most, at, rest);
+        }
+        most = fmaxf(most, rest_most);
+    }
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < c.pieces) most = piece_max<T>(x[k], most);
+    if constexpr (kLds > 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (int k = 0; k < kLds; ++k)
+            if (tid + (kHeld + k) * kThreads < c.pieces) most = piece_max<T>(lower[k * kThreads + tid], most);
+    }
+    most = group_max<kThreads>(most, red[0]);
+    const float base = most == -INFINITY ? 0.f : most;  // (without a finite logit the sum is 0, or NaN)
+    float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
+    // (the empty asm keeps the row packed in registers: without it the compiler carries converted copies across)
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+        asm volatile("" : "+v"(x[k]));
+        if (tid + k * kThreads < c.pieces) piece_sum<T>(x[k], base, s);
+    }
+    if constexpr (kLds > 0) {
+#pragma unroll 1
+        for (int k = 0; k < kLds; ++k)
+            if (tid + (kHeld + k) * kThreads < c.pieces) piece_sum<T>(lower[k * kThreads + tid], base, s);
+    }
+    float sum = group_sum<kThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+    if constexpr (kLds > 0) {
+        if (c.pieces > (kHeld + kLds) * kThreads) {
+            float r = (rest[0] + rest[1]) + (rest[2] + rest[3]);
+            if (fabsf(base) <= kPowerMost) {
+                r = group_sum<kThreads>(rest_most == -INFINITY ? r : moved(r, at, power(base)), red[2]);
+                sum = (float)((double)sum + (double)r * from_power(base));
+            } else {  // (the powers say nothing: once more, from the largest one)
+                float once[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) piece_sum<T>(load_again<V>(body + (long long)p * n), base, once);
+                sum += group_sum<kThreads>((once[0] + once[1]) + (once[2] + once[3]), red[2]);
+            }
+        }
+    }
+    if (tid == 0) {
+        a.own[m] = sum == 0.f ? -INFINITY : xl - base;
+        a.sum[m] = sum;
+    }
+    const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
+    const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
+    const GradOf grad = grad_of(base, scale);
+    const auto put = [&](int p, const V& v) {
+        store_piece(out + c.head + (long long)p * n, with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, at_label));
+    };
+    // (each thread writes what it has read: in place nobody reads what another one has written)
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+        asm volatile("" : "+v"(x[k]));
+        if (tid + k * kThreads < c.pieces) put(tid + k * kThreads, x[k]);
+    }
+    if constexpr (kLds > 0) {
+#pragma unroll 1
+        for (int k = 0; k < kLds; ++k)
+            if (tid + (kHeld + k) * kThreads < c.pieces) put(tid + (kHeld + k) * kThreads, lower[k * kThreads + tid]);
+#pragma unroll 4
+        for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) put(p, load_piece<V>(body + (long long)p * n));
+    }
+    if (extra >= 0) out[extra] = (T)(extra == label ? at_label : scale * grown(xe, base));
+}
+
+// ---- stay --------------------------------------------------------------------------------------
+// 6001 x 128256 bf16 with gradient: 580 us, 652 by the kernel above.  What the loop must not do is wait for everything between a row's fetch and its
+// stores: a single element converted where it is loaded, or an item by a vector load, costs 3 to 13 % (100352 columns 466 us, 496).
+static constexpr int kStayThreads = 1024, kStayPieces = 16, kStayLds = 9, kStayRegs = kStayPieces - kStayLds;
+static constexpr int kStayRows = 1024;  // of a work-group in a launch
+static constexpr int kHeldBytes = kStayThreads * kStayPieces * 16;  // the longest row that a work-group holds
 
 // The rows of work-group b of n: list[0 .. counted) score, list[kStayRows - 1] downwards the others do not.  Either kind is dealt out in turn, from the
 // first work-group and from the last one: a row that scores costs twice as much as one that is only written.  With the rows in turn whatever they are
@@ -334,7 +429,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
     const Dealt mine = deal_rows(a, rows, vocab, blockIdx.x, gridDim.x, list, counts);
     const int total = mine.counted + mine.others;
     if (total == 0) return;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ahead + (uint32_t)wave * 1024u;
+    const uint32_t lds0 = lds_offset(ahead) + (uint32_t)wave * 1024u;
     struct Item {  // of the row that is on its way
         int row, label;
         float weight, advantage, old_logp, ref_logp;
@@ -363,10 +458,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         uint32_t at = (uint32_t)tid * 16u;
         asm volatile("" : "+v"(at));  // (one register, not one per piece kept across the loop)
 #pragma unroll
-        for (int k = 0; k < kStayLds; ++k)  // (s_nop: a load into LDS takes one wait state after a scalar write of m0)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds0 + k * kStayThreads * 16),
-                         "v"(at + k * kStayThreads * 16), "s"(src)
-                         : "memory", "m0");
+        for (int k = 0; k < kStayLds; ++k) load_to_lds(lds0 + k * kStayThreads * 16, at + k * kStayThreads * 16, src);
 #pragma unroll
         for (int k = 0; k < kStayRegs; ++k)
             next[k] = __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row) + c.head, 0, bytes, 0x00020000),
@@ -445,24 +537,14 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
 }
 
 // ---- parts -------------------------------------------------------------------------------------
-// The sum of a row, or of a part of it, in one pass: with the largest logit so far and the power of two above its exponential, by which the terms are
-// scaled; where a larger one comes the sum is moved by the difference of the powers, exactly.  Nothing is held, so that work-groups are small
-// and many rows are on their way at once: 6001 x 128256 bf16 without gradient 272 us, 5.7 TB/s read.
+// Nothing of a part is held, so that work-groups are small and many rows are on their way at once: 6001 x 128256 bf16 without gradient 272 us, 5.7 TB/s
+// read.
 static constexpr int kPartThreads = 256, kPartBatch = 8;
 static constexpr int kMaxParts = 64, kMaxPartials = 1024;  // of a row; of a call
 
 struct Partial {  // of a part: its largest logit, and its sum of exponentials relative to that one (0: it has no finite logit)
     float most, sum;
 };
-// Beyond it a power is no longer exact (masks of the type's lowest value, for one).
-static constexpr float kPowerMost = 1048576.f;
-__device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowerMost ? ceilf(most * kLog2e) : 0.f; }
-// 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
-__device__ __forceinline__ float grown2(float x, float power) {
-    return __builtin_amdgcn_exp2f(fmaf(x, 1.9259629e-8f, fmaf(x, kLog2e, -power)));
-}
-__device__ __forceinline__ float moved(float sum, float from, float to) { return ldexpf(sum, (int)(from - to)); }
-
 // The pieces of part j of n.
 __device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, int* end) {
     const int each = (pieces + n - 1) / n;
@@ -524,27 +606,12 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
 #pragma unroll
             for (int k = 0; k < kPartBatch; ++k) x[k] = next[k];
             load(next, p + kPartBatch * kPartThreads);
-            float higher = most;
-#pragma unroll
-            for (int k = 0; k < kPartBatch; ++k) higher = piece_max<T>(x[k], higher);
-            const float to = power(higher);
-            if (to != at && most != -INFINITY) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = moved(s[i], at, to);
-            }
-            most = higher;
-            at = to;
-#pragma unroll
-            for (int k = 0; k < kPartBatch; ++k) {
-                asm volatile("" : "+v"(x[k]));
-#pragma unroll
-                for (int e = 0; e < n; ++e) s[e & 3] += grown2((float)x[k][e], at);
-            }
+            add_pieces<T>(x, most, at, s);
         }
         const float group = group_max<kPartThreads>(most, red[0]), base = group == -INFINITY ? 0.f : group, sum = (s[0] + s[1]) + (s[2] + s[3]);
         float total = group_sum<kPartThreads>(most == -INFINITY ? sum : moved(sum, at, power(group)), red[1]);
         if (fabsf(base) <= kPowerMost) {
-            total = (float)((double)total * exp2((double)power(base) - (double)base * kLog2eDouble));
+            total = (float)((double)total * from_power(base));
         } else {  // (the powers say nothing: once more, from the largest one)
             float once[4] = {extra >= 0 ? grown(xe, base) : 0.f, 0.f, 0.f, 0.f};
             int q, to;
@@ -793,12 +860,12 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? at_label : scale * grown(xe, base));
 }
 
-// Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole, of which 256 and more (128 short ones) fill the card, unless
-// they are longer than what a work-group holds.  With gradient, bf16, vocabulary 128256, in parts and whole: 64 rows 20.9 us and 49, 200 rows 38.4 and 49,
-// 400 rows 65 and 50; fp32: 512 rows 127 and 149, 700 rows 176 and 209.
+// Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole, of which 256 and more (128 short ones) fill the card, 320
+// where a work-group's registers are not enough for one.  With gradient, bf16, vocabulary 128256, in parts and whole: 64 rows 20.9 us and 49, 200 rows
+// 38.4 and 49, 400 rows 65 and 50; fp32: 260 rows 66 and 74, 400 rows 97 and 82, 500 rows 115 and 95.
 static int parts_of(int rows, int vocab, size_t element) {
     const long long bytes = (long long)vocab * (long long)element;
-    if (rows > (bytes <= kHeldBytes / 2 ? 128 : 256) && bytes <= kHeldBytes) return 1;
+    if (rows > (bytes <= kHeldBytes / 2 ? 128 : bytes <= kHeldBytes ? 256 : 320)) return 1;
     return (int)std::max<long long>(std::min<long long>(std::min<long long>((bytes + 8191) / 8192, kMaxParts), kMaxPartials / rows), 1);
 }
 
@@ -824,7 +891,8 @@ static void launch_held(const T* logits, long long ld, int rows, int vocab, cons
     else if (pieces <= 256 * 8) go(k_policy_held<T, 256, 8>, 256);
     else if (pieces <= 256 * 16) go(k_policy_held<T, 256, 16>, 256);
     else if (pieces <= 512 * 16) go(k_policy_held<T, 512, 16>, 512);
-    else go(k_policy_held<T, 1024, 16>, 1024);
+    else if (pieces <= 1024 * 16) go(k_policy_held<T, 1024, 16>, 1024);
+    else go(k_policy_held<T, 1024, 16, 9>, 1024);
 }
 
 template <typename T>

@@ -344,3 +344,41 @@ def test_more_rows_than_the_work_groups_of_a_launch_have_lists_for():
         for side in (most, least):
             assert bool(((side[c] + d[c] / V).abs() <= (2.0 ** -8 + 3 * e) * d[c].abs() / V).all())
         assert bool((most[~c] == 0).all()) and bool((got[~c].amin(1) == 0).all())
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 131080), ("bf16", 204800), ("bf16", 204808), ("bf16", 230001), ("f32", 65540), ("f32", 102400), ("f32", 102404),
+                                     ("f32", 128256), ("f32", 150003)])
+def test_rows_that_registers_do_not_hold(dtype, V):
+    """Registers hold 16 pieces of 16 bytes a thread of 1024, LDS 9 more, the rest is read again: the label, the largest logit, forbidden
+    tokens, the type's lowest value and NaN on every side of the borders."""
+    import paper_2503_01066_amd as A
+    c = make(336, V, dtype, V)
+    per = 1024 * (8 if dtype == "bf16" else 4)
+    at = sorted({min(max(e, 0), V - 1) for b in (0, 16 * per, 25 * per, V) for e in (b - 1, b, b + 9)})
+    c["label"][:len(at)] = torch.tensor(at, dtype=torch.int32, device="cuda")
+    for i, e in enumerate(at):
+        c["x"][20 + i, e] = 60.0                   # the largest one
+        c["x"][40 + i, :e] = -math.inf             # nothing before,
+        c["x"][40 + i, e] = 1.0
+        c["x"][60 + i, e + 1:] = -math.inf         # nothing behind
+        c["x"][60 + i, e] = 1.0
+        c["x"][80 + i] = torch.finfo(DT[dtype]).min
+        c["x"][80 + i, e] = 3.0
+        c["x"][100 + i, e:] = 3e38                 # (so large that no power of two scales them)
+        c["label"][100 + i] = c["label"][40 + i] = V - 1
+        c["label"][60 + i], c["label"][80 + i] = 0, e
+        if e > 0:
+            c["x"][60 + i, 0] = 2.0
+    safe = torch.where(torch.isfinite(c["x"][:120]), c["x"][:120].double(), torch.full((), -1e300, dtype=torch.float64, device="cuda"))
+    logp = torch.log_softmax(safe - safe.amax(1, keepdim=True), 1).gather(1, c["label"][:120].long()[:, None])[:, 0]
+    c["old"][:120], c["ref"][:120] = (logp + 0.03).float(), (logp - 0.1).float()  # (ratios near 1 whatever was planted)
+    c["weight"][200:220] = 0
+    check(A, c)
+    c["x"][120] = -math.inf
+    for i, e in enumerate(at):
+        c["x"][130 + i, e] = math.nan
+    items = A.PolicyItems(c["label"], c["old"], c["adv"], c["weight"], ref_logp=c["ref"])
+    loss, logp, dx = A.alch_policy_loss(c["x"], items, clip_low=LOW, clip_high=HIGH, kl_coef=KL)
+    assert logp[120].item() == -math.inf and bool((dx[120] == 0).all()) and math.isnan(loss[0].item())
+    nan = torch.isnan(dx)
+    assert bool(nan[130:130 + len(at)].all()) and not bool(nan[:130].any()) and not bool(nan[130 + len(at):].any())
