@@ -139,12 +139,12 @@ def library_path():
 
 
 _LIB = None
-_PACK = _EMBED = 0  # addresses of alch_capture_pack and alch_embed_forward
+_PACK = _EMBED = _PACK_Q8 = _POLICY = 0  # addresses of alch_capture_pack, alch_embed_forward, alch_capture_pack_q8 and alch_policy_loss
 
 
 def lib():
     """Loads libalch.so (built by paper_2503_01066_amd.build); raises if it is missing."""
-    global _LIB, _PACK, _EMBED
+    global _LIB, _PACK, _EMBED, _PACK_Q8, _POLICY
     if _LIB is not None:
         return _LIB
     path = library_path()
@@ -252,6 +252,8 @@ def lib():
     L.alch_trace_collect.argtypes = [C.POINTER(CTraceRecord), C.c_int32, C.POINTER(C.c_int32)]
     _PACK = C.cast(L.alch_capture_pack, C.c_void_p).value
     _EMBED = C.cast(L.alch_embed_forward, C.c_void_p).value
+    _PACK_Q8 = C.cast(L.alch_capture_pack_q8, C.c_void_p).value
+    _POLICY = C.cast(L.alch_policy_loss, C.c_void_p).value
     _LIB = L
     return L
 
@@ -413,14 +415,20 @@ def alch_capture_pack_q8(batch, keep_mask, streams, capacity=None, dsts=None, st
     if dsts is None:
         capacity = T if capacity is None else int(capacity)
         dsts = _q8_pairs(capacity, streams, stream)
+    new = workspace is None
+    if new:
+        workspace = _empty((max(L.alch_capture_pack_workspace_bytes(T), 256),), torch.uint8, keep_mask.device, stream)
+    if _marshal is not None and stream is None:
+        out = _marshal.capture_pack_q8(_PACK_Q8, C.addressof(batch.c), T, batch.n_seqs, keep_mask, streams, dsts, capacity, workspace, dev, handle)
+        if out is not None:
+            _check(out[0])
+            return out[1], out[2], out[3], dsts
     entries, held = _q8_entries(streams, dsts, T, dev, "streams")
     if capacity is None:
         capacity = T if held is None else held
     elif held is not None and held < capacity:
         raise ValueError("dsts hold %d rows, capacity is %d" % (held, capacity))
-    if workspace is None:
-        workspace = _empty((max(L.alch_capture_pack_workspace_bytes(T), 256),), torch.uint8, keep_mask.device, stream)
-    else:
+    if not new:
         _check_dense(workspace, "workspace", torch.uint8, dev)
     # one allocation: the index, the sequences' counts behind it, then the status
     rows, bounds = max(capacity, 1), batch.n_seqs + 1
@@ -818,6 +826,15 @@ def alch_policy_loss(logits, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0, wa
     (n, vocab), dev, dt = logits.shape, logits.get_device(), logits.dtype
     handle = _place(dev, stream)
     _check_int32("n_items, vocab", n, vocab)
+    new = workspace is None
+    if new:
+        workspace = _empty((L.alch_policy_loss_workspace_bytes(n, vocab) or 256,), torch.uint8, logits.device, stream)
+    if _marshal is not None and stream is None:
+        out = _marshal.policy_loss(_POLICY, logits, items.n_items, items.index, items.words, clip_low, clip_high, kl_coef, want_grad, dlogits, logp, loss,
+                                   workspace, dev, handle)
+        if out is not None:
+            _check(out[0])
+            return out[1:]
     if items.n_items != n or items.index != dev:
         raise ValueError("logits %s on %s for %d items" % (tuple(logits.shape), logits.device, items.n_items))
     if dlogits is None and want_grad:
@@ -834,9 +851,7 @@ def alch_policy_loss(logits, items, clip_low=0.2, clip_high=0.2, kl_coef=0.0, wa
         loss = _empty((4,), torch.float32, logits.device, stream)
     else:
         _check_dense(loss, "loss", torch.float32, dev, (4,))
-    if workspace is None:
-        workspace = _empty((L.alch_policy_loss_workspace_bytes(n, vocab) or 256,), torch.uint8, logits.device, stream)
-    else:
+    if not new:
         _check_dense(workspace, "workspace", torch.uint8, dev)
     if dlogits is None:
         grad, pitch = None, 0
