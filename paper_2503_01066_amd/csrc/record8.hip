@@ -18,7 +18,10 @@ namespace alch {
 
 static constexpr int kGroup = ALCH_Q8_GROUP, kThreads = 256;
 static constexpr int kMaxPerLaunch = 16;        // streams of a launch
-static constexpr int kSmallRows = 256;          // up to so many rows the streams of a row have a work-group each
+// Up to so many rows the streams of a row have a work-group each, one behind the other's latency otherwise; fewer where every work-group looks through the
+// mask.  Six bf16 streams, packed: 450 rows of 256 to 1024 elements 9.0 us, so 5.3; 500 rows of 1024 to 14336 22.2 and 17.5, 1000 of them 28 and 37.
+// Expanded: 700 rows of 256 to 1024 6.1 and 3.7; 1500 of 1024 to 14336 36 and 35; 3000 of 512 to 8192 38.6 and 41.
+static constexpr int kSmallRows = 2048, kSmallRowsOfScan = 512;
 static constexpr int kGridMax = 1 << 20;        // work-groups of a launch; rows behind them are gone over in rounds
 static constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: below it 127 / a would leave fp32
 
@@ -369,9 +372,9 @@ static bool short_rows(const Q8Args& a) {
     return all;
 }
 // The grid for so many rows, of a launch whose work-groups have one or four of them each.
-static dim3 rows_grid(long long rows, bool four, int streams) {
+static dim3 rows_grid(long long rows, bool four, int streams, int small) {
     const long long groups = four ? (rows + 3) / 4 : rows;
-    return dim3((unsigned)std::min<long long>(groups, kGridMax), rows <= kSmallRows ? streams : 1);
+    return dim3((unsigned)std::min<long long>(groups, kGridMax), rows <= small ? streams : 1);
 }
 
 int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long long capacity, const int* kept_index, const int* n_kept_and_status,
@@ -383,7 +386,7 @@ int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long l
         const Q8Args a = q8_args(n_streams, streams, base);
         const bool four = short_rows(a);
         const auto kernel = four ? k_gather_q8<64> : k_gather_q8<kThreads>;
-        kernel<<<rows_grid(max_rows, four, a.n), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows);
+        kernel<<<rows_grid(max_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows);
     }
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
@@ -397,7 +400,7 @@ int launch_pack_q8(const uint8_t* mask, int T, const int* cu_seqlens, int n_seqs
         const Q8Args a = q8_args(n_streams, streams, 0);
         const bool four = short_rows(a), one = T <= kTokPerBlock;
         const auto kernel = four ? (one ? k_pack_small_q8<1, 64> : k_pack_small_q8<2, 64>) : one ? k_pack_small_q8<1, kThreads> : k_pack_small_q8<2, kThreads>;
-        kernel<<<rows_grid(max_rows, four, n_streams), kScanThreads, 0, stream>>>(a, mask, T, cu_seqlens, n_seqs + 1, kept_index, cu_kept, n_kept_and_status, capacity);
+        kernel<<<rows_grid(max_rows, four, n_streams, kSmallRowsOfScan), kScanThreads, 0, stream>>>(a, mask, T, cu_seqlens, n_seqs + 1, kept_index, cu_kept, n_kept_and_status, capacity);
         ALCH_HIP_TRY(hipGetLastError());
         return ALCH_OK;
     }
@@ -420,7 +423,7 @@ int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n
         }
         const bool four = short_rows(a);
         const auto kernel = four ? k_expand<64> : k_expand<kThreads>;
-        kernel<<<rows_grid(n_rows, four, a.n), kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
+        kernel<<<rows_grid(n_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
     }
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
