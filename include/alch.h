@@ -203,8 +203,8 @@ int alch_capture_pack_q8(const alch_batch* batch, const uint8_t* keep_mask, int3
 
 /*
  * alch_capture_gather_q8: the rows of alch_capture_pack_q8 alone, with the index of an earlier alch_capture_pack or
- * alch_capture_pack_q8 on the same batch and mask; see alch_capture_gather.  kept_index == NULL and n_kept_and_status == NULL: every
- * token is kept (dst_capacity_rows >= total_tokens then).
+ * alch_capture_pack_q8 on the same batch and mask; see alch_capture_gather.  A row whose index is no token of the batch (the index of a call
+ * that had no room) is left as it was.  kept_index == NULL and n_kept_and_status == NULL: every token is kept (dst_capacity_rows >= total_tokens then).
  */
 int alch_capture_gather_q8(const alch_batch* batch, int32_t n_streams, const alch_q8_stream* streams, int64_t dst_capacity_rows,
                            const int32_t* kept_index, const int32_t* n_kept_and_status, void* hip_stream);

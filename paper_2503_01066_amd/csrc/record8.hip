@@ -266,15 +266,17 @@ __device__ __forceinline__ int row_of() { return kLanes == kThreads ? 0 : __buil
 template <int kLanes>
 __device__ __forceinline__ int lane_of() { return kLanes == kThreads ? (int)threadIdx.x : (int)threadIdx.x & (kLanes - 1); }
 
-// A work-group a row, or four rows (the grid is sized for the most rows that the call can produce).  kept_index NULL: every token, n_rows of them.
+// A work-group a row, or four rows (the grid is sized for the most rows that the call can produce).  kept_index NULL: every token, n_rows of them.  An
+// index that is no token of the batch (of a call that had no room for it) leaves its row as it was.
 template <int kLanes>
 __global__ __launch_bounds__(kThreads) void k_gather_q8(Q8Args a, const int* __restrict__ kept_index, const int* __restrict__ n_kept_and_status,
-                                                        long long n_rows) {
+                                                        long long n_rows, int T) {
     constexpr int kRows = kThreads / kLanes;
     if (kept_index) n_rows = min(n_rows, (long long)n_kept_and_status[0]);
     const int lane = lane_of<kLanes>();
     for (long long r = (long long)blockIdx.x * kRows + row_of<kLanes>(); r < n_rows; r += (long long)gridDim.x * kRows) {
         const long long t = kept_index ? kept_index[r] : r;
+        if ((unsigned long long)t >= (unsigned long long)T) continue;
         for (int k = blockIdx.y; k < a.n; k += gridDim.y) quantise_row<kLanes>(a.s[k], t, r, lane);
     }
 }
@@ -386,7 +388,7 @@ int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long l
         const Q8Args a = q8_args(n_streams, streams, base);
         const bool four = short_rows(a);
         const auto kernel = four ? k_gather_q8<64> : k_gather_q8<kThreads>;
-        kernel<<<rows_grid(max_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows);
+        kernel<<<rows_grid(max_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows, T);
     }
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;

@@ -59,8 +59,9 @@ class RecordStore:
         stream = stream or torch.cuda.current_stream()
         coded = None
         if self.bits == 8 and self.keys:
-            with torch.cuda.stream(stream):
-                coded = dict(zip(self.keys, B.alch_capture_gather_q8(self.batch, [record[k] for k in self.keys], stream=stream)))
+            coded = dict(zip(self.keys, B.alch_capture_gather_q8(self.batch, [record[k] for k in self.keys], stream=stream)))
+            for k in self.keys:
+                record[k].record_stream(stream)
         done = torch.cuda.Event()
         done.record(stream)
         self.copy_stream.wait_event(done)

@@ -292,3 +292,26 @@ def test_offsets_beyond_32_bits():
     back, = A.alch_record_expand(pairs)
     one, = A.alch_record_expand(pairs, rows=torch.tensor([rows - 1, 0], dtype=torch.int32, device="cuda"))
     assert torch.equal(back[-1], one[0]) and int((back != 0).sum()) == int((want[0] != 0).sum()) and back[-2, 5] == -3.0
+
+
+@pytest.mark.parametrize("width", [40, 2000])
+def test_an_index_that_is_no_token_leaves_its_row(width):
+    import paper_2503_01066_amd as A
+    T = 9
+    x = values(T, width, "bf16", 4)
+    index = torch.tensor([-1, 3, T, 2 ** 31 - 1, 8, -2 ** 31, 0], dtype=torch.int32, device="cuda")
+    status = torch.tensor([7, 0], dtype=torch.int32, device="cuda")
+    dsts = [(torch.full((7, width), 77, dtype=torch.int8, device="cuda"), torch.full((7, -(-width // 64)), 7.5, device="cuda"))]
+    (codes, scales), = A.alch_capture_gather_q8(A.Batch(np.array([0, T], np.int32)), [x], kept_index=index, status=status, dsts=dsts)
+    want, wscales = quantised(host(x)[[3, 8, 0]])
+    assert same(codes.cpu().numpy()[[1, 4, 6]], want) and same(scales.cpu().numpy()[[1, 4, 6]], wscales)
+    rest = [0, 2, 3, 5]
+    assert bool((codes[rest] == 77).all()) and bool((scales[rest] == 7.5).all())
+    # the index of a call without room: one element that nothing wrote, and as many kept tokens as there are
+    mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+    index, _, status, _ = A.alch_capture_pack_q8(A.Batch(np.array([0, T], np.int32)), mask, [x], capacity=0)
+    assert status.tolist() == [T, 1]
+    index.fill_(-5)
+    dsts = [(torch.full((1, width), 77, dtype=torch.int8, device="cuda"), torch.full((1, -(-width // 64)), 7.5, device="cuda"))]
+    (codes, scales), = A.alch_capture_gather_q8(A.Batch(np.array([0, T], np.int32)), [x], kept_index=index, status=status, dsts=dsts)
+    assert bool((codes == 77).all()) and bool((scales == 7.5).all())
