@@ -26,6 +26,7 @@ typedef unsigned int u32x4_p __attribute__((ext_vector_type(4)));
 typedef int i32x4_p __attribute__((ext_vector_type(4)));
 
 static constexpr float kLog2e = 1.4426950408889634f;
+static constexpr float kLog2eRest = 1.9259629e-8f;  // log2 e - kLog2e
 static constexpr double kLog2eDouble = 1.4426950408889634;
 static constexpr int kGridMax = 1 << 20;  // work-groups of a launch; rows behind them are gone over in rounds
 
@@ -99,6 +100,21 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
     return v;
 }
 
+// What the loss is made of, of an item that scores: own - log(sum) is its log-probability.  An fp32 logit's difference from the largest one is rounded, and
+// the sum takes what that leaves, r: log(sum (1 - r)) = log(sum) - r.  (Of 16 bits the difference is exact, or as far as it matters.)
+template <typename T>
+__device__ __forceinline__ void put_item(const PolicyArgs& a, int m, float label_logit, float base, float sum) {
+    float own = label_logit - base;
+    if (sum == 0.f) {
+        own = -INFINITY;
+    } else if constexpr (sizeof(T) == 4) {
+        const float part = own - label_logit, r = (label_logit - (own - part)) + (-base - part);
+        if (fabsf(r) < 1e-3f) sum = fmaf(-sum, r, sum);  // (far beyond that, or none where there is an infinity)
+    }
+    a.own[m] = own;
+    a.sum[m] = sum;
+}
+
 // ---- a row in pieces ---------------------------------------------------------------------------
 // Of 16 bytes, at multiples of 16: rows of an odd vocabulary begin anywhere.  What lies before the first and behind the last piece, less than a
 // piece each, is an element each of the first 16 threads.
@@ -133,6 +149,12 @@ __device__ __forceinline__ int extra_of(const RowCut& c, int vocab) {
 // exp(x - base)
 __device__ __forceinline__ float grown(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
 
+// The same to a rounding or two: log2 e in two parts.  (What the first alone leaves is the same side's in every term of a sum: 1.3e-8 of x - base.)
+__device__ __forceinline__ float grown_exactly(float x, float base) {
+    const float d = x - base;
+    return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eRest));
+}
+
 template <typename T, typename V>
 __device__ __forceinline__ float piece_max(const V& x, float most) {
 #pragma unroll
@@ -143,7 +165,7 @@ __device__ __forceinline__ float piece_max(const V& x, float most) {
 template <typename T, typename V>
 __device__ __forceinline__ void piece_sum(const V& x, float base, float (&s)[4]) {
 #pragma unroll
-    for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown((float)x[e], base);
+    for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown_exactly((float)x[e], base);
 }
 // scale * exp(x - base).  bf16: the scale goes into the exponent, whose rounding (2^-20 of the result where it has 5 bits before the point) is far
 // below the result's own of 2^-9.
@@ -218,7 +240,7 @@ static constexpr float kPowerMost = 1048576.f;
 __device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowerMost ? ceilf(most * kLog2e) : 0.f; }
 // 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
 __device__ __forceinline__ float grown2(float x, float power) {
-    return __builtin_amdgcn_exp2f(fmaf(x, 1.9259629e-8f, fmaf(x, kLog2e, -power)));
+    return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, fmaf(x, kLog2e, -power)));
 }
 __device__ __forceinline__ float moved(float sum, float from, float to) { return ldexpf(sum, (int)(from - to)); }
 // Adds pieces to the sums s of a thread whose largest logit so far is most, scaled by at.
@@ -332,10 +354,7 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
             }
         }
     }
-    if (tid == 0) {
-        a.own[m] = sum == 0.f ? -INFINITY : xl - base;
-        a.sum[m] = sum;
-    }
+    if (tid == 0) put_item<T>(a, m, xl, base, sum);
     const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
     const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
     const GradOf grad = grad_of(base, scale);
@@ -517,10 +536,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);
         const GradOf grad = grad_of(base, scale);
         // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
-        if (tid == 0) {
-            a.own[r] = sum == 0.f ? -INFINITY : xl - base;
-            a.sum[r] = sum;
-        }
+        if (tid == 0) put_item<T>(a, r, xl, base, sum);
         if (extra >= 0) out[extra] = (T)(extra == item.label ? at_label : scale * grown(xe, base));
         int at = tid;
         asm volatile("" : "+v"(at) :: "memory");
@@ -624,8 +640,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
                 partial[b] = {group, total};
                 if (j == 0) a.own[m] = xl;
             } else {
-                a.own[m] = total == 0.f ? -INFINITY : xl - base;
-                a.sum[m] = total;
+                put_item<T>(a, m, xl, base, total);
             }
         }
     }
