@@ -453,7 +453,7 @@ typedef struct {
  *   loss_out  device float [4] out: { loss, sum w * -min(u, b), sum w * kl, sum of w where b < u (the share that is clipped) }
  *   workspace alch_policy_loss_workspace_bytes(n_items, vocab) bytes, 16-byte aligned; the size never falls with n_items
  * Sums run in a fixed order: results repeat bit for bit.  The order goes by the number of items, by where a row begins and by whether there is a
- * gradient: a token's logp_out in another call may differ in its last bits.  Statistics are held in fp32, the loss in 64 bits.  n_items = 0
+ * gradient: a token's logp_out in another call may differ in its last bits.  Exponentials are fp32, their sums and the loss 64 bits.  n_items = 0
  * gives zeros.
  * Supported: vocab <= 2^28.  Memory that the call writes may not overlap other memory of the call, except dlogits == logits.
  */

@@ -34,10 +34,12 @@ struct PolicyArgs {
     const int* label;
     const float *old_logp, *advantage, *weight, *ref_logp;
     float low, high, kl_coef;  // 1 - clip_low, 1 + clip_high
+    double exact_low, exact_high;  // the same, for the loss
     float *own, *sum;          // of every item: its label's logit less the row's largest, and the sum of exponentials (0: it scores nothing)
 
     PolicyArgs from(int m) const {  // of the items behind the first m
-        return {label + m, old_logp + m, advantage + m, weight + m, ref_logp ? ref_logp + m : nullptr, low, high, kl_coef, own + m, sum + m};
+        return {label + m, old_logp + m, advantage + m, weight + m, ref_logp ? ref_logp + m : nullptr, low, high, kl_coef,
+                exact_low, exact_high, own + m, sum + m};
     }
 };
 
@@ -70,15 +72,26 @@ __device__ __forceinline__ float wave_max(float v) {
     v = fmaxf(v, from_lane<0x142, 0xa>(v, v));
     return last_lane(fmaxf(v, from_lane<0x143, 0xc>(v, v)));
 }
-__device__ __forceinline__ float wave_sum(float v) {
-    v += from_lane<0xB1>(0.f, v);
-    v += from_lane<0x4E>(0.f, v);
-    v += from_lane<0x141>(0.f, v);
-    v += from_lane<0x140>(0.f, v);
-    v += from_lane<0x142, 0xa>(0.f, v);
-    return last_lane(v + from_lane<0x143, 0xc>(0.f, v));
+// Sums in 64 bits: beside a term of 1 every addition in fp32 loses 2^-24, ten of them are seen in the loss of a few items.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ double from_lane(double v) {  // 0 in rows outside of the mask
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, kCtrl, kRows, 0xf, false);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), kCtrl, kRows, 0xf, false);
+    return __builtin_bit_cast(double, (unsigned long long)high << 32 | low);
 }
-// Over a work-group, the result for everybody.  red: a float a wavefront, of each call its own.
+__device__ __forceinline__ double wave_sum(double v) {
+    v += from_lane<0xB1>(v);
+    v += from_lane<0x4E>(v);
+    v += from_lane<0x141>(v);
+    v += from_lane<0x140>(v);
+    v += from_lane<0x142, 0xa>(v);
+    v += from_lane<0x143, 0xc>(v);
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63), high = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    return __builtin_bit_cast(double, (unsigned long long)high << 32 | low);
+}
+// Over a work-group, the result for everybody.  red: a number a wavefront, of each call its own.
 template <int kThreads>
 __device__ __forceinline__ float group_max(float v, float* red) {
     v = wave_max(v);
@@ -90,7 +103,7 @@ __device__ __forceinline__ float group_max(float v, float* red) {
     return v;
 }
 template <int kThreads>
-__device__ __forceinline__ float group_sum(float v, float* red) {
+__device__ __forceinline__ double group_sum(double v, double* red) {
     v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -103,16 +116,16 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
 // What the loss is made of, of an item that scores: own - log(sum) is its log-probability.  An fp32 logit's difference from the largest one is rounded, and
 // the sum takes what that leaves, r: log(sum (1 - r)) = log(sum) - r.  (Of 16 bits the difference is exact, or as far as it matters.)
 template <typename T>
-__device__ __forceinline__ void put_item(const PolicyArgs& a, int m, float label_logit, float base, float sum) {
+__device__ __forceinline__ void put_item(const PolicyArgs& a, int m, float label_logit, float base, double sum) {
     float own = label_logit - base;
-    if (sum == 0.f) {
+    if (sum == 0.0) {
         own = -INFINITY;
     } else if constexpr (sizeof(T) == 4) {
         const float part = own - label_logit, r = (label_logit - (own - part)) + (-base - part);
-        if (fabsf(r) < 1e-3f) sum = fmaf(-sum, r, sum);  // (far beyond that, or none where there is an infinity)
+        if (fabsf(r) < 1e-3f) sum -= sum * r;  // (far beyond that, or none where there is an infinity)
     }
     a.own[m] = own;
-    a.sum[m] = sum;
+    a.sum[m] = (float)sum;
 }
 
 // ---- a row in pieces ---------------------------------------------------------------------------
@@ -161,11 +174,14 @@ __device__ __forceinline__ float piece_max(const V& x, float most) {
     for (int e = 0; e < Piece<T>::n; ++e) most = fmaxf(most, (float)x[e]);
     return most;
 }
-// Adds to a sum for every element of a piece: the sums are shorter, and do not wait for one another.
+__device__ __forceinline__ float sum_of(const float (&v)[4]) { return (v[0] + v[1]) + (v[2] + v[3]); }
+__device__ __forceinline__ float sum_of(const float (&v)[8]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 template <typename T, typename V>
-__device__ __forceinline__ void piece_sum(const V& x, float base, float (&s)[4]) {
+__device__ __forceinline__ double piece_sum(const V& x, float base) {
+    float v[Piece<T>::n];
 #pragma unroll
-    for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown_exactly((float)x[e], base);
+    for (int e = 0; e < Piece<T>::n; ++e) v[e] = grown_exactly((float)x[e], base);
+    return sum_of(v);
 }
 // scale * exp(x - base).  bf16: the scale goes into the exponent, whose rounding (2^-20 of the result where it has 5 bits before the point) is far
 // below the result's own of 2^-9.
@@ -242,25 +258,24 @@ __device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowe
 __device__ __forceinline__ float grown2(float x, float power) {
     return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, fmaf(x, kLog2e, -power)));
 }
-__device__ __forceinline__ float moved(float sum, float from, float to) { return ldexpf(sum, (int)(from - to)); }
-// Adds pieces to the sums s of a thread whose largest logit so far is most, scaled by at.
+__device__ __forceinline__ double moved(double sum, float from, float to) { return ldexp(sum, (int)(from - to)); }
+// Adds pieces to the sum s of a thread whose largest logit so far is most, scaled by at.
 template <typename T, typename V, int kBatch>
-__device__ __forceinline__ void add_pieces(V (&x)[kBatch], float& most, float& at, float (&s)[4]) {
+__device__ __forceinline__ void add_pieces(V (&x)[kBatch], float& most, float& at, double& s) {
     float higher = most;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) higher = piece_max<T>(x[k], higher);
     const float to = power(higher);
-    if (to != at && most != -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = moved(s[i], at, to);
-    }
+    if (to != at && most != -INFINITY) s = moved(s, at, to);
     most = higher;
     at = to;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
         asm volatile("" : "+v"(x[k]));
+        float v[Piece<T>::n];
 #pragma unroll
-        for (int e = 0; e < Piece<T>::n; ++e) s[e & 3] += grown2((float)x[k][e], at);
+        for (int e = 0; e < Piece<T>::n; ++e) v[e] = grown2((float)x[k][e], at);
+        s += sum_of(v);
     }
 }
 // The factor of a sum scaled by the power of two above exp(base), relative to exp(base): where |base| <= kPowerMost.
@@ -276,7 +291,8 @@ template <typename T, int kThreads, int kHeld, int kLds = 0>
 __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(const T* logits, long long ld, int vocab, PolicyArgs a, T* dlogits, long long ld_grad) {
     typedef typename Piece<T>::type V;
     constexpr int n = Piece<T>::n, kBatch = 2;
-    __shared__ float red[3][kThreads / 64];
+    __shared__ float red[kThreads / 64];
+    __shared__ double red_sum[2][kThreads / 64];
     __shared__ __attribute__((aligned(1024))) V lower[kLds > 0 ? kLds * kThreads : 1];
     const int m = blockIdx.x, tid = threadIdx.x;
     const T* row = logits + m * ld;
@@ -304,7 +320,8 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     const int label = a.label[m];
     const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label];
     float most = xe;
-    float rest_most = -INFINITY, at = 0.f, rest[4] = {0.f, 0.f, 0.f, 0.f};
+    float rest_most = -INFINITY, at = 0.f;
+    double rest = 0.0;
     if constexpr (kLds > 0) {
         V least;
 #pragma unroll
@@ -326,35 +343,34 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
         for (int k = 0; k < kLds; ++k)
             if (tid + (kHeld + k) * kThreads < c.pieces) most = piece_max<T>(lower[k * kThreads + tid], most);
     }
-    most = group_max<kThreads>(most, red[0]);
+    most = group_max<kThreads>(most, red);
     const float base = most == -INFINITY ? 0.f : most;  // (without a finite logit the sum is 0, or NaN)
-    float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
+    double s = grown_exactly(xe, base);
     // (the empty asm keeps the row packed in registers: without it the compiler carries converted copies across)
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
         asm volatile("" : "+v"(x[k]));
-        if (tid + k * kThreads < c.pieces) piece_sum<T>(x[k], base, s);
+        if (tid + k * kThreads < c.pieces) s += piece_sum<T>(x[k], base);
     }
     if constexpr (kLds > 0) {
 #pragma unroll 1
         for (int k = 0; k < kLds; ++k)
-            if (tid + (kHeld + k) * kThreads < c.pieces) piece_sum<T>(lower[k * kThreads + tid], base, s);
+            if (tid + (kHeld + k) * kThreads < c.pieces) s += piece_sum<T>(lower[k * kThreads + tid], base);
     }
-    float sum = group_sum<kThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+    double total = group_sum<kThreads>(s, red_sum[0]);
     if constexpr (kLds > 0) {
         if (c.pieces > (kHeld + kLds) * kThreads) {
-            float r = (rest[0] + rest[1]) + (rest[2] + rest[3]);
             if (fabsf(base) <= kPowerMost) {
-                r = group_sum<kThreads>(rest_most == -INFINITY ? r : moved(r, at, power(base)), red[2]);
-                sum = (float)((double)sum + (double)r * from_power(base));
+                total += group_sum<kThreads>(rest_most == -INFINITY ? rest : moved(rest, at, power(base)), red_sum[1]) * from_power(base);
             } else {  // (the powers say nothing: once more, from the largest one)
-                float once[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) piece_sum<T>(load_again<V>(body + (long long)p * n), base, once);
-                sum += group_sum<kThreads>((once[0] + once[1]) + (once[2] + once[3]), red[2]);
+                double once = 0.0;
+                for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) once += piece_sum<T>(load_again<V>(body + (long long)p * n), base);
+                total += group_sum<kThreads>(once, red_sum[1]);
             }
         }
     }
-    if (tid == 0) put_item<T>(a, m, xl, base, sum);
+    const float sum = (float)total;
+    if (tid == 0) put_item<T>(a, m, xl, base, total);
     const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
     const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
     const GradOf grad = grad_of(base, scale);
@@ -442,7 +458,8 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
     typedef std::conditional_t<sizeof(T) == 2, unsigned short, unsigned int> Bits;
     constexpr int n = Piece<T>::n;
     __shared__ __attribute__((aligned(1024))) V ahead[kStayLds * kStayThreads];
-    __shared__ float red[2][kStayThreads / 64];
+    __shared__ float red[kStayThreads / 64];
+    __shared__ double red_sum[kStayThreads / 64];
     __shared__ int list[kStayRows], counts[2][64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Dealt mine = deal_rows(a, rows, vocab, blockIdx.x, gridDim.x, list, counts);
@@ -522,21 +539,22 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k)
             if (tid + k * kStayThreads < c.pieces) most = piece_max<T>(x[k], most);
-        most = group_max<kStayThreads>(most, red[0]);
+        most = group_max<kStayThreads>(most, red);
         const float base = most == -INFINITY ? 0.f : most;
-        float s[4] = {grown(xe, base), 0.f, 0.f, 0.f};
+        double s = grown_exactly(xe, base);
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) {
             asm volatile("" : "+v"(x[k]));
-            if (tid + k * kStayThreads < c.pieces) piece_sum<T>(x[k], base, s);
+            if (tid + k * kStayThreads < c.pieces) s += piece_sum<T>(x[k], base);
         }
-        const float sum = group_sum<kStayThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+        const double total_sum = group_sum<kStayThreads>(s, red_sum);
+        const float sum = (float)total_sum;
         const float logp = xl - base - logf(sum);
         const float d = sum == 0.f ? 0.f : slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, logp), scale = sum == 0.f ? 0.f : -d / sum;
         const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);
         const GradOf grad = grad_of(base, scale);
         // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
-        if (tid == 0) put_item<T>(a, r, xl, base, sum);
+        if (tid == 0) put_item<T>(a, r, xl, base, total_sum);
         if (extra >= 0) out[extra] = (T)(extra == item.label ? at_label : scale * grown(xe, base));
         int at = tid;
         asm volatile("" : "+v"(at) :: "memory");
@@ -559,7 +577,8 @@ static constexpr int kPartThreads = 256, kPartBatch = 8;
 static constexpr int kMaxParts = 64, kMaxPartials = 1024;  // of a row; of a call
 
 struct Partial {  // of a part: its largest logit, and its sum of exponentials relative to that one (0: it has no finite logit)
-    float most, sum;
+    float most;
+    double sum;
 };
 // The pieces of part j of n.
 __device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, int* end) {
@@ -571,13 +590,8 @@ __device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, in
 struct Whole {
     float base, sum;
 };
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
 __device__ __forceinline__ double part_in(const Partial& p, float base) {  // (a part of NaN alone has no largest one either)
-    return p.most == -INFINITY ? (double)p.sum : (double)p.sum * exp2(((double)p.most - (double)base) * kLog2eDouble);
+    return p.most == -INFINITY ? p.sum : p.sum * exp2(((double)p.most - (double)base) * kLog2eDouble);
 }
 __device__ __forceinline__ Whole whole_row(const Partial& p) {
     const float most = wave_max(p.most), base = most == -INFINITY ? 0.f : most;
@@ -590,7 +604,8 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
                                                                Partial* __restrict__ partial) {
     typedef typename Piece<T>::type V;
     constexpr int n = Piece<T>::n;
-    __shared__ float red[3][kPartThreads / 64];
+    __shared__ float red[kPartThreads / 64];
+    __shared__ double red_sum[2][kPartThreads / 64];
     const int tid = threadIdx.x;
     V least;
 #pragma unroll
@@ -616,7 +631,8 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
         V next[kPartBatch];
         load(next, p);
         const float xl = j == 0 && tid == 0 ? (float)row[a.label[m]] : 0.f;
-        float most = xe, at = power(xe), s[4] = {extra >= 0 ? grown2(xe, at) : 0.f, 0.f, 0.f, 0.f};
+        float most = xe, at = power(xe);
+        double s = extra >= 0 ? grown2(xe, at) : 0.f;
         for (; p < end; p += kPartBatch * kPartThreads) {
             V x[kPartBatch];
 #pragma unroll
@@ -624,20 +640,20 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
             load(next, p + kPartBatch * kPartThreads);
             add_pieces<T>(x, most, at, s);
         }
-        const float group = group_max<kPartThreads>(most, red[0]), base = group == -INFINITY ? 0.f : group, sum = (s[0] + s[1]) + (s[2] + s[3]);
-        float total = group_sum<kPartThreads>(most == -INFINITY ? sum : moved(sum, at, power(group)), red[1]);
+        const float group = group_max<kPartThreads>(most, red), base = group == -INFINITY ? 0.f : group;
+        double total = group_sum<kPartThreads>(most == -INFINITY ? s : moved(s, at, power(group)), red_sum[0]);
         if (fabsf(base) <= kPowerMost) {
-            total = (float)((double)total * from_power(base));
+            total *= from_power(base);
         } else {  // (the powers say nothing: once more, from the largest one)
-            float once[4] = {extra >= 0 ? grown(xe, base) : 0.f, 0.f, 0.f, 0.f};
+            double once = extra >= 0 ? grown_exactly(xe, base) : 0.f;
             int q, to;
             part_of(c.pieces, j, parts, &q, &to);
-            for (q += tid; q < to; q += kPartThreads) piece_sum<T>(load_piece<V>(body + (long long)q * n), base, once);
-            total = group_sum<kPartThreads>((once[0] + once[1]) + (once[2] + once[3]), red[2]);
+            for (q += tid; q < to; q += kPartThreads) once += piece_sum<T>(load_piece<V>(body + (long long)q * n), base);
+            total = group_sum<kPartThreads>(once, red_sum[1]);
         }
         if (tid == 0) {
             if (parts > 1) {
-                partial[b] = {group, total};
+                partial[b] = {group, (double)(float)total};  // (a part of one logit alone has a sum of 1, which its power of two left to fp32)
                 if (j == 0) a.own[m] = xl;
             } else {
                 put_item<T>(a, m, xl, base, total);
@@ -652,7 +668,8 @@ template <typename T, int kHeld>
 __global__ __launch_bounds__(kPartThreads) void k_policy_few(const T* logits, long long ld, int vocab, PolicyArgs a, int parts, Partial* __restrict__ partial) {
     typedef typename Piece<T>::type V;
     constexpr int n = Piece<T>::n;
-    __shared__ float red[2][kPartThreads / 64];
+    __shared__ float red[kPartThreads / 64];
+    __shared__ double red_sum[kPartThreads / 64];
     const int tid = threadIdx.x, m = (int)blockIdx.x / parts, j = (int)blockIdx.x % parts;
     const T* row = logits + m * ld;
     const RowCut c = cut_row(row, vocab);
@@ -671,13 +688,13 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_few(const T* logits, lo
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
         if (begin + tid + k * kPartThreads < end) most = piece_max<T>(x[k], most);
-    most = group_max<kPartThreads>(most, red[0]);
+    most = group_max<kPartThreads>(most, red);
     const float base = most == -INFINITY ? 0.f : most;
-    float s[4] = {extra >= 0 ? grown(xe, base) : 0.f, 0.f, 0.f, 0.f};
+    double s = extra >= 0 ? grown_exactly(xe, base) : 0.f;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-        if (begin + tid + k * kPartThreads < end) piece_sum<T>(x[k], base, s);
-    const float sum = group_sum<kPartThreads>((s[0] + s[1]) + (s[2] + s[3]), red[1]);
+        if (begin + tid + k * kPartThreads < end) s += piece_sum<T>(x[k], base);
+    const double sum = group_sum<kPartThreads>(s, red_sum);
     if (tid == 0) {
         partial[blockIdx.x] = {most, sum};
         if (j == 0) a.own[m] = xl;
@@ -705,7 +722,7 @@ __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, doub
         } else {
             logp = own - log(sum);
             const double w = a.weight[m], A = a.advantage[m], ratio = exp(logp - (double)a.old_logp[m]);
-            const double bounded = ratio < (double)a.low ? (double)a.low : ratio > (double)a.high ? (double)a.high : ratio;
+            const double bounded = ratio < a.exact_low ? a.exact_low : ratio > a.exact_high ? a.exact_high : ratio;
             const double u = A == 0.0 ? 0.0 : ratio * A, b = A == 0.0 ? 0.0 : bounded * A;
             const bool cut = b < u;
             s.surrogate = w * (cut ? -b : -u);
@@ -762,7 +779,7 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int m = first + k * rows + tid / lanes;
-            p[k] = m < n && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.f};  // (of rows that do not score: whatever was there)
+            p[k] = m < n && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.0};  // (of rows that do not score: whatever was there)
             counted[k] = m < n && scores(a, m, vocab);
         }
 #pragma unroll
@@ -848,7 +865,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m], lane = tid & 63;
     const float xe = extra >= 0 ? (float)row[extra] : 0.f, weight = a.weight[m], advantage = a.advantage[m], old_logp = a.old_logp[m];
     const float ref_logp = a.ref_logp ? a.ref_logp[m] : 0.f, own = a.own[m];  // (own, and the parts below: of a row that does not score anything)
-    const Partial part = lane < parts ? partial[(long long)m * parts + lane] : Partial{-INFINITY, 0.f};
+    const Partial part = lane < parts ? partial[(long long)m * parts + lane] : Partial{-INFINITY, 0.0};
     float base = 0.f, scale = 0.f, at_label = 0.f;
     bool some = false;  // logits that the gradient depends on
     if ((unsigned)label < (unsigned)vocab && weight != 0.f) {
@@ -891,7 +908,8 @@ size_t policy_loss_workspace_bytes(int n_items, int vocab) {
 }
 
 static PolicyArgs policy_args(const alch_policy& p, int item0, float* own, float* sum) {
-    return PolicyArgs{p.label, p.old_logp, p.advantage, p.weight, p.ref_logp, 1.f - p.clip_low, 1.f + p.clip_high, p.kl_coef, own, sum}.from(item0);
+    const double low = 1.0 - (double)p.clip_low, high = 1.0 + (double)p.clip_high;
+    return PolicyArgs{p.label, p.old_logp, p.advantage, p.weight, p.ref_logp, (float)low, (float)high, p.kl_coef, low, high, own, sum}.from(item0);
 }
 
 template <typename T>
