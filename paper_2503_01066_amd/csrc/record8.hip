@@ -20,8 +20,9 @@ static constexpr int kGroup = ALCH_Q8_GROUP, kThreads = 256;
 static constexpr int kMaxPerLaunch = 16;        // streams of a launch
 // Up to so many rows the streams of a row have a work-group each, one behind the other's latency otherwise; fewer where every work-group looks through the
 // mask.  Six bf16 streams, packed: 450 rows of 256 to 1024 elements 9.0 us, so 5.3; 500 rows of 1024 to 14336 22.2 and 17.5, 1000 of them 28 and 37.
-// Expanded: 700 rows of 256 to 1024 6.1 and 3.7; 1500 of 1024 to 14336 36 and 35; 3000 of 512 to 8192 38.6 and 41.
-static constexpr int kSmallRows = 2048, kSmallRowsOfScan = 512;
+// Expanded: 700 rows of 256 to 1024 6.1 and 3.7; 1500 of 1024 to 14336 36 and 35; 3000 of 512 to 8192 38.6 and 41.  Short rows, four to a work-group:
+// expanded up to four times as many (8095 of 256 to 1024 21.9 and 19.6), packed not (2000 of 8000 tokens 11.6 and 13.3).
+static constexpr int kFewRows = 2048, kFewOfScan = 512;
 static constexpr int kGridMax = 1 << 20;        // work-groups of a launch; rows behind them are gone over in rounds
 static constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: below it 127 / a would leave fp32
 
@@ -374,9 +375,9 @@ static bool short_rows(const Q8Args& a) {
     return all;
 }
 // The grid for so many rows, of a launch whose work-groups have one or four of them each.
-static dim3 rows_grid(long long rows, bool four, int streams, int small) {
+static dim3 rows_grid(long long rows, bool four, int streams, bool dealt) {
     const long long groups = four ? (rows + 3) / 4 : rows;
-    return dim3((unsigned)std::min<long long>(groups, kGridMax), rows <= small ? streams : 1);
+    return dim3((unsigned)std::min<long long>(groups, kGridMax), dealt ? streams : 1);
 }
 
 int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long long capacity, const int* kept_index, const int* n_kept_and_status,
@@ -388,7 +389,7 @@ int launch_gather_q8(int T, int n_streams, const alch_q8_stream* streams, long l
         const Q8Args a = q8_args(n_streams, streams, base);
         const bool four = short_rows(a);
         const auto kernel = four ? k_gather_q8<64> : k_gather_q8<kThreads>;
-        kernel<<<rows_grid(max_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows, T);
+        kernel<<<rows_grid(max_rows, four, a.n, max_rows <= kFewRows), kThreads, 0, stream>>>(a, kept_index, n_kept_and_status, max_rows, T);
     }
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
@@ -402,7 +403,7 @@ int launch_pack_q8(const uint8_t* mask, int T, const int* cu_seqlens, int n_seqs
         const Q8Args a = q8_args(n_streams, streams, 0);
         const bool four = short_rows(a), one = T <= kTokPerBlock;
         const auto kernel = four ? (one ? k_pack_small_q8<1, 64> : k_pack_small_q8<2, 64>) : one ? k_pack_small_q8<1, kThreads> : k_pack_small_q8<2, kThreads>;
-        kernel<<<rows_grid(max_rows, four, n_streams, kSmallRowsOfScan), kScanThreads, 0, stream>>>(a, mask, T, cu_seqlens, n_seqs + 1, kept_index, cu_kept, n_kept_and_status, capacity);
+        kernel<<<rows_grid(max_rows, four, n_streams, max_rows <= kFewOfScan), kScanThreads, 0, stream>>>(a, mask, T, cu_seqlens, n_seqs + 1, kept_index, cu_kept, n_kept_and_status, capacity);
         ALCH_HIP_TRY(hipGetLastError());
         return ALCH_OK;
     }
@@ -425,7 +426,7 @@ int launch_expand(long long n_rows, const int* rows, long long n_src_rows, int n
         }
         const bool four = short_rows(a);
         const auto kernel = four ? k_expand<64> : k_expand<kThreads>;
-        kernel<<<rows_grid(n_rows, four, a.n, kSmallRows), kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
+        kernel<<<rows_grid(n_rows, four, a.n, n_rows <= (four ? 4 : 1) * kFewRows), kThreads, 0, stream>>>(a, rows, n_rows, n_src_rows);
     }
     ALCH_HIP_TRY(hipGetLastError());
     return ALCH_OK;
