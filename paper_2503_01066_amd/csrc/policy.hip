@@ -713,7 +713,14 @@ struct PolicySums {
         clipped += o.clipped;
     }
 };
-__device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, double own, double sum, float* __restrict__ logp_out) {
+struct ItemIn {  // (loaded at once and first: one behind the other, and behind the logarithm, they would be most of a small call)
+    float own, sum, weight, advantage, old_logp, ref_logp;
+    int label;
+};
+__device__ __forceinline__ ItemIn load_item(const PolicyArgs& a, int m) {
+    return {a.own[m], a.sum[m], a.weight[m], a.advantage[m], a.old_logp[m], a.ref_logp ? a.ref_logp[m] : 0.f, a.label[m]};
+}
+__device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, const ItemIn& in, double own, double sum, float* __restrict__ logp_out) {
     PolicySums s = {};
     double logp = 0.0;
     if (sum != 0.0 || own != 0.0) {  // (0, 0: it does not score; its logits are all -inf: -inf, 0)
@@ -721,7 +728,7 @@ __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, doub
             logp = own;
         } else {
             logp = own - log(sum);
-            const double w = a.weight[m], A = a.advantage[m], ratio = exp(logp - (double)a.old_logp[m]);
+            const double w = in.weight, A = in.advantage, ratio = exp(logp - (double)in.old_logp);
             const double bounded = ratio < a.exact_low ? a.exact_low : ratio > a.exact_high ? a.exact_high : ratio;
             const double u = A == 0.0 ? 0.0 : ratio * A, b = A == 0.0 ? 0.0 : bounded * A;
             const bool cut = b < u;
@@ -729,7 +736,7 @@ __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, doub
             s.clipped = cut ? w : 0.0;
             s.loss = s.surrogate;
             if (a.ref_logp) {
-                const double far = (double)a.ref_logp[m] - logp;
+                const double far = (double)in.ref_logp - logp;
                 s.kl = w * (expm1(far) - far);
                 if (a.kl_coef != 0.f) s.loss += (double)a.kl_coef * s.kl;
             }
@@ -761,7 +768,10 @@ __device__ __forceinline__ void put_sums(const PolicySums& s, double (*red)[4], 
 // Thread `first` of `stride`: its items' share.
 __device__ __forceinline__ PolicySums items_sums(const PolicyArgs& a, int n, int first, int stride, float* __restrict__ logp_out) {
     PolicySums s = {};
-    for (int m = first; m < n; m += stride) s.add(item_sums(a, m, a.own[m], a.sum[m], logp_out));
+    for (int m = first; m < n; m += stride) {
+        const ItemIn in = load_item(a, m);
+        s.add(item_sums(a, m, in, in.own, in.sum, logp_out));
+    }
     return s;
 }
 // The same of rows that were summed in parts (own is the label's logit as it stands), by a work-group.  Parts are joined by as many lanes as there
@@ -773,14 +783,13 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
     __shared__ float largest[kMaxPartials / 2];
     const int lanes = parts <= 1 ? 1 : 1 << (32 - __builtin_clz(parts - 1)), tid = threadIdx.x, j = tid & (lanes - 1), rows = kThreads / lanes;
     constexpr int kAhead = 4;
+    const ItemIn mine = load_item(a, min(tid, n - 1));
     for (int first = 0; first < n; first += rows * kAhead) {
         Partial p[kAhead];
-        bool counted[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int m = first + k * rows + tid / lanes;
             p[k] = m < n && j < parts ? partial[m * parts + j] : Partial{-INFINITY, 0.0};  // (of rows that do not score: whatever was there)
-            counted[k] = m < n && scores(a, m, vocab);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -792,7 +801,7 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
             double sum = part_in(p[k], base);
             for (int d = lanes >> 1; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
             if (m < n && j == 0) {
-                joined[m] = counted[k] ? sum : -1.0;
+                joined[m] = sum;
                 largest[m] = base;
             }
         }
@@ -800,9 +809,10 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
     __syncthreads();
     PolicySums s = {};
     for (int m = tid; m < n; m += kThreads) {
-        const bool counted = joined[m] != -1.0;
+        const ItemIn in = m == tid ? mine : load_item(a, m);
+        const bool counted = (unsigned)in.label < (unsigned)vocab && in.weight != 0.f;
         const double sum = counted ? joined[m] : 0.0;
-        s.add(item_sums(a, m, !counted ? 0.0 : sum == 0.0 ? -INFINITY : (double)a.own[m] - (double)largest[m], sum, logp_out));
+        s.add(item_sums(a, m, in, !counted ? 0.0 : sum == 0.0 ? -INFINITY : (double)in.own - (double)largest[m], sum, logp_out));
     }
     return s;
 }
