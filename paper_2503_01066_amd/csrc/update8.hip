@@ -330,16 +330,22 @@ __device__ __forceinline__ void adamw8(const alch_adamw8_tensor& t, long long be
     if constexpr (kMaster) store<kFull>(master, w, n);
     store<kFull>(param, w, n);
 }
+// A chunk by rounds.  Where the tensor ends in a round, the wavefronts before that end take their elements whole (434 bf16 adapters of 2944 elements and more:
+// 13.7 us, 19.3 with every wavefront element by element).
 template <typename T, bool kMaster, int kPer = 4>
 __device__ __forceinline__ void adamw8_chunk(const alch_adamw8_tensor& t, long long begin, const Adamw8Args& a, const Rates& r) {
-    constexpr int kRound = 256 * kPer;
-    const long long left = (long long)t.n - begin;
-    if (left >= kChunk) {
+    constexpr int kRound = 256 * kPer, kWave = 64 * kPer;
+    const int left = (int)min((long long)t.n - begin, (long long)kChunk), before = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * kWave;
+    if (left == kChunk) {
 #pragma unroll 1
         for (int at = 0; at < kChunk; at += kRound) adamw8<T, kMaster, kPer, true>(t, begin + at, kRound, a, r);
-    } else {
+        return;
+    }
 #pragma unroll 1
-        for (int at = 0; at < (int)left; at += kRound) adamw8<T, kMaster, kPer, false>(t, begin + at, min(kRound, (int)left - at), a, r);
+    for (int at = 0; at < left; at += kRound) {
+        const int own = left - at - before;
+        if (own >= kWave) adamw8<T, kMaster, kPer, true>(t, begin + at, kRound, a, r);
+        else if (own > 0) adamw8<T, kMaster, kPer, false>(t, begin + at, min(kRound, left - at), a, r);
     }
 }
 

@@ -344,3 +344,32 @@ def test_tensors_beyond_32_bit_offsets():
     A.alch_adamw8_step(A.Adamw8List([p], [g], [m], [v]), 0.125)
     assert p[n - 4:].tolist() == [0.0, -0.125, -0.125, -0.125] and p[5] == -0.125 and int((p != 0).sum()) == 4
     assert int((m[0] != 0).sum()) == 4 and int((v[0] != 0).sum()) == 4
+
+
+@pytest.mark.parametrize("dtype,master", [("f32", False), ("bf16", False), ("bf16", True), ("f32", True)])
+@pytest.mark.parametrize("base", [0, 1024, 2048, 3 * 1024, 4096, 8192])
+def test_ends_in_every_wavefront_of_a_round(dtype, master, base):
+    """Rounds are of 1024 or 2048 elements, a wavefront's part of 256 or 512, blocks of 64: ends beside each, whole wavefronts before them; and what lies
+    behind a tensor in its memory stays."""
+    import paper_2503_01066_amd as A
+    sizes = sorted({max(base + k * w + e, 1) for w in (256, 512) for k in range(5) for e in (-65, -1, 0, 1, 8, 64, 100)})
+    before = make(sizes, dtype, master, base)
+    states = [state(n, i, -7) for i, n in enumerate(sizes)]
+    roomy = lambda x, fill: torch.cat([x, torch.full((64,), fill, dtype=x.dtype, device="cuda")])
+    kept = [[None if x is None else roomy(x, 9) for x in t] for t in before]
+    after = [[None if x is None else x[:n] for x in t] for n, t in zip(sizes, kept)]
+    dev = lambda a: roomy(torch.from_numpy(a).cuda(), 99)
+    held = [[(dev(c), dev(s)) for c, s in st] for st in states]
+    cut = lambda k: [(h[k][0][:n], h[k][1][:-(-n // 64)]) for n, h in zip(sizes, held)]
+    masters = [t[2] for t in after] if master else None
+    for lo in range(0, len(sizes), 40):  # (few tensors, whose table is in registers)
+        part = slice(lo, lo + 40)
+        l = A.Adamw8List([t[0] for t in after[part]], [t[1] for t in after[part]], cut(0)[part], cut(1)[part], masters=masters and masters[part], weight_decay=0.1)
+        A.alch_adamw8_step(l, seed=7, step=3, **HYPER)
+        firsts = [r.first for r in l.host][:len(sizes[part])]
+        torch.cuda.synchronize()
+        check(before[part], states[part], after[part], cut(0)[part], cut(1)[part], firsts, [0.1] * 40, None, seed=7, step=3, **HYPER)
+    for n, t, h in zip(sizes, kept, held):
+        assert all(x is None or bool((x[n:] == 9).all()) for x in t)
+        for c, s in h:
+            assert bool((c[n:] == 99).all()) and bool((s[-(-n // 64):] == 99).all())
