@@ -904,11 +904,14 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
 
 // Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole, of which 256 and more (128 short ones) fill the card, 320
 // where a work-group's registers are not enough for one.  With gradient, bf16, vocabulary 128256, in parts and whole: 64 rows 20.9 us and 49, 200 rows
-// 38.4 and 49, 400 rows 65 and 50; fp32: 260 rows 66 and 74, 400 rows 97 and 82, 500 rows 115 and 95.
-static int parts_of(int rows, int vocab, size_t element) {
+// 38.4 and 49, 400 rows 65 and 50; fp32: 260 rows 66 and 74, 400 rows 97 and 82, 500 rows 115 and 95.  The work-group that forms the loss joins all of
+// them meanwhile, so that many rows have fewer: 20 x 128256 fp32 in 32 parts 10.5 us, in 51 12.8; 64 x 32000 fp32 in parts of 16 KB 9.2, of 8 KB 10.7.
+static int parts_of(int rows, int vocab, size_t element, bool grad) {
     const long long bytes = (long long)vocab * (long long)element;
     if (rows > (bytes <= kHeldBytes / 2 ? 128 : bytes <= kHeldBytes ? 256 : 320)) return 1;
-    return (int)std::max<long long>(std::min<long long>(std::min<long long>((bytes + 8191) / 8192, kMaxParts), kMaxPartials / rows), 1);
+    const int most = std::max(std::min(rows > 8 ? kMaxParts / 2 : kMaxParts, kMaxPartials / rows), 1);
+    const auto of = [&](long long each) { return (int)std::min<long long>((bytes + each - 1) / each, most); };
+    return grad && rows * of(8192) > kMaxPartials / 2 ? of(16384) : of(8192);
 }
 
 size_t policy_scratch_bytes() { return std::max(kMaxPartials * sizeof(Partial), kSumGroups * 4 * sizeof(double)); }
@@ -943,7 +946,7 @@ static int launch_rows(const T* logits, long long ld, int rows, int vocab, const
                        float* logp_out, float* loss_out, hipStream_t stream) {
     int n_cu = 0;
     ALCH_TRY(compute_units(&n_cu));
-    const int pieces = vocab / Piece<T>::n + 1, parts = loss_out ? parts_of(rows, vocab, sizeof(T)) : 1;
+    const int pieces = vocab / Piece<T>::n + 1, parts = loss_out ? parts_of(rows, vocab, sizeof(T), dlogits) : 1;
     if (parts > 1 || !dlogits) {
         const int held = (pieces + parts * kPartThreads - 1) / (parts * kPartThreads);  // of a part, a thread
         if (parts > 1 && held <= 2) k_policy_few<T, 2><<<rows * parts, kPartThreads, 0, stream>>>(logits, ld, vocab, a, parts, partial);
