@@ -278,7 +278,10 @@ __device__ __forceinline__ void add_pieces(V (&x)[kBatch], float& most, float& a
         s += sum_of(v);
     }
 }
-// The factor of a sum scaled by the power of two above exp(base), relative to exp(base): where |base| <= kPowerMost.
+// Whether sums of threads that have such powers are whole: a thread all of whose logits are below -kPowerMost has added nothing, and 128 below the
+// largest one that is no loss (e^-128 a term).
+__device__ __forceinline__ bool by_powers(float base) { return base >= 128.f - kPowerMost && base <= kPowerMost; }
+// The factor of a sum scaled by the power of two above exp(base), relative to exp(base): where by_powers(base).
 __device__ __forceinline__ double from_power(float base) { return exp2((double)power(base) - (double)base * kLog2eDouble); }
 
 // ---- held --------------------------------------------------------------------------------------
@@ -360,7 +363,7 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     double total = group_sum<kThreads>(s, red_sum[0]);
     if constexpr (kLds > 0) {
         if (c.pieces > (kHeld + kLds) * kThreads) {
-            if (fabsf(base) <= kPowerMost) {
+            if (by_powers(base)) {
                 total += group_sum<kThreads>(rest_most == -INFINITY ? rest : moved(rest, at, power(base)), red_sum[1]) * from_power(base);
             } else {  // (the powers say nothing: once more, from the largest one)
                 double once = 0.0;
@@ -642,7 +645,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
         }
         const float group = group_max<kPartThreads>(most, red), base = group == -INFINITY ? 0.f : group;
         double total = group_sum<kPartThreads>(most == -INFINITY ? s : moved(s, at, power(group)), red_sum[0]);
-        if (fabsf(base) <= kPowerMost) {
+        if (by_powers(base)) {
             total *= from_power(base);
         } else {  // (the powers say nothing: once more, from the largest one)
             double once = extra >= 0 ? grown_exactly(xe, base) : 0.f;
