@@ -453,8 +453,9 @@ typedef struct {
  *   loss_out  device float [4] out: { loss, sum w * -min(u, b), sum w * kl, sum of w where b < u (the share that is clipped) }
  *   workspace alch_policy_loss_workspace_bytes(n_items, vocab) bytes, 16-byte aligned; the size never falls with n_items
  * Sums run in a fixed order: results repeat bit for bit.  The order goes by the number of items, by where a row begins and by whether there is a
- * gradient: a token's logp_out in another call may differ in its last bits.  Exponentials are fp32, their sums and the loss 64 bits.  n_items = 0
- * gives zeros.
+ * gradient: a token's logp_out in another call may differ in its last bits.  Exponentials are fp32, the loss and the sums beyond 16 bytes of a row 64 bits;
+ * an item's sum is rounded to fp32 once.  A label that is the row's largest logit is left out of it, so that logp_out near 0 and 1 - p of
+ * the label's gradient keep their digits where p is all but 1.  n_items = 0 gives zeros.
  * Supported: vocab <= 2^28.  Memory that the call writes may not overlap other memory of the call, except dlogits == logits.
  */
 int alch_policy_loss(alch_dtype dtype, int32_t vocab, const void* logits, int64_t ld, const alch_policy* policy, void* dlogits,

@@ -11,8 +11,9 @@
 //   stay   rows of 128 to 256 KB: a row is half of a compute unit's registers, so that no second work-group fits that could load while
 //          this one computes.  One work-group a unit stays and has the next row on its way, 9 of 16 pieces to LDS, the others to registers;
 //   parts  few rows: several work-groups share one, in two launches with the parts' sums between them.
-// The row kernels leave x_label - max and the sum of exponentials of every item; the loss is made of them in 64 bits by one launch, where
-// terms of either sign cancel and a rounding of logp to fp32 would be seen.
+// A row is summed without its label: beside a p of all but 1 (most tokens that were sampled) the others' sum r is what logp = -log(1 + r) and
+// 1 - p = r / (1 + r) are made of, and 1 + r would lose it.  The row kernels leave x_label - max and the sum of every item; the loss is made of
+// them in 64 bits by one launch, where terms of either sign cancel and a rounding of logp to fp32 would be seen.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,7 +36,7 @@ struct PolicyArgs {
     const float *old_logp, *advantage, *weight, *ref_logp;
     float low, high, kl_coef;  // 1 - clip_low, 1 + clip_high
     double exact_low, exact_high;  // the same, for the loss
-    float *own, *sum;          // of every item: its label's logit less the row's largest, and the sum of exponentials (0: it scores nothing)
+    float *own, *sum;  // of every item: its label's logit less the row's largest, and the sum of exponentials; of a label that is the largest, of the others
 
     PolicyArgs from(int m) const {  // of the items behind the first m
         return {label + m, old_logp + m, advantage + m, weight + m, ref_logp ? ref_logp + m : nullptr, low, high, kl_coef,
@@ -113,14 +114,15 @@ __device__ __forceinline__ double group_sum(double v, double* red) {
     return v;
 }
 
-// What the loss is made of, of an item that scores: own - log(sum) is its log-probability.  An fp32 logit's difference from the largest one is rounded, and
-// the sum takes what that leaves, r: log(sum (1 - r)) = log(sum) - r.  (Of 16 bits the difference is exact, or as far as it matters.)
+static constexpr float kScoresNothing = -1.f;  // in the place of a sum
+// What the loss is made of, of an item that scores: own - log(sum) is its log-probability, -log(1 + sum) where own is 0.  An fp32 logit's difference from the
+// largest one is rounded, and the sum takes what that leaves, r: log(sum (1 - r)) = log(sum) - r.  (Of 16 bits the difference is exact, or as
+// far as it matters.)
 template <typename T>
-__device__ __forceinline__ void put_item(const PolicyArgs& a, int m, float label_logit, float base, double sum) {
-    float own = label_logit - base;
-    if (sum == 0.0) {
-        own = -INFINITY;
-    } else if constexpr (sizeof(T) == 4) {
+__device__ __forceinline__ void put_item(const PolicyArgs& a, int m, float label_logit, float base, float label_part, double rest) {
+    const float own = label_logit - base;
+    double sum = own == 0.f ? rest : rest + label_part;
+    if constexpr (sizeof(T) == 4) {
         const float part = own - label_logit, r = (label_logit - (own - part)) + (-base - part);
         if (fabsf(r) < 1e-3f) sum -= sum * r;  // (far beyond that, or none where there is an infinity)
     }
@@ -157,6 +159,19 @@ __device__ __forceinline__ int extra_of(const RowCut& c, int vocab) {
     if (tid < 8) return tid < c.head ? tid : -1;
     const int e = c.head + c.pieces * Piece<T>::n + tid - 8;
     return tid < 16 && e < vocab ? e : -1;
+}
+
+// The piece that the label is in, or -1.  It is left out of the sums; its other elements, one each of the first threads, are added to them.
+template <typename T>
+__device__ __forceinline__ int label_piece(const RowCut& c, int label) {
+    const int e = label - c.head;
+    return e >= 0 && e < c.pieces * Piece<T>::n ? e / Piece<T>::n : -1;
+}
+// The element of a thread among them, or -1; `first`: of which thread on.
+template <typename T>
+__device__ __forceinline__ int beside_label(const RowCut& c, int piece, int label, int first = 0) {
+    const int k = (int)threadIdx.x - first, e = c.head + piece * Piece<T>::n + k;
+    return piece >= 0 && (unsigned)k < (unsigned)Piece<T>::n && e != label ? e : -1;
 }
 
 // exp(x - base)
@@ -304,7 +319,7 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     const int extra = extra_of<T>(c, vocab);
     const T* body = row + c.head;
     if (!scores(a, m, vocab)) {
-        if (tid == 0) a.own[m] = 0.f, a.sum[m] = 0.f;
+        if (tid == 0) a.own[m] = 0.f, a.sum[m] = kScoresNothing;
         const V zero = {};
         for (int p = tid; p < c.pieces; p += kThreads) store_piece(out + c.head + (long long)p * n, zero);
         if (extra >= 0) out[extra] = (T)0.f;
@@ -320,11 +335,11 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
 #pragma unroll
         for (int k = 0; k < kLds; ++k) load_to_lds(lds + k * kThreads * 16, (uint32_t)(tid + (kHeld + k) * kThreads) * 16u, src);
     }
-    const int label = a.label[m];
-    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label];
+    const int label = a.label[m], without = label_piece<T>(c, label), beside = beside_label<T>(c, without, label);
+    const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, xl = (float)row[label], xb = beside >= 0 ? (float)row[beside] : -INFINITY;
     float most = xe;
     float rest_most = -INFINITY, at = 0.f;
-    double rest = 0.0;
+    double again = 0.0;
     if constexpr (kLds > 0) {
         V least;
 #pragma unroll
@@ -332,10 +347,11 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
         for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kBatch * kThreads) {
             V y[kBatch];
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) y[k] = p + k * kThreads < c.pieces ? load_again<V>(body + (long long)(p + k * kThreads) * n) : least;
-            add_pieces<T>(y, rest_most, at, rest);
+            for (int k = 0; k < kBatch; ++k)
+                y[k] = p + k * kThreads < c.pieces && p + k * kThreads != without ? load_again<V>(body + (long long)(p + k * kThreads) * n) : least;
+            add_pieces<T>(y, rest_most, at, again);
         }
-        most = fmaxf(most, rest_most);
+        most = fmaxf(fmaxf(most, rest_most), fmaxf(xl, xb));
     }
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
@@ -348,34 +364,35 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     }
     most = group_max<kThreads>(most, red);
     const float base = most == -INFINITY ? 0.f : most;  // (without a finite logit the sum is 0, or NaN)
-    double s = grown_exactly(xe, base);
+    double s = (extra == label ? 0.f : grown_exactly(xe, base)) + grown_exactly(xb, base);
     // (the empty asm keeps the row packed in registers: without it the compiler carries converted copies across)
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
         asm volatile("" : "+v"(x[k]));
-        if (tid + k * kThreads < c.pieces) s += piece_sum<T>(x[k], base);
+        if (tid + k * kThreads < c.pieces && tid + k * kThreads != without) s += piece_sum<T>(x[k], base);
     }
     if constexpr (kLds > 0) {
 #pragma unroll 1
         for (int k = 0; k < kLds; ++k)
-            if (tid + (kHeld + k) * kThreads < c.pieces) s += piece_sum<T>(lower[k * kThreads + tid], base);
+            if (tid + (kHeld + k) * kThreads < c.pieces && tid + (kHeld + k) * kThreads != without) s += piece_sum<T>(lower[k * kThreads + tid], base);
     }
-    double total = group_sum<kThreads>(s, red_sum[0]);
+    double others = group_sum<kThreads>(s, red_sum[0]);
     if constexpr (kLds > 0) {
         if (c.pieces > (kHeld + kLds) * kThreads) {
             if (by_powers(base)) {
-                total += group_sum<kThreads>(rest_most == -INFINITY ? rest : moved(rest, at, power(base)), red_sum[1]) * from_power(base);
+                others += group_sum<kThreads>(rest_most == -INFINITY ? again : moved(again, at, power(base)), red_sum[1]) * from_power(base);
             } else {  // (the powers say nothing: once more, from the largest one)
                 double once = 0.0;
-                for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) once += piece_sum<T>(load_again<V>(body + (long long)p * n), base);
-                total += group_sum<kThreads>(once, red_sum[1]);
+                for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads)
+                    if (p != without) once += piece_sum<T>(load_again<V>(body + (long long)p * n), base);
+                others += group_sum<kThreads>(once, red_sum[1]);
             }
         }
     }
-    const float sum = (float)total;
-    if (tid == 0) put_item<T>(a, m, xl, base, total);
-    const float logp = xl - base - logf(sum), d = sum == 0.f ? 0.f : slope(a, m, logp), scale = sum == 0.f ? 0.f : -d / sum;
-    const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);  // (1 - p without the difference)
+    const float label_part = grown_exactly(xl, base);
+    if (tid == 0) put_item<T>(a, m, xl, base, label_part, others);
+    const float rest = (float)others, sum = rest + label_part, d = sum == 0.f ? 0.f : slope(a, m, xl - base - logf(sum));
+    const float scale = sum == 0.f ? 0.f : -d / sum, at_label = -scale * rest;  // (d (1 - p) without the difference)
     const GradOf grad = grad_of(base, scale);
     const auto put = [&](int p, const V& v) {
         store_piece(out + c.head + (long long)p * n, with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, at_label));
@@ -485,13 +502,15 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
     };
     V next[kStayRegs];
     Bits xe_next, xl_next;  // what this thread has beside its pieces, and the label's logit: as loaded, for the row's own turn to look at
+    // an element before or behind the pieces, or of the label's piece
+    const auto single_of = [&](const RowCut& c, int label) { return tid < 16 ? extra_of<T>(c, vocab) : beside_label<T>(c, label_piece<T>(c, label), label, 16); };
     // The loads of a row: a wavefront fetches what its own lanes will use.  kStayPieces of them are issued whether or not the row reaches
     // as far, or is wanted at all.
     const auto fetch = [&](const Item& i) {
         const T* row = logits + (long long)i.row * ld;
         const RowCut c = cut_row(row, vocab);
         const int bytes = i.counted ? c.pieces * 16 : 0;
-        xe_next = reinterpret_cast<const Bits*>(row)[max(extra_of<T>(c, vocab), 0)];
+        xe_next = reinterpret_cast<const Bits*>(row)[max(single_of(c, i.counted ? i.label : -1), 0)];
         xl_next = reinterpret_cast<const Bits*>(row)[i.counted ? i.label : 0];
         const i32x4_p src = resource(row + c.head, bytes);
         uint32_t at = (uint32_t)tid * 16u;
@@ -517,7 +536,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         const auto dst = __builtin_amdgcn_make_buffer_rsrc(out + c.head, 0, c.pieces * 16, 0x00020000);
         if (!item.counted) {
             fetch(item1);
-            if (tid == 0) a.own[r] = 0.f, a.sum[r] = 0.f;
+            if (tid == 0) a.own[r] = 0.f, a.sum[r] = kScoresNothing;
             if (extra >= 0) out[extra] = (T)0.f;
             int at = tid;
             asm volatile("" : "+v"(at) :: "memory");
@@ -533,7 +552,8 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
 #pragma unroll
         for (int k = 0; k < kStayRegs; ++k) x[kStayLds + k] = next[k];
         asm volatile("" : "+v"(xe_next), "+v"(xl_next));
-        const float xe = extra >= 0 ? (float)__builtin_bit_cast(T, xe_next) : -INFINITY, xl = (float)__builtin_bit_cast(T, xl_next);
+        const int single = single_of(c, item.label), without = label_piece<T>(c, item.label);
+        const float xe = single >= 0 ? (float)__builtin_bit_cast(T, xe_next) : -INFINITY, xl = (float)__builtin_bit_cast(T, xl_next);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) asm volatile("" : "+v"(x[k]));  // (in registers before the next row overwrites them)
@@ -544,20 +564,22 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
             if (tid + k * kStayThreads < c.pieces) most = piece_max<T>(x[k], most);
         most = group_max<kStayThreads>(most, red);
         const float base = most == -INFINITY ? 0.f : most;
-        double s = grown_exactly(xe, base);
+        double s = single == item.label ? 0.f : grown_exactly(xe, base);
+        int own = tid;
+        asm volatile("" : "+v"(own));  // (as above)
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) {
             asm volatile("" : "+v"(x[k]));
-            if (tid + k * kStayThreads < c.pieces) s += piece_sum<T>(x[k], base);
+            if (own + k * kStayThreads < c.pieces && own + k * kStayThreads != without) s += piece_sum<T>(x[k], base);
         }
-        const double total_sum = group_sum<kStayThreads>(s, red_sum);
-        const float sum = (float)total_sum;
-        const float logp = xl - base - logf(sum);
-        const float d = sum == 0.f ? 0.f : slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, logp), scale = sum == 0.f ? 0.f : -d / sum;
-        const float at_label = sum == 0.f ? 0.f : d * -expm1f(logp);
+        const double others = group_sum<kStayThreads>(s, red_sum);
+        const float label_part = grown_exactly(xl, base);
+        const float rest = (float)others, sum = rest + label_part;
+        const float d = sum == 0.f ? 0.f : slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, xl - base - logf(sum));
+        const float scale = sum == 0.f ? 0.f : -d / sum, at_label = -scale * rest;
         const GradOf grad = grad_of(base, scale);
         // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
-        if (tid == 0) put_item<T>(a, r, xl, base, total_sum);
+        if (tid == 0) put_item<T>(a, r, xl, base, label_part, others);
         if (extra >= 0) out[extra] = (T)(extra == item.label ? at_label : scale * grown(xe, base));
         int at = tid;
         asm volatile("" : "+v"(at) :: "memory");
@@ -579,7 +601,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
 static constexpr int kPartThreads = 256, kPartBatch = 8;
 static constexpr int kMaxParts = 64, kMaxPartials = 1024;  // of a row; of a call
 
-struct Partial {  // of a part: its largest logit, and its sum of exponentials relative to that one (0: it has no finite logit)
+struct Partial {  // of a part: its largest logit, and its sum of exponentials, the label's left out, relative to that one (0: there is nothing finite else)
     float most;
     double sum;
 };
@@ -589,9 +611,9 @@ __device__ __forceinline__ void part_of(int pieces, int j, int n, int* begin, in
     *begin = min(j * each, pieces);
     *end = min(*begin + each, pieces);
 }
-// A row of its parts, one to a lane of a wavefront (kMaxParts at most).  base is the largest logit (0: there is none), sum relative to it.
+// A row of its parts, one to a lane of a wavefront (kMaxParts at most).  base is the largest logit (0: there is none), the others' sum relative to it.
 struct Whole {
-    float base, sum;
+    float base, rest;
 };
 __device__ __forceinline__ double part_in(const Partial& p, float base) {  // (a part of NaN alone has no largest one either)
     return p.most == -INFINITY ? p.sum : p.sum * exp2(((double)p.most - (double)base) * kLog2eDouble);
@@ -617,25 +639,27 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
         const int m = (int)(b / parts), j = (int)(b % parts);
         const T* row = logits + m * ld;
         if (!scores(a, m, vocab)) {
-            if (tid == 0 && parts == 1) a.own[m] = 0.f, a.sum[m] = 0.f;
+            if (tid == 0 && parts == 1) a.own[m] = 0.f, a.sum[m] = kScoresNothing;
             continue;
         }
         const RowCut c = cut_row(row, vocab);
         int p, end;
         part_of(c.pieces, j, parts, &p, &end);
+        const int label = a.label[m], without = label_piece<T>(c, label);
         p += tid;
         const T* body = row + c.head;
-        const int extra = j == 0 ? extra_of<T>(c, vocab) : -1;
-        const float xe = extra >= 0 ? (float)row[extra] : -INFINITY;
+        // (what is outside of the pieces, and of the label's piece, is the first part's)
+        const int single = j > 0 ? -1 : tid < 16 ? extra_of<T>(c, vocab) : beside_label<T>(c, without, label, 16);
+        const float xe = single >= 0 ? (float)row[single] : -INFINITY;
         const auto load = [&](V (&x)[kPartBatch], int at) {
 #pragma unroll
-            for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
+            for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end && at + k * kPartThreads != without ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
         };
         V next[kPartBatch];
         load(next, p);
-        const float xl = j == 0 && tid == 0 ? (float)row[a.label[m]] : 0.f;
-        float most = xe, at = power(xe);
-        double s = extra >= 0 ? grown2(xe, at) : 0.f;
+        const float xl = j == 0 ? (float)row[label] : -INFINITY;
+        float most = fmaxf(xe, xl), at = power(most);
+        double s = single >= 0 && single != label ? grown2(xe, at) : 0.f;
         for (; p < end; p += kPartBatch * kPartThreads) {
             V x[kPartBatch];
 #pragma unroll
@@ -648,18 +672,19 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
         if (by_powers(base)) {
             total *= from_power(base);
         } else {  // (the powers say nothing: once more, from the largest one)
-            double once = extra >= 0 ? grown_exactly(xe, base) : 0.f;
+            double once = single >= 0 && single != label ? grown_exactly(xe, base) : 0.f;
             int q, to;
             part_of(c.pieces, j, parts, &q, &to);
-            for (q += tid; q < to; q += kPartThreads) once += piece_sum<T>(load_piece<V>(body + (long long)q * n), base);
+            for (q += tid; q < to; q += kPartThreads)
+                if (q != without) once += piece_sum<T>(load_piece<V>(body + (long long)q * n), base);
             total = group_sum<kPartThreads>(once, red_sum[1]);
         }
         if (tid == 0) {
             if (parts > 1) {
-                partial[b] = {group, (double)(float)total};  // (a part of one logit alone has a sum of 1, which its power of two left to fp32)
+                partial[b] = {group, total};
                 if (j == 0) a.own[m] = xl;
             } else {
-                put_item<T>(a, m, xl, base, total);
+                put_item<T>(a, m, xl, base, grown_exactly(xl, base), total);
             }
         }
     }
@@ -686,17 +711,18 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_few(const T* logits, lo
     const int extra = j == 0 ? extra_of<T>(c, vocab) : -1, label = a.label[m];
     const float xe = extra >= 0 ? (float)row[extra] : -INFINITY, weight = a.weight[m];
     if ((unsigned)label >= (unsigned)vocab || weight == 0.f) return;
-    const float xl = j == 0 && tid == 0 ? (float)row[label] : 0.f;
+    const int without = label_piece<T>(c, label), beside = without >= begin && without < end ? beside_label<T>(c, without, label) : -1;
+    const float xl = j == 0 ? (float)row[label] : -INFINITY, xb = beside >= 0 ? (float)row[beside] : -INFINITY;
     float most = xe;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
         if (begin + tid + k * kPartThreads < end) most = piece_max<T>(x[k], most);
     most = group_max<kPartThreads>(most, red);
     const float base = most == -INFINITY ? 0.f : most;
-    double s = extra >= 0 ? grown_exactly(xe, base) : 0.f;
+    double s = (extra >= 0 && extra != label ? grown_exactly(xe, base) : 0.f) + grown_exactly(xb, base);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-        if (begin + tid + k * kPartThreads < end) s += piece_sum<T>(x[k], base);
+        if (begin + tid + k * kPartThreads < end && begin + tid + k * kPartThreads != without) s += piece_sum<T>(x[k], base);
     const double sum = group_sum<kPartThreads>(s, red_sum);
     if (tid == 0) {
         partial[blockIdx.x] = {most, sum};
@@ -723,14 +749,16 @@ struct ItemIn {  // (loaded at once and first: one behind the other, and behind 
 __device__ __forceinline__ ItemIn load_item(const PolicyArgs& a, int m) {
     return {a.own[m], a.sum[m], a.weight[m], a.advantage[m], a.old_logp[m], a.ref_logp ? a.ref_logp[m] : 0.f, a.label[m]};
 }
+// (own and sum as put_item leaves them)
 __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, const ItemIn& in, double own, double sum, float* __restrict__ logp_out) {
     PolicySums s = {};
     double logp = 0.0;
-    if (sum != 0.0 || own != 0.0) {  // (0, 0: it does not score; its logits are all -inf: -inf, 0)
-        if (sum == 0.0) {
+    if (!(sum < 0.0)) {
+        if (sum == 0.0 && own != 0.0) {  // (its logits are all -inf)
             logp = own;
         } else {
-            logp = own - log(sum);
+            // (a small sum by its series: 2^-40 of it are left out)
+            logp = own == 0.0 && sum < 0x1p-20 ? sum * (0.5 * sum - 1.0) : own - log(own == 0.0 ? 1.0 + sum : sum);
             const double w = in.weight, A = in.advantage, ratio = exp(logp - (double)in.old_logp);
             const double bounded = ratio < a.exact_low ? a.exact_low : ratio > a.exact_high ? a.exact_high : ratio;
             const double u = A == 0.0 ? 0.0 : ratio * A, b = A == 0.0 ? 0.0 : bounded * A;
@@ -814,8 +842,8 @@ __device__ __forceinline__ PolicySums parts_sums(const PolicyArgs& a, int n, int
     for (int m = tid; m < n; m += kThreads) {
         const ItemIn in = m == tid ? mine : load_item(a, m);
         const bool counted = (unsigned)in.label < (unsigned)vocab && in.weight != 0.f;
-        const double sum = counted ? joined[m] : 0.0;
-        s.add(item_sums(a, m, in, !counted ? 0.0 : sum == 0.0 ? -INFINITY : (double)in.own - (double)largest[m], sum, logp_out));
+        const double own = counted ? (double)in.own - (double)largest[m] : 0.0;
+        s.add(item_sums(a, m, in, own, !counted ? (double)kScoresNothing : own == 0.0 ? joined[m] : joined[m] + grown_exactly(in.own, largest[m]), logp_out));
     }
     return s;
 }
@@ -883,12 +911,13 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     bool some = false;  // logits that the gradient depends on
     if ((unsigned)label < (unsigned)vocab && weight != 0.f) {
         const Whole w = whole_row(part);
-        some = w.sum != 0.f;
+        const float sum = w.rest + grown_exactly(own, w.base);
+        some = sum != 0.f;
         if (some) {
-            const float logp = own - w.base - logf(w.sum), d = slope(a, weight, advantage, old_logp, ref_logp, logp);
+            const float d = slope(a, weight, advantage, old_logp, ref_logp, own - w.base - logf(sum));
             base = w.base;
-            scale = -d / w.sum;
-            at_label = d * -expm1f(logp);
+            scale = -d / sum;
+            at_label = -scale * w.rest;
         }
     }
     const GradOf grad = grad_of(base, scale);
