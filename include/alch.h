@@ -429,9 +429,12 @@ int alch_stack_backward_dpo(const alch_layer_shape* shape, int32_t n_layers, int
  *     loss = sum over items of w * (-min(u, b) + kl_coef * kl)
  *     d loss / d logits = d * (onehot(label) - softmax),   d = w * (-(b < u ? 0 : u) + kl_coef * (1 - exp(ref_logp - logp)))
  * The weights hold the mean that is wanted (1 / items, 1 / (sequences * length), ..).  An item whose label is outside 0..vocab-1 or whose
- * weight is 0 scores nothing: its logits are not read, its gradient is zero, its logp_out 0.  Logits of -inf (forbidden tokens) have
- * probability 0 and gradient 0; an item all of whose logits are -inf scores nothing either, its logp_out is -inf.  A = 0 has u = b = 0 whatever
- * the ratio.  NaN and +inf among the logits of an item that scores make its gradient, logp_out and the loss NaN.
+ * weight is 0 scores nothing: its logits have no part in anything, its gradient is zero, its logp_out 0.  Logits of -inf (forbidden tokens) have
+ * probability 0 and gradient 0 whatever d is, the label's among them; an item all of whose logits are -inf scores nothing either, its logp_out is -inf.  A
+ * label that is forbidden while others are not has ratio 0 and kl = inf: with a kl_coef the loss is infinite and so are the gradients of the tokens that
+ * are allowed.  ref_logp = -inf has kl = inf and 1 - exp(ref_logp - logp) = 1.  A d beyond fp32 is multiplied before it is rounded: an entry of the gradient is
+ * infinite where it is beyond its type itself.  A = 0 has u = b = 0 whatever the ratio.  NaN and +inf among the logits of an item that scores make its
+ * gradient, logp_out and the loss NaN, and so do NaN and infinities of its other numbers that the formulas make no number of.
  */
 typedef struct {
     int32_t n_items;

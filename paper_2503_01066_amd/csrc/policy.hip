@@ -44,16 +44,39 @@ struct PolicyArgs {
     }
 };
 
-// d of the gradient, from an item's log-probability.
-__device__ __forceinline__ float slope(const PolicyArgs& a, float w, float A, float old, float ref, float logp) {
+static constexpr float kNoPower = 0x1p30f;  // a power of two that stands for infinity
+// 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
+__device__ __forceinline__ float grown2(float x, float power) {
+    return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, fmaf(x, kLog2e, -power)));
+}
+// d of the gradient: d 2^shift, the power of two only where the number leaves fp32.
+struct Slope {
+    float d, shift;
+};
+// With e^m taken out, m the larger of the exponents: what p makes small again is not lost, and a logit of -inf has 0 times a number.
+__device__ __forceinline__ Slope far_slope(const PolicyArgs& a, float w, float A, float old, float ref, float logp, bool cut) {
+    const bool with_kl = a.ref_logp && a.kl_coef != 0.f;
+    const float up = logp - old, far = ref - logp, m = fmaxf(fmaxf(up, with_kl ? far : 0.f), 0.f);
+    const auto without_m = [m](float x) { return x == m ? 1.f : expf(x - m); };
+    float d = cut ? 0.f : -0.25f * A * without_m(up);  // (a quarter: the sum does not overflow)
+    if (with_kl) d -= 0.25f * a.kl_coef * (without_m(far) - without_m(0.f));
+    const float power = fminf(ceilf(m * kLog2e), kNoPower);
+    const int exponents = __builtin_amdgcn_frexp_expf(d) + __builtin_amdgcn_frexp_expf(w) + 2;
+    d = __builtin_amdgcn_frexp_mantf(d) * __builtin_amdgcn_frexp_mantf(w);
+    return {power < kNoPower ? d * grown2(m, power) : d, power + (float)exponents};
+}
+// From an item's log-probability.
+__device__ __forceinline__ Slope slope(const PolicyArgs& a, float w, float A, float old, float ref, float logp) {
     const float ratio = expf(logp - old);
     const float bounded = ratio < a.low ? a.low : ratio > a.high ? a.high : ratio;  // (NaN stays)
     const float u = ratio * A;
-    float d = A == 0.f || bounded * A < u ? 0.f : -u;
+    const bool cut = A == 0.f || bounded * A < u;
+    float d = cut ? 0.f : -u;
     if (a.ref_logp && a.kl_coef != 0.f) d -= a.kl_coef * expm1f(ref - logp);
-    return w * d;
+    d *= w;
+    return __builtin_expect(fabsf(d) < INFINITY, 1) ? Slope{d, 0.f} : far_slope(a, w, A, old, ref, logp, cut);
 }
-__device__ __forceinline__ float slope(const PolicyArgs& a, int m, float logp) {
+__device__ __forceinline__ Slope slope(const PolicyArgs& a, int m, float logp) {
     return slope(a, a.weight[m], a.advantage[m], a.old_logp[m], a.ref_logp ? a.ref_logp[m] : 0.f, logp);
 }
 __device__ __forceinline__ bool scores(const PolicyArgs& a, int m, int vocab) { return (unsigned)a.label[m] < (unsigned)vocab && a.weight[m] != 0.f; }
@@ -174,10 +197,7 @@ __device__ __forceinline__ int beside_label(const RowCut& c, int piece, int labe
     return piece >= 0 && (unsigned)k < (unsigned)Piece<T>::n && e != label ? e : -1;
 }
 
-// exp(x - base)
-__device__ __forceinline__ float grown(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
-
-// The same to a rounding or two: log2 e in two parts.  (What the first alone leaves is the same side's in every term of a sum: 1.3e-8 of x - base.)
+// exp(x - base) to a rounding or two: log2 e in two parts.  (What the first alone leaves is the same side's in every term of a sum: 1.3e-8 of x - base.)
 __device__ __forceinline__ float grown_exactly(float x, float base) {
     const float d = x - base;
     return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eRest));
@@ -198,15 +218,25 @@ __device__ __forceinline__ double piece_sum(const V& x, float base) {
     for (int e = 0; e < Piece<T>::n; ++e) v[e] = grown_exactly((float)x[e], base);
     return sum_of(v);
 }
-// scale * exp(x - base).  bf16: the scale goes into the exponent, whose rounding (2^-20 of the result where it has 5 bits before the point) is far
-// below the result's own of 2^-9.
+// scale 2^shift exp(x - base); at_label in the label's place.  bf16: the scale goes into the exponent, whose rounding (2^-20 of the result where it has 5
+// bits before the point) is far below the result's own of 2^-9.
 struct GradOf {
-    float base, scale, log2_scale;
+    float base, scale, shift, log2_scale, at_label;
     uint32_t sign;
 };
-__device__ __forceinline__ GradOf grad_of(float base, float scale) {
-    return {base, scale, __builtin_amdgcn_logf(fabsf(scale)), __builtin_bit_cast(uint32_t, scale) & 0x80000000u};
+// rest: the sum of the others' exponentials, sum: with the label's (0: nothing that the gradient depends on)
+__device__ __forceinline__ GradOf grad_of(float label_logit, float base, float rest, float sum, Slope s) {
+    if (sum == 0.f) s = {0.f, 0.f};
+    float scale = sum == 0.f ? 0.f : -s.d / sum, at_label = -scale * rest;  // (d (1 - p) without the difference)
+    if (__builtin_expect(s.shift != 0.f, 0)) {  // (the scale to 1 and more, so that a product is not beyond fp32 before it has to be)
+        at_label = label_logit == -INFINITY ? 0.f : ldexpf(at_label, (int)s.shift);
+        const int e = __builtin_amdgcn_frexp_expf(scale) - 1;
+        scale = ldexpf(scale, -e);
+        s.shift += (float)e;
+    }
+    return {base, scale, s.shift, __builtin_amdgcn_logf(fabsf(scale)) + s.shift, at_label, __builtin_bit_cast(uint32_t, scale) & 0x80000000u};
 }
+__device__ __forceinline__ float single_grad(float x, const GradOf& o) { return o.scale * __builtin_amdgcn_exp2f(fmaf(x - o.base, kLog2e, o.shift)); }
 template <typename T, typename V>
 __device__ __forceinline__ V piece_grad(const V& x, const GradOf& o) {
     V g;
@@ -216,7 +246,7 @@ __device__ __forceinline__ V piece_grad(const V& x, const GradOf& o) {
         return __builtin_bit_cast(V, __builtin_bit_cast(u32x4_p, g) ^ (o.sign | o.sign >> 16));
     } else {
 #pragma unroll
-        for (int e = 0; e < Piece<T>::n; ++e) g[e] = o.scale * grown((float)x[e], o.base);
+        for (int e = 0; e < Piece<T>::n; ++e) g[e] = single_grad((float)x[e], o);
         return g;
     }
 }
@@ -269,10 +299,6 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t
 // Beyond it a power is no longer exact (masks of the type's lowest value, for one).
 static constexpr float kPowerMost = 1048576.f;
 __device__ __forceinline__ float power(float most) { return fabsf(most) <= kPowerMost ? ceilf(most * kLog2e) : 0.f; }
-// 2^(x log2 e - power), log2 e in two parts: the product alone would lose as much as x is large
-__device__ __forceinline__ float grown2(float x, float power) {
-    return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, fmaf(x, kLog2e, -power)));
-}
 __device__ __forceinline__ double moved(double sum, float from, float to) { return ldexp(sum, (int)(from - to)); }
 // Adds pieces to the sum s of a thread whose largest logit so far is most, scaled by at.
 template <typename T, typename V, int kBatch>
@@ -391,11 +417,10 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     }
     const float label_part = grown_exactly(xl, base);
     if (tid == 0) put_item<T>(a, m, xl, base, label_part, others);
-    const float rest = (float)others, sum = rest + label_part, d = sum == 0.f ? 0.f : slope(a, m, xl - base - logf(sum));
-    const float scale = sum == 0.f ? 0.f : -d / sum, at_label = -scale * rest;  // (d (1 - p) without the difference)
-    const GradOf grad = grad_of(base, scale);
+    const float rest = (float)others, sum = rest + label_part;
+    const GradOf grad = grad_of(xl, base, rest, sum, slope(a, m, xl - base - logf(sum)));
     const auto put = [&](int p, const V& v) {
-        store_piece(out + c.head + (long long)p * n, with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, at_label));
+        store_piece(out + c.head + (long long)p * n, with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, grad.at_label));
     };
     // (each thread writes what it has read: in place nobody reads what another one has written)
 #pragma unroll
@@ -410,7 +435,7 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
 #pragma unroll 4
         for (int p = tid + (kHeld + kLds) * kThreads; p < c.pieces; p += kThreads) put(p, load_piece<V>(body + (long long)p * n));
     }
-    if (extra >= 0) out[extra] = (T)(extra == label ? at_label : scale * grown(xe, base));
+    if (extra >= 0) out[extra] = (T)(extra == label ? grad.at_label : single_grad(xe, grad));
 }
 
 // ---- stay --------------------------------------------------------------------------------------
@@ -575,18 +600,16 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         const double others = group_sum<kStayThreads>(s, red_sum);
         const float label_part = grown_exactly(xl, base);
         const float rest = (float)others, sum = rest + label_part;
-        const float d = sum == 0.f ? 0.f : slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, xl - base - logf(sum));
-        const float scale = sum == 0.f ? 0.f : -d / sum, at_label = -scale * rest;
-        const GradOf grad = grad_of(base, scale);
+        const GradOf grad = grad_of(xl, base, rest, sum, slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, xl - base - logf(sum)));
         // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
         if (tid == 0) put_item<T>(a, r, xl, base, label_part, others);
-        if (extra >= 0) out[extra] = (T)(extra == item.label ? at_label : scale * grown(xe, base));
+        if (extra >= 0) out[extra] = (T)(extra == item.label ? grad.at_label : single_grad(xe, grad));
         int at = tid;
         asm volatile("" : "+v"(at) :: "memory");
 #pragma unroll
         for (int k = 0; k < kStayPieces; ++k) {
             asm volatile("" : "+v"(x[k]));
-            const V g = with_label<T>(piece_grad<T>(x[k], grad), item.label - c.head - (at + k * kStayThreads) * n, at_label);
+            const V g = with_label<T>(piece_grad<T>(x[k], grad), item.label - c.head - (at + k * kStayThreads) * n, grad.at_label);
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_p, g), dst, (at + k * kStayThreads) * 16, 0, 0);
         }
         item = item1;
@@ -652,8 +675,13 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_parts(const T* logits, 
         const int single = j > 0 ? -1 : tid < 16 ? extra_of<T>(c, vocab) : beside_label<T>(c, without, label, 16);
         const float xe = single >= 0 ? (float)row[single] : -INFINITY;
         const auto load = [&](V (&x)[kPartBatch], int at) {
+            if ((unsigned)(without - at + tid) < (unsigned)(kPartBatch * kPartThreads)) {  // (of one batch: 1501 x 32000 bf16 26.9 us, 28.1 if of all)
 #pragma unroll
-            for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end && at + k * kPartThreads != without ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
+                for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end && at + k * kPartThreads != without ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
+                return;
+            }
+#pragma unroll
+            for (int k = 0; k < kPartBatch; ++k) x[k] = at + k * kPartThreads < end ? load_piece<V>(body + (long long)(at + k * kPartThreads) * n) : least;
         };
         V next[kPartBatch];
         load(next, p);
@@ -768,7 +796,7 @@ __device__ __forceinline__ PolicySums item_sums(const PolicyArgs& a, int m, cons
             s.loss = s.surrogate;
             if (a.ref_logp) {
                 const double far = (double)in.ref_logp - logp;
-                s.kl = w * (expm1(far) - far);
+                s.kl = w * (far == INFINITY ? far : expm1(far) - far);  // (a label that the logits forbid)
                 if (a.kl_coef != 0.f) s.loss += (double)a.kl_coef * s.kl;
             }
         }
@@ -907,23 +935,17 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     const float xe = extra >= 0 ? (float)row[extra] : 0.f, weight = a.weight[m], advantage = a.advantage[m], old_logp = a.old_logp[m];
     const float ref_logp = a.ref_logp ? a.ref_logp[m] : 0.f, own = a.own[m];  // (own, and the parts below: of a row that does not score anything)
     const Partial part = lane < parts ? partial[(long long)m * parts + lane] : Partial{-INFINITY, 0.0};
-    float base = 0.f, scale = 0.f, at_label = 0.f;
+    GradOf grad = {};
     bool some = false;  // logits that the gradient depends on
     if ((unsigned)label < (unsigned)vocab && weight != 0.f) {
         const Whole w = whole_row(part);
         const float sum = w.rest + grown_exactly(own, w.base);
         some = sum != 0.f;
-        if (some) {
-            const float d = slope(a, weight, advantage, old_logp, ref_logp, own - w.base - logf(sum));
-            base = w.base;
-            scale = -d / sum;
-            at_label = -scale * w.rest;
-        }
+        if (some) grad = grad_of(own, w.base, w.rest, sum, slope(a, weight, advantage, old_logp, ref_logp, own - w.base - logf(sum)));
     }
-    const GradOf grad = grad_of(base, scale);
     const auto put = [&](int p, const V& v) {
         V g = {};
-        if (some) g = with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, at_label);
+        if (some) g = with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, grad.at_label);
         store_piece(out + c.head + (long long)p * n, g);
     };
 #pragma unroll
@@ -931,7 +953,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
         if (begin + tid + k * kPartThreads < end) put(begin + tid + k * kPartThreads, x[k]);
 #pragma unroll 4
     for (int p = begin + tid + kHeld * kPartThreads; p < end; p += kPartThreads) put(p, load_piece<V>(body + (long long)p * n));
-    if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? at_label : scale * grown(xe, base));
+    if (extra >= 0) out[extra] = (T)(!some ? 0.f : extra == label ? grad.at_label : single_grad(xe, grad));
 }
 
 // Parts of each row of a call: 8 KB to a work-group, kMaxPartials in all.  1: rows as a whole, of which 256 and more (128 short ones) fill the card, 320
