@@ -246,8 +246,8 @@ __device__ __forceinline__ void adamw8(const alch_adamw8_tensor& t, long long be
 #pragma unroll
         for (int e = 0; e < 4; ++e) m[4 * k + e] = x[e], v[4 * k + e] = y[e];
     }
-    // b1 m and b2 v.  A power of two and a beta as one factor round as one after the other do, unless the factor leaves the normal numbers: scale bytes
-    // of 1 (of blocks that are 0, mostly), and of v beyond 2^30.
+    // b1 m and b2 v.  A power of two and a beta as one factor round as one after the other do, unless the factor leaves the normal numbers: for m with scale
+    // bytes of 1 (of blocks that are 0, mostly), for betas below a half with some more, for v with a beta below 2^-112, and beyond 2^30.
     float fm, fv = as_float((vs + 112u) << 23) * a.b2;
     if (vs == 0u) fv = 0.f;
     if (vs == 255u) fv = __builtin_nanf("");
@@ -256,7 +256,8 @@ __device__ __forceinline__ void adamw8(const alch_adamw8_tensor& t, long long be
     uint32_t codes = 0;
 #pragma unroll
     for (int k = 0; k < kWords; ++k) codes |= mc[k];
-    if (__builtin_expect(__any((ms == 1u && codes != 0u) || (vs > 142u && vs != 255u)), 0)) {
+    const float low_m = a.b1 > 0.f ? 0x1p-126f : 0.f, low_v = a.b2 > 0.f ? 0x1p-126f : 0.f;  // (0 times anything is 0)
+    if (__builtin_expect(__any((fm < low_m && codes != 0u) || (fv < low_v && vs != 0u) || (vs > 142u && vs != 255u)), 0)) {
         const float sv = scale_of(vs);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
