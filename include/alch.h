@@ -683,7 +683,8 @@ typedef struct {
  *   bits = mix((i mod 2^32) + mix(mix(seed ^ mix(step)) ^ (i >> 32)));   m takes the lower 16, v the upper 16: up where the 20 bits
  * of mantissa that a code has not, plus these 16 bits times 16, carry (values below the smallest normal code, after adding that one).
  * Results are therefore the same wherever a tensor is cut or in whatever order tensors are listed, given the numbers of its elements.
- * params as in alch_adamw_step, step (or the schedule's) also chooses the random bits, together with seed.
+ * params as in alch_adamw_step, step (or the schedule's) also chooses the random bits, together with seed; an eps between 0 and 2^-126 counts as 2^-126.
+ * The root and the quotient of the update are to one unit in the last place.
  */
 int alch_adamw8_step(int32_t n_tensors, const alch_adamw8_tensor* tensors, const alch_adamw8_tensor* tensors_host,
                      const alch_adamw* params, uint32_t seed, void* hip_stream);
