@@ -827,9 +827,9 @@ __device__ __forceinline__ void put_sums(const PolicySums& s, double (*red)[4], 
 // Thread `first` of `stride`: its items' share.
 __device__ __forceinline__ PolicySums items_sums(const PolicyArgs& a, int n, int first, int stride, float* __restrict__ logp_out) {
     PolicySums s = {};
-    for (int m = first; m < n; m += stride) {
-        const ItemIn in = load_item(a, m);
-        s.add(item_sums(a, m, in, in.own, in.sum, logp_out));
+    for (unsigned m = first; m < (unsigned)n; m += stride) {  // (n may be 2^31 - 1)
+        const ItemIn in = load_item(a, (int)m);
+        s.add(item_sums(a, (int)m, in, in.own, in.sum, logp_out));
     }
     return s;
 }
@@ -900,7 +900,7 @@ static void launch_sums(const PolicyArgs& a, int n, void* scratch, float* logp_o
         k_policy_sums<<<1, kSumThreads, 0, stream>>>(a, n, 0, 0, nullptr, logp_out, loss_out);
         return;
     }
-    const int groups = std::min((n + kSumThreads - 1) / kSumThreads, kSumGroups);
+    const int groups = (int)std::min(((long long)n + kSumThreads - 1) / kSumThreads, (long long)kSumGroups);
     const auto sums = static_cast<double(*)[4]>(scratch);
     k_policy_sums_of<<<groups, kSumThreads, 0, stream>>>(a, n, logp_out, sums);
     k_policy_sums_join<<<1, 64, 0, stream>>>(sums, groups, loss_out);
@@ -983,8 +983,8 @@ template <typename T>
 static void launch_held(const T* logits, long long ld, int rows, int vocab, const PolicyArgs& a, T* dlogits, long long ld_grad, hipStream_t stream) {
     const int pieces = vocab / Piece<T>::n + 1;
     const auto go = [&](auto kernel, int threads) {
-        for (int r = 0; r < rows; r += kGridMax)
-            kernel<<<std::min(rows - r, kGridMax), threads, 0, stream>>>(logits + r * ld, ld, vocab, a.from(r), dlogits + r * ld_grad, ld_grad);
+        for (long long r = 0; r < rows; r += kGridMax)
+            kernel<<<(int)std::min<long long>(rows - r, kGridMax), threads, 0, stream>>>(logits + r * ld, ld, vocab, a.from((int)r), dlogits + r * ld_grad, ld_grad);
     };
     if (pieces <= 256) go(k_policy_held<T, 256, 1>, 256);
     else if (pieces <= 256 * 4) go(k_policy_held<T, 256, 4>, 256);
