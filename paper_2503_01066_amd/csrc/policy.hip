@@ -5,12 +5,13 @@
 //   dx_v = d ((v == label) - exp(x_v - logz)),   d = w (-(b < u ? 0 : u) + c (1 - exp(ref - logp)))
 //
 // A row of logits is one softmax, and its gradient needs the row's sum alone: bound by memory, a row read once and written once.
-// Three kernels:
+// Four forms:
 //   held   a work-group a row, which stays in its registers between the sum and the gradient (up to 256 KB; rows longer than that also in LDS, up to
 //          400 KB; what they have beyond is read twice);
 //   stay   rows of 128 to 256 KB: a row is half of a compute unit's registers, so that no second work-group fits that could load while
 //          this one computes.  One work-group a unit stays and has the next row on its way, 9 of 16 pieces to LDS, the others to registers;
-//   parts  few rows: several work-groups share one, in two launches with the parts' sums between them.
+//   few    few rows: several work-groups share one, in two launches with the parts' sums between them;
+//   parts  the forward alone (and few rows whose parts are long): nothing is held, small work-groups go over a row, or its part, in one pass.
 // A row is summed without its label: beside a p of all but 1 (most tokens that were sampled) the others' sum r is what logp = -log(1 + r) and
 // 1 - p = r / (1 + r) are made of, and 1 + r would lose it.  The row kernels leave x_label - max and the sum of every item; the loss is made of
 // them in 64 bits by one launch, where terms of either sign cancel and a rounding of logp to fp32 would be seen.
@@ -224,10 +225,11 @@ struct GradOf {
     float base, scale, shift, log2_scale, at_label;
     uint32_t sign;
 };
-// rest: the sum of the others' exponentials, sum: with the label's (0: nothing that the gradient depends on)
-__device__ __forceinline__ GradOf grad_of(float label_logit, float base, float rest, float sum, Slope s) {
+// rest: the sum of the others' exponentials, sum: with the label's (0: nothing that the gradient depends on).  In the label's place d (1 - p) by the one of
+// its two forms that rounds the smaller part.
+__device__ __forceinline__ GradOf grad_of(float label_logit, float base, float label_part, float rest, float sum, Slope s) {
     if (sum == 0.f) s = {0.f, 0.f};
-    float scale = sum == 0.f ? 0.f : -s.d / sum, at_label = -scale * rest;  // (d (1 - p) without the difference)
+    float scale = sum == 0.f ? 0.f : -s.d / sum, at_label = label_part < rest ? fmaf(scale, label_part, s.d) : -scale * rest;
     if (__builtin_expect(s.shift != 0.f, 0)) {  // (the scale to 1 and more, so that a product is not beyond fp32 before it has to be)
         at_label = label_logit == -INFINITY ? 0.f : ldexpf(at_label, (int)s.shift);
         const int e = __builtin_amdgcn_frexp_expf(scale) - 1;
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(kThreads, kHeld <= 8 ? 6 : 4) void k_policy_held(co
     const float label_part = grown_exactly(xl, base);
     if (tid == 0) put_item<T>(a, m, xl, base, label_part, others);
     const float rest = (float)others, sum = rest + label_part;
-    const GradOf grad = grad_of(xl, base, rest, sum, slope(a, m, xl - base - logf(sum)));
+    const GradOf grad = grad_of(xl, base, label_part, rest, sum, slope(a, m, xl - base - logf(sum)));
     const auto put = [&](int p, const V& v) {
         store_piece(out + c.head + (long long)p * n, with_label<T>(piece_grad<T>(v, grad), label - c.head - p * n, grad.at_label));
     };
@@ -600,7 +602,7 @@ __global__ __launch_bounds__(kStayThreads) void k_policy_stay(const T* logits, l
         const double others = group_sum<kStayThreads>(s, red_sum);
         const float label_part = grown_exactly(xl, base);
         const float rest = (float)others, sum = rest + label_part;
-        const GradOf grad = grad_of(xl, base, rest, sum, slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, xl - base - logf(sum)));
+        const GradOf grad = grad_of(xl, base, label_part, rest, sum, slope(a, item.weight, item.advantage, item.old_logp, item.ref_logp, xl - base - logf(sum)));
         // (what is stored beside the pieces goes first: the wait above counts the last kStayPieces stores)
         if (tid == 0) put_item<T>(a, r, xl, base, label_part, others);
         if (extra >= 0) out[extra] = (T)(extra == item.label ? grad.at_label : single_grad(xe, grad));
@@ -939,9 +941,9 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part_grads(const T* log
     bool some = false;  // logits that the gradient depends on
     if ((unsigned)label < (unsigned)vocab && weight != 0.f) {
         const Whole w = whole_row(part);
-        const float sum = w.rest + grown_exactly(own, w.base);
+        const float label_part = grown_exactly(own, w.base), sum = w.rest + label_part;
         some = sum != 0.f;
-        if (some) grad = grad_of(own, w.base, w.rest, sum, slope(a, weight, advantage, old_logp, ref_logp, own - w.base - logf(sum)));
+        if (some) grad = grad_of(own, w.base, label_part, w.rest, sum, slope(a, weight, advantage, old_logp, ref_logp, own - w.base - logf(sum)));
     }
     const auto put = [&](int p, const V& v) {
         V g = {};
