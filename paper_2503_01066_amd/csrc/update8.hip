@@ -9,8 +9,8 @@
 // codes, where four bits of exponent would leave 2^7.
 //
 // Bound by memory: 16 bytes an element with a master copy (28 with fp32 moments).  The random bits are computed, 14 operations an
-// element, not read.  218 M elements with master copies: 607 us, 5.8 TB/s (1.9 times less than with fp32 moments at a copy's rate).  Without
-// master copies there are 8 bytes an element for the same arithmetic, and the vector units bound it: 4.3 to 4.6 TB/s.
+// element, not read.  218 M elements with master copies: 607 us, 5.8 TB/s (1.9 times less than with fp32 moments at a copy's rate).  In bf16 without
+// master copies there are 10 bytes an element for the same arithmetic, and the vector units bound it: 67 M elements 140 us, 4.8 TB/s.
 #include <algorithm>
 #include <float.h>
 #include <math.h>
@@ -220,7 +220,7 @@ __device__ __forceinline__ void root(const float (&v)[kPer], float (&r)[kPer]) {
 enum Kind { kAny, kBf16, kBf16Master, kF32 };
 
 // A round of 256 * kPer elements.  Eight elements a lane share more of what a block takes; where fp32 is read beside them its loads then leave
-// every other 16 bytes to the next one, so that they pay for bf16 alone (67 M elements without master copies: 191 us with four, 155 with eight).
+// every other 16 bytes to the next one, so that they pay for bf16 alone (67 M elements without master copies: 146 us with four, 140 with eight).
 template <typename T, bool kMaster, int kPer, bool kFull>
 __device__ __forceinline__ void adamw8(const alch_adamw8_tensor& t, long long begin, int elements, const Adamw8Args& a, const Rates& r) {
 #pragma clang fp contract(off)
